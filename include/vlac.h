@@ -290,6 +290,133 @@ int vlac_sparse_prefill(vlac_ctx* ctx, const float* embeds, int B, int L_v, int 
 int vlac_decode_action(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_token,
                        void* kv_cache, int32_t* out_tokens, float* out_logits, void* stream);
 
+/* ---- Pages of the cache: several continuations of one observation (beyond the paper) ----
+ *
+ * A control step may want several candidate action sequences from one prefill (sampled, ranked,
+ * decoded as chunks).  A pool of pages holds their K/V so that what they have in common is stored
+ * once and read once.  A page holds K and V of 32 consecutive positions for all layers:
+ *   [n_layers][K, V][n_kv_heads][32 * head_dim] 16-bit values, a head's 32 positions as in the cache:
+ *   K, feature 16 a + 8 g + e of position r (after the rotary embedding) at [a][g][r][e]
+ *     of [head_dim / 16][2][32][8];
+ *   V, feature 32 b + f of position 16 t + 8 i + 4 g + e at [b][t][g][f][i][e]
+ *     of [head_dim / 32][2][2][32][2][4].
+ * Position p of sequence s lies in page table[s][p / 32]; a sequence of len[s] positions holds
+ * exactly ceil(len[s] / 32) pages, the other entries of its row are -1.  refs[page] counts the
+ * table entries that name a page: 0 is free.  A page that is not full is held by one sequence only.
+ *
+ * All buffers are the caller's (device memory of the current device, contiguous); the library keeps
+ * nothing of a pool between calls and allocates nothing for it, so every call but vlac_pages_check
+ * may be captured into a graph.  Calls on one pool go to one stream or are ordered by the caller.
+ * Lists (of sequences, positions) are device int32 with n <= VLAC_PAGES_MAX_LIST entries, n = 0 is
+ * allowed and does nothing.  Entries that do not fit (index out of range, a sequence whose len or
+ * pages are out of range, a sequence listed twice where it would be changed twice) are ignored and
+ * reported by vlac_pages_check.
+ * Fresh pages are the free ones of lowest index, given out in the order of the list and of the
+ * positions.  A call that needs more than there are changes nothing and is reported by vlac_pages_check. */
+#define VLAC_PAGES_MAX_LIST 4096
+typedef struct {
+  int32_t n_layers, n_kv_heads, head_dim; /* head_dim 64 or 128 */
+  int32_t operand_dtype; /* type of the values: VLAC_OPERAND_BF16, or VLAC_OPERAND_F16 / _F16_W8 (both fp16) */
+  int32_t n_pages;       /* pages in the pool, at most 2^24 */
+  int32_t max_seqs;      /* sequences (rows of the table), at most 65536 */
+  int32_t max_pages;     /* pages per sequence (columns of the table), at most 32768 */
+  void* data;            /* n_pages * vlac_page_bytes(), 16-byte aligned */
+  int32_t* refs;         /* [n_pages] */
+  int32_t* table;        /* [max_seqs][max_pages] */
+  int32_t* len;          /* [max_seqs] */
+  int32_t* scratch;      /* vlac_pages_scratch_bytes(), zero before the first call (vlac_pages_reset does it) */
+} vlac_pages;
+
+/* Bytes of one page and of the scratch; 0 if the sizes in `pages` are not allowed (pointers are not looked at). */
+size_t vlac_page_bytes(const vlac_pages* pages);
+size_t vlac_pages_scratch_bytes(const vlac_pages* pages);
+
+/* Empties the pool: every page free, every sequence of length 0, scratch zero.  data is left as it is. */
+int vlac_pages_reset(const vlac_pages* pages, void* stream);
+
+/* Waits for `stream`, then reports what calls on this pool since the last check could not do:
+ * VLAC_E_NOMEM (a call found too few free pages), else VLAC_E_RANGE (an entry was ignored), else 0;
+ * reported once, then cleared. */
+int vlac_pages_check(const vlac_pages* pages, void* stream);
+
+/* Copies the first L positions (a prefill's) of streams 0 .. B - 1 of the context's cache into
+ * sequences seqs[0 .. B - 1] of the pool, whose shape must be the context's; what these sequences
+ * held before is released.  VLAC_E_STATE if one of the streams was never filled. */
+int vlac_pages_import(vlac_ctx* ctx, const void* kv_cache, int B, int L, const vlac_pages* pages,
+                      const int32_t* seqs, void* stream);
+
+/* For every i < n: sequence dst[i] becomes a continuation of sequence src[i]; what it held before is
+ * released.  deep = 0: the full pages are shared, a last page that is not full is copied (whole) to
+ * a fresh one.  deep != 0: every page is copied (for a sequence whose positions are rewritten in place,
+ * or whose pages must outlive the pool's other users).  A source may be listed many times, a
+ * destination once, and no destination may be a source of the same call. */
+int vlac_pages_fork(const vlac_pages* pages, const int32_t* src, const int32_t* dst, int n, int deep,
+                    void* stream);
+
+/* Makes every listed sequence `tokens` positions longer (fresh pages where they are needed; their
+ * contents are what they were) and writes the first new position to out_pos[i] (device int32 [n]),
+ * -1 for an entry that was ignored; all are -1 if there were too few pages. */
+int vlac_pages_extend(const vlac_pages* pages, const int32_t* seqs, int n, int tokens, int32_t* out_pos,
+                      void* stream);
+
+/* Writes K and V of `tokens` tokens per entry into layer `layer` of the listed sequences, at positions
+ * pos[i] .. pos[i] + tokens - 1 (vlac_pages_extend's out_pos; negative: the entry is skipped, not reported).
+ * k, v: device, 16-bit values of the pool's type, row (i, t) at element (i * tokens + t) * row_stride, in it
+ * [n_kv_heads][head_dim]; row_stride >= n_kv_heads * head_dim, a multiple of 8, the pointers 16-byte
+ * aligned (so k and v may be columns of a joint projection).  K is stored as given (the caller has applied the
+ * rotary embedding).  Positions outside the sequence, and pages that more than one sequence
+ * holds, are not written and reported.  Two entries that write the same position race. */
+int vlac_pages_append(const vlac_pages* pages, int layer, const int32_t* seqs, const int32_t* pos, int n,
+                      int tokens, const void* k, const void* v, int64_t row_stride, void* stream);
+
+/* Releases the pages of the listed sequences and sets their length to 0 (one listed twice is released once). */
+int vlac_pages_free(const vlac_pages* pages, const int32_t* seqs, int n, void* stream);
+
+/* Moves the pages in use to the front of the pool: with m pages in use, those at index m and above go, in
+ * ascending order, to the free ones below m, in ascending order; table and refs follow.  out_live
+ * (device int32 [1]) = m: pages m, m + 1, ... are free afterwards. */
+int vlac_pages_compact(const vlac_pages* pages, int32_t* out_live, void* stream);
+
+/* Attention of new tokens over pages, for a batch that shares prefixes.
+ * Query row (i, t), i < n, t < tokens, belongs to sequence seqs[i] and stands at position pos[i] + t; it sees
+ * positions 0 .. pos[i] + t:  out[i, t, h] = sum_p softmax_p(q[i, t, h] . k_p / sqrt(head_dim)) v_p, query head
+ * h on kv head floor(h n_kv_heads / n_q_heads); scores and sums in fp32 (a score beyond its range is infinite), the
+ * weights rounded to the pool's type for the product with V.
+ * Consecutive entries with the same value in group (device int32 [n]; NULL: all of them) form a group; the pages
+ * that all its tables have in common at the front and that lie wholly before every query of it are
+ * read once for the whole group.  A group is a hint: results do not depend on it but for the
+ * order of the sums.
+ *
+ * vlac_attend_plan looks at the tables once (for all layers of a pass) and leaves in the workspace how the work is cut;
+ * vlac_attend_shared runs one layer with it.  Between the two, and while passes on a workspace run, nothing else may
+ * use that workspace, and the sequences' tables must stay.
+ * An entry whose pos is negative, or that does not fit (reported), gets rows of zeros.
+ * n <= VLAC_PAGES_MAX_LIST, tokens <= 65536, n * tokens <= 2^20; n_q_heads is a multiple of n_kv_heads, at most 1024.
+ * q: device, row (i, t) at element (i * tokens + t) * q_stride, in it [n_q_heads][head_dim] values of the pool's type;
+ * q_stride >= n_q_heads * head_dim and a multiple of 8.  out: device [n, tokens, n_q_heads, head_dim], same type.
+ * workspace: device, vlac_attend_workspace_bytes (0 if the arguments are not allowed), 16-byte aligned. */
+size_t vlac_attend_workspace_bytes(const vlac_pages* pages, int n, int tokens, int n_q_heads);
+int vlac_attend_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens,
+                     int n_q_heads, const int32_t* group, void* workspace, size_t workspace_bytes,
+                     void* stream);
+int vlac_attend_shared(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q,
+                       int64_t q_stride, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* vlac_decode_action for candidates: greedy decode of n_new further tokens for n <= max_batch sequences of a pool,
+ * all of length L (imported prefills and their forks; one whose length is another is ignored and
+ * reported).  Each continues from its own first token (device int32 [n]: drawn by the caller from the
+ * prefill's logits), embedded at position L.  The sequences are extended by n_new positions and keep them (fork, decode
+ * again, or vlac_pages_free).  group: as for vlac_attend_plan.  With too few pages nothing is decoded: the
+ * sequences stay, out_tokens and out_logits are not meaningful, vlac_pages_check reports it.
+ * The pool has the context's shape; L + n_new <= max_seq.
+ * out_tokens: device int32 [n, n_new]; out_logits: device fp32 [n, n_new, vocab] or NULL.
+ * workspace: device, vlac_candidates_workspace_bytes, 16-byte aligned. */
+size_t vlac_candidates_workspace_bytes(const vlac_ctx* ctx, const vlac_pages* pages, int n);
+int vlac_decode_candidates(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L,
+                           const int32_t* group, int n_new, const int32_t* first_token,
+                           int32_t* out_tokens, float* out_logits, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,13 @@ class LayerW(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("wqkv", "wo", "w_gate_up", "w_down", "g_attn", "g_ffn")]
 
 
+class Pages(C.Structure):
+    """vlac_pages; made by `pages` or `new_pages`, which keep the tensors alive."""
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_kv_heads", "head_dim", "operand_dtype",
+                                         "n_pages", "max_seqs", "max_pages")] + [
+        (n, C.c_void_p) for n in ("data", "refs", "table", "len", "scratch")]
+
+
 _PATH = os.path.join(_HERE, "libvlac.so")
 _LOADED = {}
 
@@ -92,6 +99,29 @@ def lib():
         L.vlac_layer_ratio.argtypes = [vp, vp, i32, i32, f32, vp, vp, vp, vp]
         L.vlac_sparse_prefill.argtypes = [vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
         L.vlac_decode_action.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
+        pp, sz, i64 = C.POINTER(Pages), C.c_size_t, C.c_int64
+        for name in ("vlac_page_bytes", "vlac_pages_scratch_bytes"):
+            getattr(L, name).argtypes = [pp]
+            getattr(L, name).restype = sz
+        L.vlac_pages_reset.argtypes = [pp, vp]
+        L.vlac_pages_check.argtypes = [pp, vp]
+        L.vlac_pages_import.argtypes = [vp, vp, i32, i32, pp, vp, vp]
+        L.vlac_pages_fork.argtypes = [pp, vp, vp, i32, i32, vp]
+        L.vlac_pages_extend.argtypes = [pp, vp, i32, i32, vp, vp]
+        L.vlac_pages_append.argtypes = [pp, i32, vp, vp, i32, i32, vp, vp, i64, vp]
+        L.vlac_pages_free.argtypes = [pp, vp, i32, vp]
+        L.vlac_pages_compact.argtypes = [pp, vp, vp]
+        L.vlac_attend_workspace_bytes.argtypes = [pp, i32, i32, i32]
+        L.vlac_attend_workspace_bytes.restype = sz
+        L.vlac_attend_plan.argtypes = [pp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.vlac_attend_shared.argtypes = [pp, i32, i32, i32, i32, vp, i64, vp, vp, sz, vp]
+        L.vlac_candidates_workspace_bytes.argtypes = [vp, pp, i32]
+        L.vlac_candidates_workspace_bytes.restype = sz
+        L.vlac_decode_candidates.argtypes = [vp, pp, vp, i32, i32, vp, i32, vp, vp, vp, vp, sz, vp]
+        for name in ("vlac_pages_reset", "vlac_pages_check", "vlac_pages_import", "vlac_pages_fork", "vlac_pages_extend",
+                     "vlac_pages_append", "vlac_pages_free", "vlac_pages_compact", "vlac_attend_plan",
+                     "vlac_attend_shared", "vlac_decode_candidates"):
+            getattr(L, name).restype = i32
         for name in ("vlac_create", "vlac_destroy", "vlac_last_hip_error", "vlac_set_layer_weights",
                      "vlac_set_head_weights", "vlac_reset_stream", "vlac_check",
                      "vlac_profile_select", "vlac_profile_read", "vlac_profile_read2",
@@ -322,3 +352,199 @@ def vlac_decode_action(ctx, B, L, n_new, first_token, kv_cache, out_tokens, out_
         _ptr(kv_cache, None, "kv_cache"), _ptr(out_tokens, torch.int32, "out_tokens"),
         _ptr(out_logits, torch.float32, "out_logits"), _stream(stream))
     return _ret(st, "vlac_decode_action", check)
+
+
+# ---- pages of the cache, and attention over them ----
+#
+# These calls run on the pool's device, whatever the current one is (stream=None: that device's
+# current stream), and check every tensor they are given: device, type, size, contiguity.
+
+def pages(n_layers, n_kv_heads, head_dim, operand_dtype, data, refs, table, length, scratch=None):
+    """The vlac_pages over the caller's GPU tensors: data (any 16-bit or byte type, a whole number of pages),
+    refs int32 [n_pages], table int32 [max_seqs, max_pages], length int32 [max_seqs]; the scratch is
+    allocated (zero) if it is not given."""
+    import torch
+    p = Pages(n_layers, n_kv_heads, head_dim, operand_dtype, refs.numel(), table.shape[0], table.shape[1])
+    bytes_, words = int(lib().vlac_page_bytes(C.byref(p))), int(lib().vlac_pages_scratch_bytes(C.byref(p))) // 4
+    if bytes_ == 0:
+        raise VlacError(VLAC_E_SHAPE, "vlac_pages: sizes that no pool may have")
+    if scratch is None:
+        scratch = torch.zeros(words, dtype=torch.int32, device=refs.device)
+    if data.numel() * data.element_size() != bytes_ * p.n_pages:
+        raise ValueError("data holds %d bytes, %d pages take %d" % (data.numel() * data.element_size(), p.n_pages,
+                                                                    bytes_ * p.n_pages))
+    if length.numel() != p.max_seqs or scratch.numel() < words or table.dim() != 2:
+        raise ValueError("table [max_seqs, max_pages], length [max_seqs], scratch of vlac_pages_scratch_bytes")
+    i32 = torch.int32
+    p.device = refs.device
+    p.tensors = (data, refs, table, length, scratch)
+    for x in p.tensors:
+        _on(p, x)
+    p.data, p.refs, p.table = _ptr(data, None, "data"), _ptr(refs, i32, "refs"), _ptr(table, i32, "table")
+    p.len, p.scratch = _ptr(length, i32, "length"), _ptr(scratch, i32, "scratch")
+    return p
+
+
+def new_pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, max_pages, device="cuda"):
+    """An empty pool in new tensors on `device`."""
+    import torch
+    p = Pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, max_pages)
+    size = int(lib().vlac_page_bytes(C.byref(p)))
+    if size == 0:
+        raise VlacError(VLAC_E_SHAPE, "vlac_pages: sizes that no pool may have")
+    i32 = dict(dtype=torch.int32, device=device)
+    made = pages(n_layers, n_kv_heads, head_dim, operand_dtype,
+                 torch.empty((n_pages, size), dtype=torch.uint8, device=device), torch.empty(n_pages, **i32),
+                 torch.empty((max_seqs, max_pages), **i32), torch.empty(max_seqs, **i32))
+    vlac_pages_reset(made)
+    return made
+
+
+def _on(p, x):
+    """x if it lies on the pool's device."""
+    dev = getattr(p, "device", None)
+    if x is not None and not isinstance(x, int) and dev is not None and x.device != dev:
+        raise ValueError("a tensor on %s for a pool on %s" % (x.device, dev))
+    return x
+
+
+def _list(p, x, n, name):
+    """Pointer of an int32 list of n entries on the pool's device."""
+    import torch
+    _sized(x, n, name)
+    return _ptr(_on(p, x), torch.int32, name)
+
+
+def _sized(x, n, name):
+    if x is not None and not isinstance(x, int) and x.numel() < n:
+        raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
+
+
+def _rows(p, x, n, tokens, heads, name):
+    """Pointer and row stride of values [n, tokens, heads, head_dim] (the last two dimensions dense, the rows
+    equally far apart), or [n * tokens, heads * head_dim]."""
+    import torch
+    want = torch.bfloat16 if p.operand_dtype == OPERAND_BF16 else torch.float16
+    if x is None or isinstance(x, int):
+        return x, heads * p.head_dim
+    _on(p, x)
+    if not x.is_cuda:
+        raise ValueError("%s must live in GPU memory" % name)
+    if x.dtype != want:
+        raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, want))
+    width = heads * p.head_dim
+    if x.numel() != n * tokens * width:
+        raise ValueError("%s holds %d values, expected %d x %d x %d" % (name, x.numel(), n, tokens, width))
+    try:
+        y = x.view(n * tokens, width)   # (a view exists if the rows are equally far apart and dense)
+    except RuntimeError:
+        raise ValueError("%s: rows must be dense and equally far apart" % name) from None
+    if width > 1 and y.shape[0] and y.stride(1) != 1:
+        raise ValueError("%s: rows must be dense" % name)
+    return y.data_ptr(), (y.stride(0) if y.shape[0] > 1 else width)
+
+
+def _call(p, name, stream, check, *args):
+    """One library call on the pool's device."""
+    import torch
+    fn = getattr(lib(), name)
+    dev = getattr(p, "device", None)
+    if dev is None or dev.type != "cuda":
+        return _ret(fn(*args, _stream(stream)), name, check)
+    with torch.cuda.device(dev):
+        return _ret(fn(*args, _stream(stream)), name, check)
+
+
+def _ref(p):
+    return C.byref(p) if p is not None else None
+
+
+def vlac_page_bytes(p):
+    return int(lib().vlac_page_bytes(_ref(p)))
+
+
+def vlac_pages_scratch_bytes(p):
+    return int(lib().vlac_pages_scratch_bytes(_ref(p)))
+
+
+def vlac_pages_reset(p, stream=None, check=True):
+    return _call(p, "vlac_pages_reset", stream, check, _ref(p))
+
+
+def vlac_pages_check(p, stream=None, check=True):
+    return _call(p, "vlac_pages_check", stream, check, _ref(p))
+
+
+def vlac_pages_import(ctx, kv_cache, B, L, p, seqs, stream=None, check=True):
+    return _call(p, "vlac_pages_import", stream, check, ctx, _ptr(_on(p, kv_cache), None, "kv_cache"), B, L, _ref(p),
+                 _list(p, seqs, B, "seqs"))
+
+
+def vlac_pages_fork(p, src, dst, n, deep=False, stream=None, check=True):
+    return _call(p, "vlac_pages_fork", stream, check, _ref(p), _list(p, src, n, "src"), _list(p, dst, n, "dst"), n,
+                 1 if deep else 0)
+
+
+def vlac_pages_extend(p, seqs, n, tokens, out_pos, stream=None, check=True):
+    return _call(p, "vlac_pages_extend", stream, check, _ref(p), _list(p, seqs, n, "seqs"), n, tokens,
+                 _list(p, out_pos, n, "out_pos"))
+
+
+def vlac_pages_append(p, layer, seqs, pos, n, tokens, k, v, stream=None, check=True):
+    """k, v: [n, tokens, n_kv_heads, head_dim] of the pool's type; slices of a joint projection have one row stride."""
+    kp, ks = _rows(p, k, n, tokens, p.n_kv_heads, "k")
+    vp, vs = _rows(p, v, n, tokens, p.n_kv_heads, "v")
+    if ks != vs:
+        raise ValueError("k and v: rows %d and %d values apart" % (ks, vs))
+    return _call(p, "vlac_pages_append", stream, check, _ref(p), layer, _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"),
+                 n, tokens, kp, vp, ks)
+
+
+def vlac_pages_free(p, seqs, n, stream=None, check=True):
+    return _call(p, "vlac_pages_free", stream, check, _ref(p), _list(p, seqs, n, "seqs"), n)
+
+
+def vlac_pages_compact(p, out_live, stream=None, check=True):
+    return _call(p, "vlac_pages_compact", stream, check, _ref(p), _list(p, out_live, 1, "out_live"))
+
+
+def vlac_attend_workspace_bytes(p, n, tokens, n_q_heads):
+    return int(lib().vlac_attend_workspace_bytes(_ref(p), n, tokens, n_q_heads))
+
+
+def _workspace(p, ws):
+    """Pointer and bytes of a workspace tensor."""
+    if ws is None:
+        return None, 0
+    return _ptr(_on(p, ws), None, "workspace"), ws.numel() * ws.element_size()
+
+
+def vlac_attend_plan(p, seqs, pos, n, tokens, n_q_heads, group, workspace, stream=None, check=True):
+    ws, size = _workspace(p, workspace)
+    return _call(p, "vlac_attend_plan", stream, check, _ref(p), _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n, tokens,
+                 n_q_heads, _list(p, group, n, "group"), ws, size)
+
+
+def vlac_attend_shared(p, layer, n, tokens, n_q_heads, q, out, workspace, stream=None, check=True):
+    """q: [n, tokens, n_q_heads, head_dim] of the pool's type, rows equally far apart; out the same, contiguous."""
+    qp, qs = _rows(p, q, n, tokens, n_q_heads, "q")
+    op, stride = _rows(p, out, n, tokens, n_q_heads, "out")
+    if out is not None and not isinstance(out, int) and not out.is_contiguous():
+        raise ValueError("out must be contiguous")
+    ws, size = _workspace(p, workspace)
+    return _call(p, "vlac_attend_shared", stream, check, _ref(p), layer, n, tokens, n_q_heads, qp, qs, op, ws, size)
+
+
+def vlac_candidates_workspace_bytes(ctx, p, n):
+    return int(lib().vlac_candidates_workspace_bytes(ctx, _ref(p), n))
+
+
+def vlac_decode_candidates(ctx, p, seqs, n, L, group, n_new, first_token, out_tokens, out_logits, workspace, stream=None,
+                           check=True):
+    import torch
+    _sized(out_tokens, n * n_new, "out_tokens")
+    ws, size = _workspace(p, workspace)
+    return _call(p, "vlac_decode_candidates", stream, check, ctx, _ref(p), _list(p, seqs, n, "seqs"), n, L,
+                 _list(p, group, n, "group"), n_new, _list(p, first_token, n, "first_token"),
+                 _ptr(_on(p, out_tokens), torch.int32, "out_tokens"), _ptr(_on(p, out_logits), torch.float32, "out_logits"),
+                 ws, size)

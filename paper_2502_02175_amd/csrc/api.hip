@@ -8,6 +8,7 @@
 #include <new>
 
 #include "common.h"
+#include "pages.h"
 
 namespace {
 
@@ -508,6 +509,32 @@ int vlac_layer_ratio(vlac_ctx* ctx, const float* attn_mean, int B, int L_v, floa
 
 namespace {
 
+// A decode pass over pages (vlac_decode_candidates): row i is sequence seqs[i] of a pool at position pos[i] + add.  The
+// QKV projection writes the new K and V into tiles of their own, one per row and kv head and 32 positions long (`tiles`, in
+// the place of the stream cache, whose layout the projections know), from where they go into the pages.
+struct PagePath {
+  PoolView p;
+  const int *seqs, *pos;
+  int add, n;
+  bf16_t* tiles;
+  void* ws;
+};
+
+void kv_into_tiles(const vlac_ctx* c, const PagePath& pg, int pos, GemmEpi& e) {
+  const vlac_model_cfg& m = c->cfg;
+  const size_t tile = (size_t)kPage * m.head_dim;
+  e.max_seq = kPage;
+  e.kv_layer_off = 0;
+  e.kv_stream_stride = 2 * m.n_kv_heads * tile;
+  e.kv = pg.tiles - (size_t)(pos / kPage) * tile;  // (all rows stand at `pos`: in the first tile of each head)
+}
+
+void attend_pages(vlac_ctx* c, const PagePath& pg, int layer, hipStream_t st) {
+  launch_append_tiles(pg.p, layer, pg.seqs, pg.pos, pg.add, pg.n, pg.tiles, st);
+  const AttendIo io = {c->qbuf, -1, c->xa, c->kpad_q / 16};
+  launch_attend(pg.p, c->f16, layer, pg.n, 1, c->cfg.n_q_heads, io, pg.ws, st);
+}
+
 // One decoder layer over the rows of plane `rows` (count *n_rows <= rows_cap).
 // n_host >= 0: the row count is known on the host; decode_pos >= 0: the rows are
 // (stream b, position decode_pos) for b < n_host, and the row lists are not read.
@@ -517,7 +544,7 @@ namespace {
 void run_layer(vlac_ctx* c, int layer, int B, int rows_cap, int rows_cap_per_stream, int L_v, int L_t,
                const float* resid_in, int resid_stride, const int* rows, const int* n_rows,
                int n_host, int decode_pos, const int* slot_off, const int* prev_slot, bf16_t* kv,
-               float* out_attn_mean, int* pending, hipStream_t st) {
+               float* out_attn_mean, int* pending, hipStream_t st, const PagePath* pg = nullptr) {
   const vlac_model_cfg& m = c->cfg;
   const LayerW& W = c->layers[layer];
   GemmEpi e;
@@ -531,6 +558,7 @@ void run_layer(vlac_ctx* c, int layer, int B, int rows_cap, int rows_cap_per_str
   e.kv_layer_off = (size_t)layer * 2 * m.n_kv_heads * m.max_seq * m.head_dim;
   e.n_q_heads = m.n_q_heads; e.n_kv_heads = m.n_kv_heads; e.head_dim = m.head_dim;
   e.max_seq = m.max_seq;
+  if (pg) kv_into_tiles(c, *pg, decode_pos, e);
   e.h = c->h; e.h_seq_stride = m.max_seq; e.d_model = m.d_model;
   e.rpart = c->rpart; e.rpart_rows = rows_cap;
   e.xf = c->xf; e.kc_f = c->kpad_f / 16; e.d_ffn = m.d_ffn;
@@ -545,8 +573,10 @@ void run_layer(vlac_ctx* c, int layer, int B, int rows_cap, int rows_cap_per_str
                         W.g_attn, m.rms_eps, m.d_model, c->xa, kc_d, st);
   launch_gemm(c, EPI_QKV, W.wqkv, W.s_qkv, c->qkv_dim / 32, c->kpad_d, c->xa, n_rows, n_host, rows_cap, e, st);
   *pending = 0;
-  launch_attention(c, layer, B, rows_cap_per_stream, L_v, L_t, rows, slot_off, decode_pos, kv,
-                   out_attn_mean, st);
+  if (pg) attend_pages(c, *pg, layer, st);
+  else
+    launch_attention(c, layer, B, rows_cap_per_stream, L_v, L_t, rows, slot_off, decode_pos, kv,
+                     out_attn_mean, st);
   e.resid_src = resid_in; e.resid_seq_stride = resid_stride;
   const int s_o = launch_gemm(c, EPI_RESID, W.wo, W.s_o, m.d_model / 32, c->kpad_q, c->xa, n_rows, n_host,
                               rows_cap, e, st);
@@ -599,7 +629,7 @@ NormIn decode_norm(vlac_ctx* c, int B, DecodeResid& r, const float* gain, bool k
 // every RMSNorm is fused into the GEMM that follows it, and the two projections with a
 // residual leave their split-K partial rows to the next norm (no hand-over inside them).
 void run_layer_decode(vlac_ctx* c, int layer, int B, int pos, bf16_t* kv, DecodeResid& r,
-                      hipStream_t st) {
+                      hipStream_t st, const PagePath* pg) {
   const vlac_model_cfg& m = c->cfg;
   const LayerW& W = c->layers[layer];
   GemmEpi e;
@@ -612,6 +642,7 @@ void run_layer_decode(vlac_ctx* c, int layer, int B, int pos, bf16_t* kv, Decode
   e.kv_layer_off = (size_t)layer * 2 * m.n_kv_heads * m.max_seq * m.head_dim;
   e.n_q_heads = m.n_q_heads; e.n_kv_heads = m.n_kv_heads; e.head_dim = m.head_dim;
   e.max_seq = m.max_seq;
+  if (pg) kv_into_tiles(c, *pg, pos, e);
   e.d_model = m.d_model;
   e.h_compact = 1; e.h_seq_stride = 1; e.resid_seq_stride = 1;
   e.rpart = c->rpart; e.rpart_rows = B;
@@ -619,7 +650,8 @@ void run_layer_decode(vlac_ctx* c, int layer, int B, int pos, bf16_t* kv, Decode
 
   NormIn n = decode_norm(c, B, r, W.g_attn, true);
   launch_gemm(c, EPI_QKV, W.wqkv, W.s_qkv, c->qkv_dim / 32, c->kpad_d, c->xa, nullptr, B, B, e, st, &n);
-  launch_attention(c, layer, B, 1, 0, 0, nullptr, nullptr, pos, kv, nullptr, st);
+  if (pg) attend_pages(c, *pg, layer, st);
+  else launch_attention(c, layer, B, 1, 0, 0, nullptr, nullptr, pos, kv, nullptr, st);
   float* hrow = c->hdec + (size_t)r.cur * m.max_batch * m.d_model;
   e.resid_src = hrow; e.h = hrow;
   const int s_o = launch_gemm(c, EPI_RESID, W.wo, W.s_o, m.d_model / 32, c->kpad_q, c->xa, nullptr, B, B, e, st);
@@ -655,6 +687,54 @@ void run_head(vlac_ctx* c, int B, int pos, float* logits, size_t logits_stride, 
     launch_gemm(c, EPI_LOGITS, c->w_head, c->s_head, m.vocab / 32, c->kpad_d, c->xa, nullptr, B, B, e, st);
   }
   launch_argmax(c->head_best, B, m.vocab, out_token, out_stride, next, st);
+}
+
+// n_new decode passes over B rows at positions L, L + 1, ...: streams of the cache, or sequences of a pool
+void decode_passes(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_token, bf16_t* kv, int32_t* out_tokens,
+                   float* out_logits, PagePath* pg, hipStream_t st, const int* group = nullptr) {
+  const vlac_model_cfg& m = ctx->cfg;
+  const int ms = m.max_seq;
+  const bool fused = gemm_can_fuse_norm(B, L, ctx->kpad_d) && ctx->rpart_floats >= (size_t)8 * B * m.d_model;
+  if (!fused) launch_decode_plan(ctx, B, L, n_new, st);
+  for (int t = 0; t < n_new; ++t) {
+    float* logits = out_logits ? out_logits + (size_t)t * m.vocab : ctx->logits;
+    const size_t lstride = out_logits ? (size_t)n_new * m.vocab : (size_t)m.vocab;
+    // (the residual rows of every later pass are written by the argmax of the pass before it)
+    const bool more = t + 1 < n_new;
+    if (pg) {
+      pg->add = t;
+      launch_attend_plan(pg->p, pg->seqs, pg->pos, t, B, 1, m.n_q_heads, group, pg->ws, st);
+    }
+    if (fused) {
+      // rows (b, 0) of a [max_batch, 1, d] plane: the first residual row set
+      if (t == 0) launch_embed_rows(ctx->embed, first_token, B, m.d_model, m.vocab, ctx->hdec, 1, 0, st);
+      const NextEmbed next = {ctx->embed, m.d_model, more ? ctx->hdec : nullptr, 1, 0};
+      DecodeResid r = {0, 0};
+      for (int l = 0; l < m.n_layers; ++l)
+        run_layer_decode(ctx, l, B, L + t, kv, r, st, pg);
+      const NormIn n = decode_norm(ctx, B, r, ctx->g_final, false);
+      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st, &n);
+    } else {
+      // More than 4 streams: the general layer pass over the rows (b, L + t).  With more than
+      // 32 of them the prefill's GEMM and row kernels serve the pass, and those read the row
+      // list (only the few-rows kernels derive a row from decode_pos): plane t of the decode
+      // row lists.  Their projections with a residual may leave split-K partial rows
+      // (`pending`), which the next layer's first row kernel adds up, and after the last
+      // layer a row kernel without a norm.
+      if (t == 0) launch_embed_rows(ctx->embed, first_token, B, m.d_model, m.vocab, ctx->h, ms, L, st);
+      const NextEmbed next = {ctx->embed, m.d_model, more ? ctx->h : nullptr, ms, L + t + 1};
+      const int* drows = ctx->dec_rows + (size_t)t * m.max_batch;
+      int pending = 0;
+      for (int l = 0; l < m.n_layers; ++l)
+        run_layer(ctx, l, B, B, 1, 0, 0, ctx->h, ms, drows, nullptr, B, L + t, nullptr, nullptr,
+                  kv, nullptr, &pending, st, pg);
+      if (pending)
+        launch_resid_norm_rows(ctx->f16, ctx->h, ms, ctx->rpart, pending, B, ctx->h, ms, drows, nullptr,
+                               nullptr, B, B, nullptr, m.rms_eps, m.d_model, ctx->xa, ctx->kpad_d / 16,
+                               st, &ctx->pending_adapt);
+      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st);
+    }
+  }
 }
 
 int weights_ready(const vlac_ctx* c) {
@@ -733,45 +813,49 @@ int vlac_decode_action(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* fi
   for (int b = 0; b < B; ++b)
     if (!ctx->filled[b]) return VLAC_E_STATE;
   if (n_new == 0) return VLAC_OK;
+  decode_passes(ctx, B, L, n_new, first_token, (bf16_t*)kv_cache, out_tokens, out_logits, nullptr, (hipStream_t)stream);
+  VLAC_HIP(hipGetLastError());
+  return VLAC_OK;
+}
+
+// workspace of vlac_decode_candidates: positions, tiles of the new K and V, then the attention's
+static size_t candidates_pos_bytes(int n) { return ((size_t)n * sizeof(int) + 255) / 256 * 256; }
+static size_t candidates_tile_bytes(const vlac_ctx* ctx, int n) {
+  return (size_t)n * 2 * ctx->cfg.n_kv_heads * kPage * ctx->cfg.head_dim * sizeof(bf16_t);
+}
+static bool pool_fits(const vlac_ctx* ctx, const vlac_pages* p) {
+  const vlac_model_cfg& m = ctx->cfg;
+  return p->n_layers == m.n_layers && p->n_kv_heads == m.n_kv_heads && p->head_dim == m.head_dim && pages_f16(p) == ctx->f16;
+}
+
+size_t vlac_candidates_workspace_bytes(const vlac_ctx* ctx, const vlac_pages* pages, int n) {
+  if (!ctx || check_pages(pages, false) != VLAC_OK || !pool_fits(ctx, pages) || n < 0 || n > ctx->cfg.max_batch) return 0;
+  const size_t att = vlac_attend_workspace_bytes(pages, n, 1, ctx->cfg.n_q_heads);
+  return att ? candidates_pos_bytes(n) + candidates_tile_bytes(ctx, n) + att : 0;
+}
+
+int vlac_decode_candidates(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L,
+                           const int32_t* group, int n_new, const int32_t* first_token, int32_t* out_tokens,
+                           float* out_logits, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!ctx) return VLAC_E_NULL;
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  const vlac_model_cfg& m = ctx->cfg;
+  if (n < 0 || n > m.max_batch || n > VLAC_PAGES_MAX_LIST || L < 1 || n_new < 0) return VLAC_E_RANGE;
+  if (!pool_fits(ctx, pages) || (long)L + n_new > m.max_seq || (long)L + n_new > (long)pages->max_pages * kPage) return VLAC_E_SHAPE;
+  if (n == 0 || n_new == 0) return VLAC_OK;
+  if (!seqs || !first_token || !out_tokens || !workspace) return VLAC_E_NULL;
+  if ((uintptr_t)workspace % 16) return VLAC_E_SHAPE;
+  const size_t need = vlac_candidates_workspace_bytes(ctx, pages, n);
+  if (need == 0 || workspace_bytes < need) return VLAC_E_RANGE;
+  if (!weights_ready(ctx)) return VLAC_E_STATE;
   hipStream_t st = (hipStream_t)stream;
-  const int ms = m.max_seq;
-  const bool fused = gemm_can_fuse_norm(B, L, ctx->kpad_d) && ctx->rpart_floats >= (size_t)8 * B * m.d_model;
-  if (!fused) launch_decode_plan(ctx, B, L, n_new, st);
-  for (int t = 0; t < n_new; ++t) {
-    float* logits = out_logits ? out_logits + (size_t)t * m.vocab : ctx->logits;
-    const size_t lstride = out_logits ? (size_t)n_new * m.vocab : (size_t)m.vocab;
-    // (the residual rows of every later pass are written by the argmax of the pass before it)
-    const bool more = t + 1 < n_new;
-    if (fused) {
-      // rows (b, 0) of a [max_batch, 1, d] plane: the first residual row set
-      if (t == 0) launch_embed_rows(ctx->embed, first_token, B, m.d_model, m.vocab, ctx->hdec, 1, 0, st);
-      const NextEmbed next = {ctx->embed, m.d_model, more ? ctx->hdec : nullptr, 1, 0};
-      DecodeResid r = {0, 0};
-      for (int l = 0; l < m.n_layers; ++l)
-        run_layer_decode(ctx, l, B, L + t, (bf16_t*)kv_cache, r, st);
-      const NormIn n = decode_norm(ctx, B, r, ctx->g_final, false);
-      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st, &n);
-    } else {
-      // More than 4 streams: the general layer pass over the rows (b, L + t).  With more than
-      // 32 of them the prefill's GEMM and row kernels serve the pass, and those read the row
-      // list (only the few-rows kernels derive a row from decode_pos): plane t of the decode
-      // row lists.  Their projections with a residual may leave split-K partial rows
-      // (`pending`), which the next layer's first row kernel adds up, and after the last
-      // layer a row kernel without a norm.
-      if (t == 0) launch_embed_rows(ctx->embed, first_token, B, m.d_model, m.vocab, ctx->h, ms, L, st);
-      const NextEmbed next = {ctx->embed, m.d_model, more ? ctx->h : nullptr, ms, L + t + 1};
-      const int* drows = ctx->dec_rows + (size_t)t * m.max_batch;
-      int pending = 0;
-      for (int l = 0; l < m.n_layers; ++l)
-        run_layer(ctx, l, B, B, 1, 0, 0, ctx->h, ms, drows, nullptr, B, L + t, nullptr, nullptr,
-                  (bf16_t*)kv_cache, nullptr, &pending, st);
-      if (pending)
-        launch_resid_norm_rows(ctx->f16, ctx->h, ms, ctx->rpart, pending, B, ctx->h, ms, drows, nullptr,
-                               nullptr, B, B, nullptr, m.rms_eps, m.d_model, ctx->xa, ctx->kpad_d / 16,
-                               st, &ctx->pending_adapt);
-      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st);
-    }
-  }
+  char* ws = (char*)workspace;
+  int* pos = (int*)ws;
+  PagePath pg = {pool_view(pages), seqs, pos, 0, n, (bf16_t*)(ws + candidates_pos_bytes(n)),
+                 ws + candidates_pos_bytes(n) + candidates_tile_bytes(ctx, n)};
+  launch_extend(pg.p, seqs, n, n_new, L, pos, st);
+  decode_passes(ctx, n, L, n_new, first_token, nullptr, out_tokens, out_logits, &pg, st, group);
   VLAC_HIP(hipGetLastError());
   return VLAC_OK;
 }

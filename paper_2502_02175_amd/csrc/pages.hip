@@ -1,0 +1,558 @@
+// Pages of the cache: forking, growing, releasing and compacting sequences, writing new tokens, and taking
+// over a prefill.  No arithmetic: integers of the tables, and values that are copied bit for bit.
+//
+// The state of the allocator is refs alone (0 = free), so which pages a call takes is a function of the state and
+// the list: the free pages in ascending order, entry by entry.  One workgroup works that out (ranks by
+// prefix sums, no order of atomics decides anything); the pages themselves are copied by a second
+// launch over the whole chip, from a list in the pool's scratch.
+#include <algorithm>
+
+#include "pages.h"
+
+namespace {
+
+constexpr int kPlan = 1024;  // threads of a planning workgroup
+
+// refs change by atomics, which go to the L2: read them there (this CU's L1 may hold what was before)
+__device__ inline int ld_agent(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Everything before it is done for every thread of the workgroup
+__device__ inline void meet() {
+  stores_done();
+  __syncthreads();
+}
+
+// Sum over the workgroup's threads before this one; *total: over all of them.  sums: [kPlan / 64 + 1] words of LDS
+__device__ inline int scan_before(int x, int* sums, int* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int run = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(run, d);
+    if (lane >= d) run += y;
+  }
+  if (lane == 63) sums[w] = run;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    int s = lane < kPlan / 64 ? sums[lane] : 0;
+    const int mine = s;
+#pragma unroll
+    for (int d = 1; d < kPlan / 64; d <<= 1) {
+      const int y = __shfl_up(s, d);
+      if (lane >= d) s += y;
+    }
+    if (lane < kPlan / 64) sums[lane] = s - mine;
+    if (lane == kPlan / 64 - 1) sums[kPlan / 64] = s;
+  }
+  __syncthreads();
+  const int before = sums[w] + run - x;
+  *total = sums[kPlan / 64];
+  __syncthreads();
+  return before;
+}
+
+// The free pages of lowest index, ascending, to out[0 .. most): -> how many there are (at most `most` are looked for)
+__device__ int lowest_free(const PoolView& p, int most, int* out, int* sums) {
+  int found = 0;
+  for (int base = 0; base < p.n_pages && found < most; base += 4 * kPlan) {
+    const int at = base + 4 * (int)threadIdx.x;
+    int mine = 0, bits = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (at + e < p.n_pages && ld_agent(p.refs + at + e) == 0) {
+        bits |= 1 << e;
+        ++mine;
+      }
+    int total;
+    int rank = found + scan_before(mine, sums, &total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (bits >> e & 1) {
+        if (rank < most) out[rank] = at + e;
+        ++rank;
+      }
+    found += total;
+  }
+  return min(found, most);
+}
+
+enum { FORK, EXTEND, IMPORT };
+
+struct PlanArgs {
+  PoolView p;
+  const int *src, *dst;  // dst: the sequences that change
+  int n, tokens, deep, want_len;
+  int* out_pos;
+};
+
+// What entry i asks for.  dst < 0: the entry is ignored.
+struct Entry {
+  int dst, src, held, pages, fresh, len;  // pages it holds before (and loses), pages after, fresh ones, length of the source
+};
+
+template <int MODE>
+__device__ Entry entry_of(const PlanArgs& a, int i) {
+  const PoolView& p = a.p;
+  Entry e = {-1, 0, 0, 0, 0, 0};
+  const int d = a.dst[i];
+  const int ld = checked_len(p, d);
+  if (ld < 0 || ld_agent(p.is_dst() + d) != a.n - i) return e;  // (only the first entry of a sequence counts)
+  if (MODE == FORK) {
+    e.src = a.src[i];
+    e.len = checked_len(p, e.src);
+    if (e.len < 0 || ld_agent(p.is_src() + d) != 0) return e;
+    e.held = pages_of(ld);
+    e.pages = pages_of(e.len);
+    e.fresh = a.deep ? e.pages : (e.len % kPage != 0);
+  } else if (MODE == EXTEND) {
+    if ((long long)ld + a.tokens > (long long)p.max_pages * kPage || (a.want_len >= 0 && ld != a.want_len)) return e;
+    e.len = ld;
+    e.held = pages_of(ld);
+    e.pages = pages_of(ld + a.tokens);
+    e.fresh = e.pages - e.held;
+  } else {
+    e.len = a.tokens;
+    e.held = pages_of(ld);
+    e.pages = e.fresh = pages_of(a.tokens);
+  }
+  e.dst = d;
+  return e;
+}
+
+// One workgroup.  Everything or nothing: the destinations' pages are released, the fresh pages looked for, and if
+// they do not suffice the release is taken back.
+template <int MODE>
+__global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
+  __shared__ int sums[kPlan / 64 + 1];
+  __shared__ int first[kPlan];  // first fresh page (in copy_dst) of the entries of a round
+  const PoolView& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int* const fresh_pages = p.copy_dst();
+
+  for (int i = tid; i < a.n; i += kPlan) {
+    const int d = a.dst[i];
+    if ((unsigned)d < (unsigned)p.max_seqs) atomicMax(p.is_dst() + d, a.n - i);
+    if (MODE == FORK) {
+      const int s = a.src[i];
+      if ((unsigned)s < (unsigned)p.max_seqs) atomicOr(p.is_src() + s, 1);
+    }
+  }
+  meet();
+
+  int need = 0;
+  bool bad = false;
+  for (int i = tid; i < a.n; i += kPlan) {
+    const Entry e = entry_of<MODE>(a, i);
+    bad |= e.dst < 0;
+    need += e.fresh;
+  }
+  if (bad) report(p, PAGES_BAD_ENTRY);
+  // (by `by` = -1 released, by +1 taken back)
+  auto release = [&](int by) {
+    for (int i = w; i < a.n; i += kPlan / 64) {
+      const Entry e = entry_of<MODE>(a, i);
+      if (e.dst < 0) continue;
+      for (int j = lane; j < e.held; j += 64) {
+        const int pg = p.table[(size_t)e.dst * p.max_pages + j];
+        if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, by);
+      }
+    }
+  };
+  if (MODE != EXTEND) release(-1);
+  meet();
+  int want;
+  (void)scan_before(need, sums, &want);
+  const int found = want > 0 ? lowest_free(p, min(want, p.n_pages), fresh_pages, sums) : 0;
+  meet();
+  const bool room = found >= want;
+  if (!room) {
+    if (MODE != EXTEND) release(1);
+    if (tid == 0) report(p, PAGES_NO_ROOM);
+  }
+  if (tid == 0) p.scratch[PG_COPIES] = room && MODE != EXTEND ? want : 0;
+
+  int given = 0;
+  for (int base = 0; base < a.n; base += kPlan) {
+    const int i = base + tid;
+    Entry e = {-1, 0, 0, 0, 0, 0};
+    if (i < a.n) e = entry_of<MODE>(a, i);
+    int total;
+    first[tid] = given + scan_before(e.fresh, sums, &total);
+    given += total;
+    if (MODE == EXTEND && i < a.n) a.out_pos[i] = room && e.dst >= 0 ? e.len : -1;
+    __syncthreads();
+    if (room) {
+      const int end = min(kPlan, a.n - base);
+      for (int k = w; k < end; k += kPlan / 64) {
+        const Entry e = entry_of<MODE>(a, base + k);
+        if (e.dst < 0) continue;
+        int* const row = p.table + (size_t)e.dst * p.max_pages;
+        const int* const from = p.table + (size_t)e.src * p.max_pages;
+        const int whole = MODE == FORK && !a.deep ? e.len / kPage : 0;  // pages shared with the source
+        for (int j = (MODE == EXTEND ? e.held : 0) + lane; j < max(e.held, e.pages); j += 64) {
+          int pg = -1;
+          if (j < e.pages) {
+            if (j < whole) {
+              pg = from[j];
+            } else {
+              const int f = first[k] + j - (MODE == EXTEND ? e.held : whole);
+              pg = fresh_pages[f];
+              if (MODE == FORK) p.copy_src()[f] = from[j];
+              if (MODE == IMPORT) p.copy_src()[f] = ((base + k) << 16) | j;
+            }
+            if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, 1);
+          }
+          row[j] = pg;
+        }
+      }
+      __syncthreads();  // (len is what entry_of reads; it changes when every wave is through)
+      if (e.dst >= 0) p.len[e.dst] = MODE == EXTEND ? e.len + a.tokens : e.len;
+    }
+    __syncthreads();
+  }
+  meet();
+  for (int i = tid; i < a.n; i += kPlan) {
+    const int d = a.dst[i];
+    if ((unsigned)d < (unsigned)p.max_seqs) p.is_dst()[d] = 0;
+    if (MODE == FORK) {
+      const int s = a.src[i];
+      if ((unsigned)s < (unsigned)p.max_seqs) p.is_src()[s] = 0;
+    }
+  }
+}
+
+// copy_src -> copy_dst, whole pages; how many of them only the device knows.  A workgroup takes 16 KiB at a time, four
+// loads in flight per thread.  REMAP: also lets the tables follow (compact).
+constexpr int kChunk = 1024;  // 16-byte words of a work item
+template <bool REMAP>
+__global__ __launch_bounds__(256) void pages_copy_kernel(PoolView p, long long page16) {
+  const int n = ld_scalar(p.scratch + PG_COPIES);
+  const int chunks = (int)((page16 + kChunk - 1) / kChunk);
+  const long long items = (long long)n * chunks;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int k = (int)(it / chunks), c = (int)(it - (long long)k * chunks);
+    const int from = ld_scalar(p.copy_src() + k), to = ld_scalar(p.copy_dst() + k);
+    if ((unsigned)from >= (unsigned)p.n_pages) continue;
+    const uint4* s = (const uint4*)p.data + (long long)from * page16;
+    uint4* d = (uint4*)p.data + (long long)to * page16;
+    const long long at = (long long)c * kChunk + threadIdx.x;
+    // (a page is a multiple of 512 words: the last item holds two or four of a thread's words)
+    const uint4 x0 = s[at], x1 = s[at + 256];
+    if ((long long)(c + 1) * kChunk <= page16) {
+      const uint4 x2 = s[at + 512], x3 = s[at + 768];
+      d[at + 512] = x2;
+      d[at + 768] = x3;
+    }
+    d[at] = x0;
+    d[at + 256] = x1;
+  }
+  if (REMAP && n > 0) {
+    const int live = ld_scalar(p.scratch + PG_COPIES + 1);
+    for (int s = blockIdx.x; s < p.max_seqs; s += gridDim.x) {
+      const int l = checked_len(p, s);
+      for (int j = threadIdx.x; j < (l > 0 ? pages_of(l) : 0); j += 256) {
+        int* at = p.table + (size_t)s * p.max_pages + j;
+        const int pg = *at;
+        if (pg >= live && pg < p.n_pages) *at = p.moved_to()[pg];
+      }
+    }
+  }
+}
+
+// Tiles of the streams' cache into fresh pages: work item = (page, layer, K or V, kv head)
+__global__ __launch_bounds__(256) void pages_import_kernel(PoolView p, const uint4* cache, long long stream16, int max_seq) {
+  const int n = ld_scalar(p.scratch + PG_COPIES);
+  const int tile16 = (int)(p.tile() / 8), heads = p.n_layers * 2 * p.n_kv_heads;
+  const long long items = (long long)n * heads, head16 = (long long)max_seq * p.head_dim / 8, page16 = (long long)heads * tile16;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int k = (int)(it / heads), h = (int)(it - (long long)k * heads);
+    const int from = ld_scalar(p.copy_src() + k), to = ld_scalar(p.copy_dst() + k);
+    const uint4* s = cache + (from >> 16) * stream16 + h * head16 + (long long)(from & 0xffff) * tile16;
+    uint4* d = (uint4*)p.data + to * page16 + (long long)h * tile16;
+    for (int i = threadIdx.x; i < tile16; i += 256) d[i] = s[i];
+  }
+}
+
+__global__ __launch_bounds__(256) void pages_reset_kernel(PoolView p, int scratch_words) {
+  const long long rows = (long long)p.max_seqs * p.max_pages, step = (long long)gridDim.x * 256;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  for (long long i = at; i < rows; i += step) p.table[i] = -1;
+  for (long long i = at; i < p.n_pages; i += step) p.refs[i] = 0;
+  for (long long i = at; i < p.max_seqs; i += step) p.len[i] = 0;
+  for (long long i = at; i < scratch_words; i += step) p.scratch[i] = 0;
+}
+
+// One workgroup per entry; whoever takes the length of a sequence first releases its pages
+__global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* __restrict__ seqs) {
+  __shared__ int s_len;
+  const int s = seqs[blockIdx.x];
+  if ((unsigned)s >= (unsigned)p.max_seqs) {
+    if (threadIdx.x == 0) report(p, PAGES_BAD_ENTRY);
+    return;
+  }
+  if (threadIdx.x == 0) s_len = atomicExch(p.len + s, 0);
+  __syncthreads();
+  int l = s_len;
+  if (l < 0 || l > p.max_pages * kPage) {
+    if (threadIdx.x == 0) report(p, PAGES_BAD_ENTRY);
+    return;
+  }
+  for (int j = threadIdx.x; j < pages_of(l); j += 256) {
+    int* at = p.table + (size_t)s * p.max_pages + j;
+    const int pg = *at;
+    *at = -1;
+    if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, -1);
+  }
+}
+
+// One workgroup: counts the pages in use, then pairs those at or beyond the count with the free ones below it
+__global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* out_live) {
+  __shared__ int sums[kPlan / 64 + 1];
+  const int tid = threadIdx.x;
+  int mine = 0;
+  for (int i = tid; i < p.n_pages; i += kPlan) mine += p.refs[i] > 0;
+  int live;
+  (void)scan_before(mine, sums, &live);
+  int holes = 0, moves = 0;  // (equal in the end)
+  for (int base = 0; base < p.n_pages; base += kPlan) {
+    const int i = base + tid;
+    const bool in = i < p.n_pages, used = in && p.refs[i] > 0;
+    const bool hole = in && i < live && !used, move = in && i >= live && used;
+    int total;
+    const int rank = scan_before((hole ? 1 << 16 : 0) + (move ? 1 : 0), sums, &total);
+    if (hole) p.copy_dst()[holes + (rank >> 16)] = i;
+    if (move) p.copy_src()[moves + (rank & 0xffff)] = i;
+    holes += total >> 16;
+    moves += total & 0xffff;
+  }
+  meet();
+  for (int k = tid; k < moves; k += kPlan) {
+    const int from = p.copy_src()[k], to = p.copy_dst()[k];
+    p.moved_to()[from] = to;
+    p.refs[to] = p.refs[from];
+    p.refs[from] = 0;
+  }
+  if (tid == 0) {
+    p.scratch[PG_COPIES] = moves;
+    p.scratch[PG_COPIES + 1] = live;
+    *out_live = live;
+  }
+}
+
+// K and V of new tokens.  A thread takes 8 features of one row: 16 bytes of a K tile, 8 values of a V tile
+// 16 bytes apart.  TILES: the rows come from tiles (one token per entry), else from rows.
+struct AppendArgs {
+  PoolView p;
+  int layer, n, tokens, add;
+  const int *seqs, *pos;
+  const bf16_t *k, *v;
+  long long row_stride;
+};
+template <bool TILES>
+__global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
+  const PoolView& p = a.p;
+  const int c8 = p.head_dim / 8, per_row = p.n_kv_heads * c8;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long row = at / per_row;
+  if (row >= (long long)a.n * a.tokens) return;
+  const int x = (int)(at - row * per_row), h = x / c8, f = (x - h * c8) * 8;
+  const int i = (int)(row / a.tokens), t = (int)(row - (long long)i * a.tokens);
+  const int p0 = a.pos[i], s = a.seqs[i];
+  if (p0 < 0) return;
+  const int l = checked_len(p, s);
+  const long long at_pos = (long long)p0 + a.add + t;
+  int pg = -1;
+  if (l >= 0 && at_pos < l) pg = p.table[(size_t)s * p.max_pages + at_pos / kPage];
+  if ((unsigned)pg >= (unsigned)p.n_pages || p.refs[pg] != 1) {
+    report(p, PAGES_BAD_ENTRY);
+    return;
+  }
+  const int r = (int)at_pos & 31;
+  const size_t tile = p.tile();
+  bf16_t* kd = p.data + (size_t)pg * p.page() + ((size_t)a.layer * 2 * p.n_kv_heads + h) * tile;
+  bf16_t* vd = kd + p.n_kv_heads * tile;
+  const size_t k_at = (size_t)(f >> 4) * 512 + (size_t)((f >> 3) & 1) * 256 + r * 8;
+  const size_t v_at = (size_t)(f >> 5) * 1024 + (r >> 4) * 512 + ((r >> 2) & 1) * 256 + (f & 31) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
+  if (TILES) {
+    const bf16_t* ks = a.k + ((size_t)i * 2 * p.n_kv_heads + h) * tile;
+    const bf16_t* vs = ks + p.n_kv_heads * tile;
+    *(uint4*)(kd + k_at) = *(const uint4*)(ks + k_at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) vd[v_at + e * 8] = vs[v_at + e * 8];
+  } else {
+    const size_t src = (size_t)row * a.row_stride + (size_t)h * p.head_dim + f;
+    *(uint4*)(kd + k_at) = *(const uint4*)(a.k + src);
+    const uint4 v8 = *(const uint4*)(a.v + src);
+    const uint32_t two[4] = {v8.x, v8.y, v8.z, v8.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      vd[v_at + e * 16] = (bf16_t)two[e];
+      vd[v_at + e * 16 + 8] = (bf16_t)(two[e] >> 16);
+    }
+  }
+}
+
+size_t scratch_words(const vlac_pages* p) { return PG_LISTS + 3 * (size_t)p->n_pages + 2 * (size_t)p->max_seqs; }
+
+// Workgroups that copy up to `most` pages of `items` work items each
+int copy_grid(long long most, long long items) { return (int)std::max(1LL, std::min(most * items, 2048LL)); }
+
+int check_list(const vlac_pages* p, int n) {
+  const int rc = check_pages(p, true);
+  if (rc != VLAC_OK) return rc;
+  return n < 0 || n > VLAC_PAGES_MAX_LIST ? VLAC_E_RANGE : VLAC_OK;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP; }
+
+}  // namespace
+
+int check_pages(const vlac_pages* p, bool pointers) {
+  if (!p) return VLAC_E_NULL;
+  if (p->n_layers < 1 || p->n_layers > 512 || p->n_kv_heads < 1 || p->n_kv_heads > 1024 || p->n_pages < 1 ||
+      p->n_pages > 1 << 24 || p->max_seqs < 1 || p->max_seqs > 65536 || p->max_pages < 1 || p->max_pages > 32768)
+    return VLAC_E_RANGE;
+  if (p->head_dim != 64 && p->head_dim != 128) return VLAC_E_SHAPE;
+  if (p->operand_dtype != VLAC_OPERAND_BF16 && p->operand_dtype != VLAC_OPERAND_F16 && p->operand_dtype != VLAC_OPERAND_F16_W8)
+    return VLAC_E_RANGE;
+  if (pointers) {
+    if (!p->data || !p->refs || !p->table || !p->len || !p->scratch) return VLAC_E_NULL;
+    if ((uintptr_t)p->data % 16) return VLAC_E_SHAPE;
+  }
+  return VLAC_OK;
+}
+
+void launch_extend(const PoolView& p, const int* seqs, int n, int tokens, int want_len, int* out_pos, hipStream_t st) {
+  const PlanArgs a = {p, nullptr, seqs, n, tokens, 0, want_len, out_pos};
+  hipLaunchKernelGGL(pages_plan_kernel<EXTEND>, dim3(1), dim3(kPlan), 0, st, a);
+}
+
+static void launch_append(bool tiles, const AppendArgs& a, hipStream_t st) {
+  const long long threads = (long long)a.n * a.tokens * a.p.n_kv_heads * (a.p.head_dim / 8);
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  if (tiles) hipLaunchKernelGGL(pages_append_kernel<true>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(pages_append_kernel<false>, grid, dim3(256), 0, st, a);
+}
+
+void launch_append_tiles(const PoolView& p, int layer, const int* seqs, const int* pos, int add, int n,
+                         const bf16_t* tiles, hipStream_t st) {
+  const AppendArgs a = {p, layer, n, 1, add, seqs, pos, tiles, nullptr, 0};
+  launch_append(true, a, st);
+}
+
+extern "C" {
+
+size_t vlac_page_bytes(const vlac_pages* pages) {
+  return check_pages(pages, false) == VLAC_OK ? pool_view(pages).page() * sizeof(bf16_t) : 0;
+}
+
+size_t vlac_pages_scratch_bytes(const vlac_pages* pages) {
+  return check_pages(pages, false) == VLAC_OK ? scratch_words(pages) * sizeof(int) : 0;
+}
+
+int vlac_pages_reset(const vlac_pages* pages, void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  hipLaunchKernelGGL(pages_reset_kernel, dim3(512), dim3(256), 0, (hipStream_t)stream, pool_view(pages), (int)scratch_words(pages));
+  return launched();
+}
+
+int vlac_pages_check(const vlac_pages* pages, void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  int word = 0;
+  if (hipMemcpyAsync(&word, pages->scratch + PG_STATUS, sizeof(int), hipMemcpyDeviceToHost, st) != hipSuccess ||
+      hipStreamSynchronize(st) != hipSuccess)
+    return VLAC_E_HIP;
+  if (!word) return VLAC_OK;
+  if (hipMemsetAsync(pages->scratch + PG_STATUS, 0, sizeof(int), st) != hipSuccess || hipStreamSynchronize(st) != hipSuccess)
+    return VLAC_E_HIP;
+  return word & PAGES_NO_ROOM ? VLAC_E_NOMEM : VLAC_E_RANGE;
+}
+
+int vlac_pages_import(vlac_ctx* ctx, const void* kv_cache, int B, int L, const vlac_pages* pages, const int32_t* seqs,
+                      void* stream) {
+  if (!ctx || !kv_cache || !seqs) return VLAC_E_NULL;
+  const int rc = check_list(pages, B);
+  if (rc != VLAC_OK) return rc;
+  const vlac_model_cfg& m = ctx->cfg;
+  if (B < 1 || B > m.max_batch || L < 1) return VLAC_E_RANGE;
+  if (L > m.max_seq || (long long)L > (long long)pages->max_pages * kPage || pages->n_layers != m.n_layers ||
+      pages->n_kv_heads != m.n_kv_heads || pages->head_dim != m.head_dim || pages_f16(pages) != ctx->f16)
+    return VLAC_E_SHAPE;
+  for (int b = 0; b < B; ++b)
+    if (!ctx->filled[b]) return VLAC_E_STATE;
+  hipStream_t st = (hipStream_t)stream;
+  const PoolView p = pool_view(pages);
+  const PlanArgs a = {p, nullptr, seqs, B, L, 0, -1, nullptr};
+  hipLaunchKernelGGL(pages_plan_kernel<IMPORT>, dim3(1), dim3(kPlan), 0, st, a);
+  const long long stream16 = (long long)m.n_layers * 2 * m.n_kv_heads * m.max_seq * m.head_dim / 8;
+  const int heads = p.n_layers * 2 * p.n_kv_heads;
+  hipLaunchKernelGGL(pages_import_kernel, dim3(copy_grid((long long)B * ((L + 31) / 32), heads)), dim3(256), 0, st, p,
+                     (const uint4*)kv_cache, stream16, m.max_seq);
+  VLAC_HIP(hipGetLastError());
+  return VLAC_OK;
+}
+
+int vlac_pages_fork(const vlac_pages* pages, const int32_t* src, const int32_t* dst, int n, int deep, void* stream) {
+  const int rc = check_list(pages, n);
+  if (rc != VLAC_OK) return rc;
+  if (n == 0) return VLAC_OK;
+  if (!src || !dst) return VLAC_E_NULL;
+  hipStream_t st = (hipStream_t)stream;
+  const PoolView p = pool_view(pages);
+  const PlanArgs a = {p, src, dst, n, 0, deep != 0, -1, nullptr};
+  hipLaunchKernelGGL(pages_plan_kernel<FORK>, dim3(1), dim3(kPlan), 0, st, a);
+  const long long page16 = (long long)(p.page() / 8), most = std::min((long long)n * (deep ? p.max_pages : 1), (long long)p.n_pages);
+  hipLaunchKernelGGL(pages_copy_kernel<false>, dim3(copy_grid(most, (page16 + kChunk - 1) / kChunk)), dim3(256), 0, st, p, page16);
+  return launched();
+}
+
+int vlac_pages_extend(const vlac_pages* pages, const int32_t* seqs, int n, int tokens, int32_t* out_pos, void* stream) {
+  const int rc = check_list(pages, n);
+  if (rc != VLAC_OK) return rc;
+  if (tokens < 1 || tokens > 1 << 20) return VLAC_E_RANGE;
+  if (n == 0) return VLAC_OK;
+  if (!seqs || !out_pos) return VLAC_E_NULL;
+  launch_extend(pool_view(pages), seqs, n, tokens, -1, out_pos, (hipStream_t)stream);
+  return launched();
+}
+
+int vlac_pages_append(const vlac_pages* pages, int layer, const int32_t* seqs, const int32_t* pos, int n, int tokens,
+                      const void* k, const void* v, int64_t row_stride, void* stream) {
+  const int rc = check_list(pages, n);
+  if (rc != VLAC_OK) return rc;
+  if (layer < 0 || layer >= pages->n_layers || tokens < 1 || (long long)n * tokens > 1 << 20) return VLAC_E_RANGE;
+  if (row_stride < (int64_t)pages->n_kv_heads * pages->head_dim || row_stride % 8 || row_stride > 1 << 30) return VLAC_E_SHAPE;
+  if (n == 0) return VLAC_OK;
+  if (!seqs || !pos || !k || !v) return VLAC_E_NULL;
+  if ((uintptr_t)k % 16 || (uintptr_t)v % 16) return VLAC_E_SHAPE;
+  const AppendArgs a = {pool_view(pages), layer, n, tokens, 0, seqs, pos, (const bf16_t*)k, (const bf16_t*)v, row_stride};
+  launch_append(false, a, (hipStream_t)stream);
+  return launched();
+}
+
+int vlac_pages_free(const vlac_pages* pages, const int32_t* seqs, int n, void* stream) {
+  const int rc = check_list(pages, n);
+  if (rc != VLAC_OK) return rc;
+  if (n == 0) return VLAC_OK;
+  if (!seqs) return VLAC_E_NULL;
+  hipLaunchKernelGGL(pages_free_kernel, dim3(n), dim3(256), 0, (hipStream_t)stream, pool_view(pages), seqs);
+  return launched();
+}
+
+int vlac_pages_compact(const vlac_pages* pages, int32_t* out_live, void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  if (!out_live) return VLAC_E_NULL;
+  hipStream_t st = (hipStream_t)stream;
+  const PoolView p = pool_view(pages);
+  hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kPlan), 0, st, p, out_live);
+  const long long page16 = (long long)(p.page() / 8);
+  hipLaunchKernelGGL(pages_copy_kernel<true>,
+                     dim3(copy_grid(std::max<long long>(p.n_pages / 2, 1), (page16 + kChunk - 1) / kChunk)), dim3(256), 0, st, p, page16);
+  return launched();
+}
+
+}  // extern "C"
