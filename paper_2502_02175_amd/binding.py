@@ -357,39 +357,43 @@ def vlac_decode_action(ctx, B, L, n_new, first_token, kv_cache, out_tokens, out_
 # ---- pages of the cache, and attention over them ----
 #
 # These calls run on the pool's device, whatever the current one is (stream=None: that device's
-# current stream), and check every tensor they are given: device, type, size, contiguity.
+# current stream), and check every tensor they are given: device, type, size, contiguity.  A decode step
+# makes two of them per layer, each a launch of a few microseconds, so what they do per call is kept
+# short: a tensor is asked for its device as a number, and the current stream is read without making an object.
 
 def pages(n_layers, n_kv_heads, head_dim, operand_dtype, data, refs, table, length, scratch=None):
     """The vlac_pages over the caller's GPU tensors: data (any 16-bit or byte type, a whole number of pages),
     refs int32 [n_pages], table int32 [max_seqs, max_pages], length int32 [max_seqs]; the scratch is
     allocated (zero) if it is not given."""
     import torch
+    if table.dim() != 2:
+        raise ValueError("table [max_seqs, max_pages]")
     p = Pages(n_layers, n_kv_heads, head_dim, operand_dtype, refs.numel(), table.shape[0], table.shape[1])
-    bytes_, words = int(lib().vlac_page_bytes(C.byref(p))), int(lib().vlac_pages_scratch_bytes(C.byref(p))) // 4
-    if bytes_ == 0:
+    size, words = vlac_page_bytes(p), vlac_pages_scratch_bytes(p) // 4
+    if size == 0:
         raise VlacError(VLAC_E_SHAPE, "vlac_pages: sizes that no pool may have")
     if scratch is None:
         scratch = torch.zeros(words, dtype=torch.int32, device=refs.device)
-    if data.numel() * data.element_size() != bytes_ * p.n_pages:
+    if data.numel() * data.element_size() != size * p.n_pages:
         raise ValueError("data holds %d bytes, %d pages take %d" % (data.numel() * data.element_size(), p.n_pages,
-                                                                    bytes_ * p.n_pages))
-    if length.numel() != p.max_seqs or scratch.numel() < words or table.dim() != 2:
-        raise ValueError("table [max_seqs, max_pages], length [max_seqs], scratch of vlac_pages_scratch_bytes")
-    i32 = torch.int32
-    p.device = refs.device
+                                                                    size * p.n_pages))
+    if length.numel() != p.max_seqs:
+        raise ValueError("length holds %d sequences, table %d" % (length.numel(), p.max_seqs))
     p.tensors = (data, refs, table, length, scratch)
-    for x in p.tensors:
-        _on(p, x)
-    p.data, p.refs, p.table = _ptr(data, None, "data"), _ptr(refs, i32, "refs"), _ptr(table, i32, "table")
-    p.len, p.scratch = _ptr(length, i32, "length"), _ptr(scratch, i32, "scratch")
+    p.index = refs.get_device()
+    p.torch = torch
+    p.rows_dtype = torch.bfloat16 if operand_dtype == OPERAND_BF16 else torch.float16
+    p.data = _at(p, data, None, 0, "data")
+    p.refs, p.table = _at(p, refs, torch.int32, 0, "refs"), _at(p, table, torch.int32, 0, "table")
+    p.len, p.scratch = _at(p, length, torch.int32, 0, "length"), _at(p, scratch, torch.int32, words, "scratch")
+    p.ref = C.byref(p)
     return p
 
 
 def new_pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, max_pages, device="cuda"):
     """An empty pool in new tensors on `device`."""
     import torch
-    p = Pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, max_pages)
-    size = int(lib().vlac_page_bytes(C.byref(p)))
+    size = vlac_page_bytes(Pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, max_pages))
     if size == 0:
         raise VlacError(VLAC_E_SHAPE, "vlac_pages: sizes that no pool may have")
     i32 = dict(dtype=torch.int32, device=device)
@@ -400,63 +404,57 @@ def new_pages(n_layers, n_kv_heads, head_dim, operand_dtype, n_pages, max_seqs, 
     return made
 
 
-def _on(p, x):
-    """x if it lies on the pool's device."""
-    dev = getattr(p, "device", None)
-    if x is not None and not isinstance(x, int) and dev is not None and x.device != dev:
-        raise ValueError("a tensor on %s for a pool on %s" % (x.device, dev))
-    return x
+def _at(p, x, dtype, n, name):
+    """Address of a contiguous tensor of at least n values on the pool's device (an address or None as it is)."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.get_device() != p.index or p.index < 0:
+        raise ValueError("%s lies on %s, the pool on GPU %d" % (name, x.device, p.index))
+    if dtype is not None and x.dtype != dtype:
+        raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, dtype))
+    if not x.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if x.numel() < n:
+        raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
+    return x.data_ptr()
 
 
 def _list(p, x, n, name):
-    """Pointer of an int32 list of n entries on the pool's device."""
-    import torch
-    _sized(x, n, name)
-    return _ptr(_on(p, x), torch.int32, name)
+    return _at(p, x, p.torch.int32, n, name)
 
 
-def _sized(x, n, name):
-    if x is not None and not isinstance(x, int) and x.numel() < n:
-        raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
-
-
-def _rows(p, x, n, tokens, heads, name):
-    """Pointer and row stride of values [n, tokens, heads, head_dim] (the last two dimensions dense, the rows
-    equally far apart), or [n * tokens, heads * head_dim]."""
-    import torch
-    want = torch.bfloat16 if p.operand_dtype == OPERAND_BF16 else torch.float16
+def _rows(p, x, count, width, name):
+    """Address and row stride of `count` rows of `width` dense values, equally far apart, of the pool's type."""
     if x is None or isinstance(x, int):
-        return x, heads * p.head_dim
-    _on(p, x)
-    if not x.is_cuda:
-        raise ValueError("%s must live in GPU memory" % name)
-    if x.dtype != want:
-        raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, want))
-    width = heads * p.head_dim
-    if x.numel() != n * tokens * width:
-        raise ValueError("%s holds %d values, expected %d x %d x %d" % (name, x.numel(), n, tokens, width))
+        return x, width
+    if x.numel() != count * width:
+        raise ValueError("%s holds %d values, expected %d rows of %d" % (name, x.numel(), count, width))
+    if x.is_contiguous():
+        return _at(p, x, p.rows_dtype, 0, name), width
     try:
-        y = x.view(n * tokens, width)   # (a view exists if the rows are equally far apart and dense)
+        y = x.view(count, width)   # (such a view exists if the rows are equally far apart and dense)
     except RuntimeError:
-        raise ValueError("%s: rows must be dense and equally far apart" % name) from None
-    if width > 1 and y.shape[0] and y.stride(1) != 1:
-        raise ValueError("%s: rows must be dense" % name)
-    return y.data_ptr(), (y.stride(0) if y.shape[0] > 1 else width)
+        y = None
+    if y is None or y.stride(1) != 1:
+        raise ValueError("%s: rows must be dense and equally far apart" % name)
+    return _at(p, y[0], p.rows_dtype, 0, name), (y.stride(0) if count > 1 else width)
 
 
 def _call(p, name, stream, check, *args):
     """One library call on the pool's device."""
-    import torch
-    fn = getattr(lib(), name)
-    dev = getattr(p, "device", None)
-    if dev is None or dev.type != "cuda":
+    fn, index = getattr(lib(), name), getattr(p, "index", -1)
+    if index < 0:                      # (no pool, or one of bare addresses: the current device's)
         return _ret(fn(*args, _stream(stream)), name, check)
-    with torch.cuda.device(dev):
-        return _ret(fn(*args, _stream(stream)), name, check)
+    cuda = p.torch.cuda
+    raw = p.torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+    if cuda.current_device() == index:
+        return _ret(fn(*args, raw), name, check)
+    with cuda.device(index):
+        return _ret(fn(*args, raw), name, check)
 
 
 def _ref(p):
-    return C.byref(p) if p is not None else None
+    return getattr(p, "ref", None) or (C.byref(p) if p is not None else None)
 
 
 def vlac_page_bytes(p):
@@ -476,7 +474,7 @@ def vlac_pages_check(p, stream=None, check=True):
 
 
 def vlac_pages_import(ctx, kv_cache, B, L, p, seqs, stream=None, check=True):
-    return _call(p, "vlac_pages_import", stream, check, ctx, _ptr(_on(p, kv_cache), None, "kv_cache"), B, L, _ref(p),
+    return _call(p, "vlac_pages_import", stream, check, ctx, _at(p, kv_cache, None, 0, "kv_cache"), B, L, _ref(p),
                  _list(p, seqs, B, "seqs"))
 
 
@@ -492,12 +490,13 @@ def vlac_pages_extend(p, seqs, n, tokens, out_pos, stream=None, check=True):
 
 def vlac_pages_append(p, layer, seqs, pos, n, tokens, k, v, stream=None, check=True):
     """k, v: [n, tokens, n_kv_heads, head_dim] of the pool's type; slices of a joint projection have one row stride."""
-    kp, ks = _rows(p, k, n, tokens, p.n_kv_heads, "k")
-    vp, vs = _rows(p, v, n, tokens, p.n_kv_heads, "v")
-    if ks != vs:
-        raise ValueError("k and v: rows %d and %d values apart" % (ks, vs))
+    width = p.n_kv_heads * p.head_dim
+    k_at, k_stride = _rows(p, k, n * tokens, width, "k")
+    v_at, v_stride = _rows(p, v, n * tokens, width, "v")
+    if k_stride != v_stride:
+        raise ValueError("k and v: rows %d and %d values apart" % (k_stride, v_stride))
     return _call(p, "vlac_pages_append", stream, check, _ref(p), layer, _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"),
-                 n, tokens, kp, vp, ks)
+                 n, tokens, k_at, v_at, k_stride)
 
 
 def vlac_pages_free(p, seqs, n, stream=None, check=True):
@@ -513,10 +512,8 @@ def vlac_attend_workspace_bytes(p, n, tokens, n_q_heads):
 
 
 def _workspace(p, ws):
-    """Pointer and bytes of a workspace tensor."""
-    if ws is None:
-        return None, 0
-    return _ptr(_on(p, ws), None, "workspace"), ws.numel() * ws.element_size()
+    """Address and bytes of a workspace tensor."""
+    return (None, 0) if ws is None else (_at(p, ws, None, 0, "workspace"), ws.numel() * ws.element_size())
 
 
 def vlac_attend_plan(p, seqs, pos, n, tokens, n_q_heads, group, workspace, stream=None, check=True):
@@ -527,12 +524,11 @@ def vlac_attend_plan(p, seqs, pos, n, tokens, n_q_heads, group, workspace, strea
 
 def vlac_attend_shared(p, layer, n, tokens, n_q_heads, q, out, workspace, stream=None, check=True):
     """q: [n, tokens, n_q_heads, head_dim] of the pool's type, rows equally far apart; out the same, contiguous."""
-    qp, qs = _rows(p, q, n, tokens, n_q_heads, "q")
-    op, stride = _rows(p, out, n, tokens, n_q_heads, "out")
-    if out is not None and not isinstance(out, int) and not out.is_contiguous():
-        raise ValueError("out must be contiguous")
+    count, width = n * tokens, n_q_heads * p.head_dim
+    q_at, q_stride = _rows(p, q, count, width, "q")
     ws, size = _workspace(p, workspace)
-    return _call(p, "vlac_attend_shared", stream, check, _ref(p), layer, n, tokens, n_q_heads, qp, qs, op, ws, size)
+    return _call(p, "vlac_attend_shared", stream, check, _ref(p), layer, n, tokens, n_q_heads, q_at, q_stride,
+                 _at(p, out, p.rows_dtype, count * width, "out"), ws, size)
 
 
 def vlac_candidates_workspace_bytes(ctx, p, n):
@@ -541,10 +537,7 @@ def vlac_candidates_workspace_bytes(ctx, p, n):
 
 def vlac_decode_candidates(ctx, p, seqs, n, L, group, n_new, first_token, out_tokens, out_logits, workspace, stream=None,
                            check=True):
-    import torch
-    _sized(out_tokens, n * n_new, "out_tokens")
     ws, size = _workspace(p, workspace)
     return _call(p, "vlac_decode_candidates", stream, check, ctx, _ref(p), _list(p, seqs, n, "seqs"), n, L,
                  _list(p, group, n, "group"), n_new, _list(p, first_token, n, "first_token"),
-                 _ptr(_on(p, out_tokens), torch.int32, "out_tokens"), _ptr(_on(p, out_logits), torch.float32, "out_logits"),
-                 ws, size)
+                 _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, p.torch.float32, 0, "out_logits"), ws, size)
