@@ -1,82 +1,78 @@
 // Attention of new tokens over pages, for sequences that share prefixes:
 //   out[row] = sum_p exp(s_p - M) v_p / sum_p exp(s_p - M),  s_p = q . k_p / sqrt(head_dim), p <= position of the row.
-// The keys of a row are cut into segments: the pages that its group has in common at the front (all of them wholly
-// before every query of the group: no mask), and its own behind them.  A segment is cut further over the keys, and
-// every part leaves (max, sum, output) of its columns in fp32; a second kernel joins a row's parts:
-//   M = max m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i   (scores in units of log2).
-// What is gained: a shared page is read once for all columns of its group (candidates x tokens x query heads of the kv
-// head), 32 of them to a matrix product, where one pass per sequence reads it once for each.
+// The pages that a group's tables have in common at the front (all of them wholly before every query of the group: no mask) are
+// read once for all its columns (candidates x tokens x query heads of the kv head), 32 of them to a matrix product, where
+// one pass per sequence reads them once for each; the pages behind them are each sequence's own.
 //
-// A column is a query (entry, token, head of the group); 32 columns are a column block.  S^T = K Q^T and O^T += V^T P^T as in
-// the attention over the stream cache: a page's tiles are the operands as they lie, a lane owns a column.
-// A workgroup of 4 waves takes a work item: of a segment with one column block the waves take every
-// 4th key tile, with two every 2nd, and with more a column block each; or (short segments of one block, the usual
-// decode step) four such segments, one per wave.
+// A column is a query (entry, token, head of the kv head's group); 32 columns are a column block, whose work is a list of key
+// tiles: the shared pages, then the own pages of its entries, which only the entry's columns see.  S^T = K Q^T and O^T += V^T P^T
+// as in the attention over the stream cache: a page's tiles are the operands as they lie, a lane owns a column.
+// A workgroup of 8 waves takes an item: 1, 2 or 4 column blocks side by side (they share the pages) and the key tiles dealt
+// to the waves of a block, which meet in LDS.  Where that leaves the chip empty the list is cut into parts, one item each,
+// which leave (max, sum, output) in fp32, and a second kernel joins them in the order of the parts:
+//   M = max m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i   (scores in units of log2).
 #include <algorithm>
+#include <type_traits>
 
 #include "pages.h"
 
 namespace {
 
-constexpr int kPlan = 1024;          // threads of the planning workgroup
-constexpr int kMaxSplit = 64;        // parts of a segment (a lane each when they are joined)
-constexpr int kSlots = 512;          // workgroups that the chip holds at a time (two per CU)
-constexpr int kWaveTiles = 4;        // own segments of at most this many pages are a wave's work
+constexpr int kWaves = 8;            // of a workgroup; one workgroup per CU (256 registers a wave)
+constexpr int kCus = 256;
+constexpr int kMaxParts = 64;
+constexpr int kPartTiles = 2048;     // column blocks x parts that the workspace holds at most
 
-// What a row has to know, per entry
-struct Ent {
-  int seq, pos;          // row of the table (-1: the entry is ignored), position of its first query
-  int shared;            // pages that its group reads together
-  int sh_parts, sh_base; // parts of that segment, first partial column of head 0, part 0
-  int c0, cols;          // first column of the entry in its group's segment, columns of the segment
-  int own_parts, own_base;
-  int group;             // index of its group (for the planning kernel)
-  int pad[2];
-};
-// A work item.  what: 0 shared, 1 own, 2 own segments of four (entry, kv head) pairs
+// What a row has to know, per entry: row of the table (-1: the entry is ignored), position of its first query
+struct Ent { int seq, pos; };
+// A step over a page of an entry's own: page | valid positions of it << 24, tile | entry of the group << 16
+struct Own { uint32_t page, what; };
+// A work item: column blocks block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry e0, part `part` of
+// `parts` of their key tiles: the shared pages of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
+// tile: where block0's parts lie.
 struct Item {
-  int what, e0, seq, head, block, t0, t1, base, cols, waves_c, pad[2];
+  int e0, seq, head, block0, waves_c, part, parts, cols, shared, tile, pad[2], own_at[4], own_n[4];
 };
-static_assert(sizeof(Ent) == 48 && sizeof(Item) == 48, "read as three 16-byte words");
+static_assert(sizeof(Item) == 80, "read as five 16-byte words");
 
 struct Layout {
-  size_t ent, item, ml, o, total;
-  size_t max_items, max_cols;
-  int split_shared, split_own;  // most parts of a segment
+  size_t ent, own, item, ml, o, total;
+  size_t max_items;
+  int part_tiles;
+  bool parts;  // there may be parts to join
 };
-// Parts are bounded so that what they leave is bounded: as many as give every slot of the chip an item twice over where
-// the batch has the fewest column blocks that its rows can make
-inline Layout layout_of(int n, int tokens, int n_q_heads, int n_kv_heads, int head_dim) {
+inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   Layout l;
-  const size_t rows = (size_t)n * tokens * n_q_heads, per_kv = rows / n_kv_heads;
-  const size_t own_cols = (size_t)tokens * (n_q_heads / n_kv_heads);
-  const size_t blocks = (per_kv + 31) / 32 * n_kv_heads, own_blocks = (own_cols + 31) / 32 * n * n_kv_heads;
-  auto split = [](size_t b) { return (int)std::max<size_t>(1, std::min<size_t>(kMaxSplit, (2 * kSlots + b - 1) / b)); };
-  l.split_shared = split(blocks);
-  l.split_own = split(own_blocks);
-  l.max_cols = rows * (l.split_shared + l.split_own);
-  // (a group of few columns is a block of its own: at most n groups)
-  l.max_items = (blocks + (size_t)n * n_kv_heads) * l.split_shared + own_blocks * l.split_own + n_kv_heads;
+  const size_t cols = (size_t)n * tokens * (n_q_heads / p.n_kv_heads);  // per kv head
+  const size_t least = (cols + 31) / 32 * p.n_kv_heads, max_blocks = least + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
+  // Parts where the column blocks do not fill the chip by themselves and the tables have room for lists that are long
+  // for 8 waves (that decides whether the second kernel is launched: 2.5 us where it finds nothing to join)
+  l.parts = least < 2 * kCus && p.max_pages > 48;
+  l.part_tiles = l.parts ? (int)std::min<size_t>(kPartTiles, max_blocks * kMaxParts) : 0;
+  l.max_items = max_blocks + l.part_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   l.ent = 256;
-  l.item = l.ent + up(sizeof(Ent) * n);
+  l.own = l.ent + up(sizeof(Ent) * n);
+  l.item = l.own + up(sizeof(Own) * n * p.max_pages);
   l.ml = l.item + up(sizeof(Item) * l.max_items);
-  l.o = l.ml + up(8 * l.max_cols);
-  l.total = l.o + up(4 * l.max_cols * head_dim);
+  l.o = l.ml + (size_t)l.part_tiles * 64 * sizeof(float2);
+  l.total = l.o + (size_t)l.part_tiles * 32 * p.head_dim * sizeof(float);
   return l;
 }
 
 struct PlanArgs {
   PoolView p;
   const int *seqs, *pos, *group;
-  int add, n, tokens, n_q_heads, split_shared, split_own, max_items;
+  int add, n, tokens, n_q_heads, part_tiles, max_items;
   int* head;  // [0] number of items
   Ent* ent;
+  Own* own;
   Item* item;
 };
 
 // Sums of two numbers over the threads before this one, and over all
 struct Two { int a, b; };
+template <int NT>
 __device__ inline Two scan_before(Two x, Two* sums, Two* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   Two run = x;
@@ -87,221 +83,283 @@ __device__ inline Two scan_before(Two x, Two* sums, Two* total) {
   }
   if (lane == 63) sums[w] = run;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    Two s = {0, 0};
-    for (int i = 0; i < kPlan / 64; ++i) {
-      const Two t = sums[i];
-      sums[i] = s;
-      s.a += t.a; s.b += t.b;
-    }
-    sums[kPlan / 64] = s;
+  // (every wave adds the sums of all 16 for itself: no second meeting)
+  const Two mine = lane < NT / 64 ? sums[lane] : Two{0, 0};
+  Two s = mine;
+#pragma unroll
+  for (int d = 1; d < NT / 64; d <<= 1) {
+    const int ya = __shfl_up(s.a, d), yb = __shfl_up(s.b, d);
+    if (lane >= d) { s.a += ya; s.b += yb; }
   }
-  __syncthreads();
-  const Two before = {sums[w].a + run.a - x.a, sums[w].b + run.b - x.b};
-  *total = sums[kPlan / 64];
+  *total = {__builtin_amdgcn_readlane(s.a, NT / 64 - 1), __builtin_amdgcn_readlane(s.b, NT / 64 - 1)};
+  const Two before = {__shfl(s.a - mine.a, w) + run.a - x.a, __shfl(s.b - mine.b, w) + run.b - x.b};
   __syncthreads();
   return before;
 }
 
-// How the waves of a workgroup share a segment: column blocks side by side
-__device__ inline int waves_over_columns(int blocks) { return blocks >= 3 ? 4 : blocks; }
+// How a group is cut: column blocks, of which `waves_c` are side by side in an item
+struct Cut { int blocks, waves_c, chunks, wk; };
+__device__ inline Cut cut_of(int cols, int log_most) {
+  Cut x;
+  x.blocks = (cols + 31) >> 5;
+  const int log = min(x.blocks >= 3 ? 2 : x.blocks >> 1, log_most);
+  x.waves_c = 1 << log;
+  x.chunks = (x.blocks + x.waves_c - 1) >> log;
+  x.wk = kWaves >> log;
+  return x;
+}
 
-struct Cut { int waves_c, chunks, parts; };
-
-// One workgroup.  Groups and their common pages, then the cut, then the items.
-__global__ __launch_bounds__(kPlan) void attend_plan_kernel(PlanArgs a) {
-  __shared__ Two sums[kPlan / 64 + 1];
-  constexpr int N = VLAC_PAGES_MAX_LIST;
-  __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_item[N], g_base[N], o_item[N];
-  __shared__ int s_own_most;
-  __shared__ unsigned long long s_work[2];
+// One workgroup.  Groups and their common pages, then the cut, then the items.  Memory is asked for in three rounds
+// (lists, lengths, tables), all else is in LDS.
+// (NT threads and room for N entries: a workgroup of 4 waves meets sooner than one of 16)
+template <int NT, int N>
+__global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
+  __shared__ Two sums[NT / 64];
+  __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_own[N], g_item[N + 1], g_tile[N], l_seq[N], l_pos[N], l_own[N + 1];
+  __shared__ unsigned short l_group[N];
+  __shared__ int s_bad, s_width, s_steps, s_longest, s_blocks, s_own;
+  __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int hkv = p.n_kv_heads, per_entry = a.tokens * (a.n_q_heads / hkv);  // columns of an entry per kv head
+  read_args(a.seqs, a.pos, a.group, a.add, a.n, a.tokens, a.n_q_heads, a.part_tiles, a.max_items, a.head, a.ent, a.own,
+            a.item, p.table, p.len, p.max_seqs, p.max_pages, p.n_kv_heads);
+  const int hkv = p.n_kv_heads, grp = a.n_q_heads / hkv, per_entry = a.tokens * grp;  // columns of an entry per kv head
   if (tid == 0) {
-    s_own_most = 0;
-    s_work[0] = s_work[1] = 0;
+    s_bad = s_width = s_longest = s_blocks = s_own = 0;
+    s_work = 0;
   }
 
   int n_groups = 0;
-  for (int base = 0; base < a.n; base += kPlan) {
-    const int i = base + tid;
-    const bool start = i < a.n && (i == 0 || (a.group && a.group[i] != a.group[i - 1]));
+  for (int base = 0; base < a.n; base += NT) {
+    const int i = base + tid, ii = min(i, a.n - 1);
+    const int label = a.group ? a.group[ii] : 0, label_before = a.group ? a.group[max(ii - 1, 0)] : 0;
+    const int s = a.seqs[ii], p0 = a.pos[ii];
+    const int l = checked_len(p, s);
+    const bool start = i < a.n && (i == 0 || label != label_before);
     Two total;
-    const Two before = scan_before({start ? 1 : 0, 0}, sums, &total);
-    if (start) g_start[n_groups + before.a] = i;
-    if (i < a.n) a.ent[i].group = n_groups + before.a + (start ? 1 : 0) - 1;
+    const Two before = scan_before<NT>({start ? 1 : 0, 0}, sums, &total);
+    if (start) {
+      const int g = n_groups + before.a;
+      g_start[g] = i;
+      g_lead[g] = g_shared[g] = 0x7fffffff;
+      g_own[g] = 0;
+    }
+    if (i < a.n) {
+      const long long at = (long long)p0 + a.add;
+      const bool fits = p0 >= 0 && l >= 0 && at + a.tokens <= l;
+      if (p0 >= 0 && !fits) s_bad = 1;
+      l_seq[i] = fits ? s : -1;
+      l_pos[i] = fits ? (int)at : 0;
+      l_group[i] = (unsigned short)(n_groups + before.a + (start ? 1 : 0) - 1);
+    }
     n_groups += total.a;
-  }
-  for (int g = tid; g < n_groups; g += kPlan) {
-    g_lead[g] = 0x7fffffff;
-    g_shared[g] = 0x7fffffff;
   }
   if (tid == 0) g_start[n_groups] = a.n;
   __syncthreads();
-  bool bad = false;
-  for (int i = tid; i < a.n; i += kPlan) {
-    const int s = a.seqs[i], p0 = a.pos[i];
-    const int l = checked_len(p, s);
-    const long long at = (long long)p0 + a.add;
-    const bool fits = p0 >= 0 && l >= 0 && at + a.tokens <= l;
-    bad |= p0 >= 0 && !fits;
-    a.ent[i].seq = fits ? s : -1;
-    a.ent[i].pos = fits ? (int)at : 0;
-    if (fits) {
-      const int g = a.ent[i].group;
-      atomicMin(&g_lead[g], i);
-      atomicMin(&g_shared[g], (int)(at / kPage));
+  if (tid == 0 && s_bad) report(p, PAGES_BAD_ENTRY);
+  int widest = 0;
+  for (int i = tid; i < a.n; i += NT)
+    if (l_seq[i] >= 0) {
+      atomicMin(&g_lead[l_group[i]], i);
+      atomicMin(&g_shared[l_group[i]], l_pos[i] / kPage);
+      widest = max(widest, l_pos[i] / kPage);
     }
-  }
-  if (bad) report(p, PAGES_BAD_ENTRY);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) widest = max(widest, __shfl_xor(widest, d));
+  if (lane == 0) atomicMax(&s_width, widest);
   __syncthreads();
-  // the common pages: every entry against its group's first, 512 pages in flight
-  for (int i = w; i < a.n; i += kPlan / 64) {
-    const int seq = a.ent[i].seq, g = a.ent[i].group;
-    if (seq < 0) continue;
-    const int lead = a.ent[g_lead[g]].seq;
-    if (lead == seq) continue;
-    const int* mine = p.table + (size_t)seq * p.max_pages;
-    const int* other = p.table + (size_t)lead * p.max_pages;
-    for (int j0 = 0; j0 < g_shared[g]; j0 += 512) {
-      const int end = g_shared[g];
+  // The common pages: every entry's against its group's first.  A wave takes an entry's next 512 pages or, where tables
+  // are short, as many entries as they leave lanes for; all of a turn's pages are asked for at once.
+  const int width = s_width;
+  if (width > 0) {
+    const int lanes = width <= 32 ? 4 : width <= 64 ? 8 : width <= 256 ? 32 : 64, per_wave = 64 / lanes;
+    const int spans = (width + 8 * lanes - 1) / (8 * lanes), blocks = (a.n + per_wave - 1) / per_wave;
+    for (int k = w; k < blocks * spans; k += NT / 64) {
+      const int span = k / blocks, i = min((k - span * blocks) * per_wave + lane / lanes, a.n - 1);  // (first spans first)
+      const int seq = l_seq[i], g = l_group[i];
+      const int lead = seq < 0 ? -1 : l_seq[g_lead[g]], end = g_shared[g], j0 = span * 8 * lanes + lane % lanes;
+      if (lead == seq || j0 >= end) continue;
+      const int* mine = p.table + (size_t)seq * p.max_pages;
+      const int* other = p.table + (size_t)lead * p.max_pages;
       int x[8], y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int j = j0 + 64 * e + lane;
-        x[e] = j < end ? mine[j] : -1;
-        y[e] = j < end ? other[j] : -1;
+        const int j = min(j0 + lanes * e, end - 1);
+        x[e] = mine[j];
+        y[e] = other[j];
       }
       int differ = 0x7fffffff;
 #pragma unroll
       for (int e = 7; e >= 0; --e)
-        if (x[e] != y[e]) differ = j0 + 64 * e + lane;
-      if (__any(differ != 0x7fffffff)) {
-        if (differ != 0x7fffffff) atomicMin(&g_shared[g], differ);
-        break;
+        if (x[e] != y[e]) differ = min(j0 + lanes * e, end - 1);
+      if (differ != 0x7fffffff) atomicMin(&g_shared[g], differ);
+    }
+  }
+  __syncthreads();
+
+  // Work in steps of a wave: a key tile of a column block.  (An entry's own tiles are dealt to its blocks as if each
+  // had them all; a block of tokens before the last sees fewer.)
+  auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
+  for (int g = tid; g < n_groups; g += NT)
+    if (g_lead[g] == 0x7fffffff) g_shared[g] = 0;
+  __syncthreads();
+  // own pages of every entry, and where they begin in the list of all of them
+  int owned = 0;
+  for (int base = 0; base < a.n; base += NT) {
+    const int i = base + tid;
+    int own = 0;
+    if (i < a.n) {
+      const int seq = l_seq[i], pos = l_pos[i], g = l_group[i];
+      a.ent[i] = {seq, pos};
+      if (seq >= 0) {
+        own = pages_of(pos + a.tokens) - g_shared[g];
+        atomicAdd(&g_own[g], own);
+        atomicMax(&s_own, own);
+      }
+    }
+    Two total;
+    const Two before = scan_before<NT>({own, 0}, sums, &total);
+    if (i < a.n) l_own[i] = owned + before.a;
+    owned += total.a;
+  }
+  if (tid == 0) l_own[a.n] = owned;
+  __syncthreads();
+  {
+    const int lanes = s_own <= 2 ? 2 : s_own <= 16 ? 8 : 64;
+    for (int i = tid / lanes; i < a.n; i += NT / lanes) {
+      const int own = l_own[i + 1] - l_own[i], shared = g_shared[l_group[i]];
+      for (int t = tid % lanes; t < own; t += lanes) {
+        int pg = p.table[(size_t)l_seq[i] * p.max_pages + shared + t];
+        if ((unsigned)pg >= (unsigned)p.n_pages) {  // (the table is the caller's)
+          pg = 0;
+          s_bad = 2;
+        }
+        const int valid = min(l_pos[i] + a.tokens - kPage * (shared + t), kPage);
+        a.own[l_own[i] + t] = {(uint32_t)pg | (uint32_t)valid << 24, (uint32_t)(shared + t) | (uint32_t)(i - g_start[l_group[i]]) << 16};
       }
     }
   }
-  __syncthreads();
-
-  // work in steps of a wave: a key tile of a column block
-  unsigned long long work = 0;
-  for (int g = tid; g < n_groups; g += kPlan) {
-    if (g_lead[g] == 0x7fffffff) g_shared[g] = 0;
-    const int blocks = ((g_start[g + 1] - g_start[g]) * per_entry + 31) / 32;
-    work += (unsigned long long)blocks * g_shared[g] * hkv;
+  const int entry_blocks = (per_entry + 31) / 32;
+  // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
+  // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
+  {
+    int blocks = 0;
+    for (int g = tid; g < n_groups; g += NT) blocks += (group_cols(g) + 31) / 32 * hkv;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
+    if (lane == 0) atomicAdd(&s_blocks, blocks);
   }
-  atomicAdd(&s_work[0], work);
   __syncthreads();
-  const int own_blocks = (per_entry + 31) / 32;
-  work = 0;
-  for (int i = tid; i < a.n; i += kPlan)
-    if (a.ent[i].seq >= 0) {
-      const int own = pages_of(a.ent[i].pos + a.tokens) - g_shared[a.ent[i].group];
-      atomicMax(&s_own_most, own);
-      work += (unsigned long long)own * own_blocks * hkv;
+  const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  // tiles of the list of a group's block
+  {
+    unsigned long long work = 0;
+    int longest = 0;
+    for (int g = tid; g < n_groups; g += NT) {
+      const Cut x = cut_of(group_cols(g), log_most);
+      const int tiles = g_shared[g] + (int)(((long long)g_own[g] * entry_blocks + x.blocks - 1) / x.blocks);
+      g_own[g] = tiles;  // (from here on: of the whole list of a block)
+      work += (unsigned long long)x.blocks * tiles * hkv;
+      longest = max(longest, (tiles + x.wk - 1) / x.wk);
     }
-  atomicAdd(&s_work[1], work);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      work += __shfl_xor(work, d);
+      longest = max(longest, __shfl_xor(longest, d));
+    }
+    if (lane == 0) {
+      atomicAdd(&s_work, work);
+      atomicMax(&s_longest, longest);
+    }
+  }
   __syncthreads();
-  const bool by_wave = own_blocks == 1 && s_own_most <= kWaveTiles;
-  // steps of a wave per item: what fills the chip's slots, and no fewer than two, so that a part is worth its columns
-  const int steps = (int)max(2ull, (s_work[0] + s_work[1] + 4ull * kSlots - 1) / (4ull * kSlots));
-  auto cut = [&](int c, int tiles, int most) {  // c columns per kv head, `tiles` pages
-    Cut x;
-    const int blocks = (c + 31) / 32;
-    x.waves_c = waves_over_columns(blocks);
-    x.chunks = (blocks + x.waves_c - 1) / x.waves_c;
-    const long long per_item = (long long)steps * (4 / x.waves_c);
-    x.parts = (int)min((long long)most, (tiles + per_item - 1) / per_item);
-    return x;
+  // Steps of a wave per item: the lanes of the first wave try the longest list in 1, 2, ... 64 parts, and take what
+  // ends first: rounds of one item per CU x (steps + 3 for an item's start and end), + 3 for parts that have to be joined.
+  // With many groups the chip is full anyhow, and the work per wave is the measure.
+  if (tid == 0 && s_bad == 2) report(p, PAGES_BAD_ENTRY);
+  const int most = max(1, a.part_tiles / max(s_blocks, 1));  // parts that the workspace has room for
+  auto parts_of = [&](int g, int steps) {
+    const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most).wk;
+    return max(1, min(min(most, kMaxParts), (int)((g_own[g] + per_item - 1) / per_item)));
   };
-  auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
+  if (w == 0) {
+    int steps = max((s_longest + lane) / (lane + 1), 1), best;
+    if (most == 1) {
+      steps = s_longest;
+    } else if (n_groups <= 64) {
+      int items = 0;
+      bool joined = false;
+      for (int g = 0; g < n_groups; ++g) {
+        const int parts = parts_of(g, steps);
+        items += hkv * cut_of(group_cols(g), log_most).chunks * parts;
+        joined |= parts > 1;
+      }
+      const float cost = (float)((items + kCus - 1) / kCus) * (float)(steps + 3) + (joined ? 3.f : 0.f);
+      best = (int)fminf(cost, 1e9f);  // (ties: the fewest parts)
+      int who = lane;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int c = __shfl_xor(best, d), o = __shfl_xor(who, d);
+        if (c < best || (c == best && o < who)) { best = c; who = o; }
+      }
+      steps = __shfl(steps, who);
+    } else {
+      steps = (int)max(2ull, min((s_work + kCus * kWaves - 1) / (kCus * kWaves), 1ull << 30));
+    }
+    if (lane == 0) s_steps = steps;
+  }
+  __syncthreads();
+  const int steps = s_steps;
 
-  // first item and first partial column of every segment
-  int items = 0, cols = 0;
-  for (int base = 0; base < n_groups; base += kPlan) {
+  // first item and first partial tile of every group
+  int items = 0, tiles = 0;
+  for (int base = 0; base < n_groups; base += NT) {
     const int g = base + tid;
     Two mine = {0, 0};
     if (g < n_groups) {
-      const Cut x = cut(group_cols(g), g_shared[g], a.split_shared);
-      mine = {hkv * x.chunks * x.parts, hkv * group_cols(g) * x.parts};
+      const Cut x = cut_of(group_cols(g), log_most);
+      const int parts = parts_of(g, steps);
+      mine = {hkv * x.chunks * parts, parts > 1 ? hkv * x.blocks * parts : 0};
     }
     Two total;
-    const Two before = scan_before(mine, sums, &total);
+    const Two before = scan_before<NT>(mine, sums, &total);
     if (g < n_groups) {
       g_item[g] = items + before.a;
-      g_base[g] = cols + before.b;
+      g_tile[g] = tiles + before.b;
     }
     items += total.a;
-    cols += total.b;
+    tiles += total.b;
   }
-  const int shared_items = items;
-  for (int base = 0; base < a.n; base += kPlan) {
-    const int i = base + tid;
-    Two mine = {0, 0};
-    int parts = 0;
-    if (i < a.n) {
-      Ent& e = a.ent[i];
-      const int g = e.group, c = group_cols(g);
-      e.shared = g_shared[g];
-      e.sh_parts = cut(c, g_shared[g], a.split_shared).parts;
-      e.sh_base = g_base[g];
-      e.c0 = (i - g_start[g]) * per_entry;
-      e.cols = c;
-      if (by_wave) {  // (entry, kv head) pairs in order, whose partial columns lie in the same order
-        parts = e.seq >= 0;
-        mine = {0, hkv * per_entry};
-      } else if (e.seq >= 0) {
-        const Cut x = cut(per_entry, pages_of(e.pos + a.tokens) - g_shared[g], a.split_own);
-        parts = x.parts;
-        mine = {hkv * x.chunks * parts, hkv * per_entry * parts};
-      }
-    }
-    Two total;
-    const Two before = scan_before(mine, sums, &total);
-    if (i < a.n) {
-      a.ent[i].own_parts = parts;
-      a.ent[i].own_base = cols + before.b;
-      o_item[i] = items + before.a;
-    }
-    items += total.a;
-    cols += total.b;
-  }
-  if (by_wave) items += (a.n * hkv + 3) / 4;
-  if (tid == 0) a.head[0] = min(items, a.max_items);
+  items = min(items, a.max_items);
+  if (tid == 0) a.head[0] = items;
   __syncthreads();
-
-  // the last of first[0 .. n) that is at most x (ascending; a segment without items begins where the next one does)
-  auto segment_of = [](const int* first, int n, int x) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first[mid] <= x) lo = mid;
+  for (int it = tid; it < items; it += NT) {
+    int g = 0, hi = n_groups;  // the last group that begins at or before this item
+    while (hi - g > 1) {
+      const int mid = (g + hi) >> 1;
+      if (g_item[mid] <= it) g = mid;
       else hi = mid;
     }
-    return lo;
-  };
-  for (int it = tid; it < min(items, a.max_items); it += kPlan) {
+    const int c = group_cols(g), parts = parts_of(g, steps);
+    const Cut x = cut_of(c, log_most);
+    // (heads fastest: workgroup id % 8, the XCD, is then the same for all chunks of a head where there are 8 heads or a
+    // multiple of them, and its pages come into one L2 only)
+    const int r = it - g_item[g], h = r % hkv, r1 = r / hkv, part = r1 % parts, chunk = r1 / parts;
     Item im = {};
-    if (it < shared_items) {
-      const int g = segment_of(g_item, n_groups, it), c = group_cols(g), tiles = g_shared[g];
-      const Cut x = cut(c, tiles, a.split_shared);
-      const int r = it - g_item[g], hs = r / x.chunks, h = hs / x.parts, s = hs - h * x.parts;
-      im.what = 0; im.e0 = g_start[g]; im.seq = a.ent[g_lead[g]].seq; im.head = h;
-      im.block = (r - hs * x.chunks) * x.waves_c;
-      im.t0 = (int)((long long)s * tiles / x.parts); im.t1 = (int)((long long)(s + 1) * tiles / x.parts);
-      im.base = g_base[g] + hs * c; im.cols = c; im.waves_c = x.waves_c;
-    } else if (by_wave) {
-      im.what = 2; im.e0 = 4 * (it - shared_items); im.seq = a.n * hkv; im.cols = per_entry; im.waves_c = 1;
-    } else {
-      const int i = segment_of(o_item, a.n, it), own = pages_of(a.ent[i].pos + a.tokens) - a.ent[i].shared, from = a.ent[i].shared;
-      const Cut x = cut(per_entry, own, a.split_own);
-      const int r = it - o_item[i], hs = r / x.chunks, h = hs / x.parts, s = hs - h * x.parts;
-      im.what = 1; im.e0 = i; im.seq = a.ent[i].seq; im.head = h;
-      im.block = (r - hs * x.chunks) * x.waves_c;
-      im.t0 = from + (int)((long long)s * own / x.parts); im.t1 = from + (int)((long long)(s + 1) * own / x.parts);
-      im.base = a.ent[i].own_base + hs * per_entry; im.cols = per_entry; im.waves_c = x.waves_c;
+    im.e0 = g_start[g]; im.seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im.head = h;
+    im.block0 = chunk * x.waves_c; im.waves_c = x.waves_c; im.part = part; im.parts = parts; im.cols = c;
+    im.shared = g_shared[g];
+    im.tile = g_tile[g] + (h * x.blocks + chunk * x.waves_c) * parts;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // the own pages of the block's entries, one behind the other; of the last entry those that its tokens of
+      // the block see
+      const int block = im.block0 + k, last_col = min(block * 32 + 31, c - 1);
+      if (k >= x.waves_c || block >= x.blocks) break;
+      const int lo = im.e0 + (block * 32) / per_entry, e = last_col / per_entry, hi = im.e0 + e;
+      const int seen = l_seq[hi] < 0 ? 0 : (l_pos[hi] + (last_col - e * per_entry) / grp) / kPage + 1 - g_shared[g];
+      im.own_at[k] = l_own[lo];
+      im.own_n[k] = l_own[hi] + seen - l_own[lo];
     }
     a.item[it] = im;
   }
@@ -311,9 +369,10 @@ struct AttendArgs {
   PoolView p;
   const int* head;
   const Ent* ent;
+  const Own* own;
   const Item* item;
-  float2* ml;  // [columns] reference point of the exponentials (log2 units) and sum
-  float* o;    // [columns][head_dim] unnormalised output
+  float2* ml;                // [part tiles][64 lanes] reference point of the exponentials (log2 units) and sum
+  float4* o;                 // [part tiles][head_dim / 8][64 lanes] four of a lane's sums of the output
   const bf16_t* q;
   long long q_stride;
   bf16_t* out;
@@ -340,182 +399,204 @@ __device__ inline uint32_t far_values(uint32_t x, bool lo, bool hi) {
   return (lo && (x & kExp) == kExp ? 0xffffu : 0u) | (hi && (x >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
 }
 
+// The result of a column: features 4 * quad' .. + 3 of 32 * ib + 8 * q4 + 4 * g from its sums 4 * quad .. + 3 (quad = 4 ib + q4)
 template <int HD, bool F16>
-__global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
-  constexpr int NC = HD / 16, NI = HD / 32;
-  __shared__ float park[4][2 + NI * 16][64];
+__device__ inline void store_out(const AttendArgs& a, int row, int h, int quad, int g, const float4& x, float inv, bool valid) {
+  const int f = h * HD + 32 * (quad >> 2) + 8 * (quad & 3) + 4 * g;
+  const uint2 y = valid ? make_uint2(pack2<F16>(x.x * inv, x.y * inv), pack2<F16>(x.z * inv, x.w * inv)) : make_uint2(0, 0);
+  *(uint2*)(a.kc_out > 0 ? a.out + frag_off(row, f, a.kc_out) : a.out + (size_t)row * a.n_q_heads * HD + f) = y;
+}
+
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
+  constexpr int NC = HD / 16, NI = HD / 32, REGS = NI * 16;
+  __shared__ float park[kWaves][2 + REGS][64];
   const PoolView& p = a.p;
+  read_args(a.head, a.item, a.ent, a.q, a.q_stride, a.out, a.kc_out, a.layer, a.tokens, a.n_q_heads, a.scale_log2e, p.data, p.table,
+            p.n_pages, p.max_pages, p.n_layers, p.n_kv_heads, a.ml, a.o, a.own);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
   const int n_items = ld_scalar(a.head);
-  const size_t tile = (size_t)kPage * HD, page = p.page();
+  const size_t tile = (size_t)kPage * HD, page = (size_t)p.n_layers * 2 * p.n_kv_heads * tile;
   for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
     const Item* im = a.item + it;
-    const int what = ld_scalar(&im->what);
-    int e0 = ld_scalar(&im->e0), seq = ld_scalar(&im->seq), hk = ld_scalar(&im->head), t0 = ld_scalar(&im->t0), t1 = ld_scalar(&im->t1);
-    int base = ld_scalar(&im->base);
-    const int cols = ld_scalar(&im->cols), wc = ld_scalar(&im->waves_c), wk = 4 / wc;
-    int block = ld_scalar(&im->block), step = 1, pos = 0;
-    bool idle = false;
-    if (what == 2) {
-      const int pair = e0 + w;
-      idle = pair >= seq;
-      e0 = idle ? 0 : pair / p.n_kv_heads;
-      hk = idle ? 0 : pair - e0 * p.n_kv_heads;
-      const Ent* e = a.ent + e0;
-      seq = ld_scalar(&e->seq);
-      idle = idle || seq < 0;
-      pos = ld_scalar(&e->pos);
-      t0 = ld_scalar(&e->shared);
-      t1 = idle ? t0 : (pos + a.tokens + kPage - 1) / kPage;
-      base = ld_scalar(&e->own_base) + hk * per_entry;
-    } else {
-      if (what == 1) pos = ld_scalar(&a.ent[e0].pos);
-      block += w & (wc - 1);
-      t0 += w / wc;
-      step = wk;
-      idle = block * 32 >= cols;
-      if (idle) t1 = t0;
-    }
+    const int e0 = ld_scalar(&im->e0), lead = ld_scalar(&im->seq), hk = ld_scalar(&im->head), wc = ld_scalar(&im->waves_c);
+    const int part = ld_scalar(&im->part), parts = ld_scalar(&im->parts), cols = ld_scalar(&im->cols), shared = ld_scalar(&im->shared);
+    const int tile0 = ld_scalar(&im->tile);
+    // this wave's block and its place among the block's waves (neighbours, on SIMDs of their own, read the same page)
+    const int wk = kWaves / wc, bw = w & (wc - 1), phase = w / wc;
+    const int block = ld_scalar(&im->block0) + bw;
+    const bool idle = block * 32 >= cols;
+
     // this lane's column
     const int c = block * 32 + j, cc = min(c, cols - 1);
     const int ei = cc / per_entry, ci = cc - ei * per_entry, ti = ci / grp, row = (e0 + ei) * a.tokens + ti;
     const int h = hk * grp + ci - ti * grp;
-    const bool masked = what != 0;
-    const int last = pos + ti;                 // own segments: this column's last visible position
-    const int end = pos + a.tokens;            // positions from here on were never written
+    const Ent mine = a.ent[e0 + ei];
+    const int last = mine.pos + ti;  // its last visible position
+    const bool valid = c < cols && mine.seq >= 0;
     uint4 qf[NC];
-    if (t0 < t1) {
+    {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)NC * 512 + (size_t)(((row & 31) + 32 * g) << 3)
                                        : a.q + (size_t)row * a.q_stride + (size_t)h * HD + 8 * g;
       const int q_step = a.q_stride < 0 ? 512 : 16;
 #pragma unroll
       for (int x = 0; x < NC; ++x) qf[x] = *(const uint4*)(q + (size_t)x * q_step);
     }
-    const bf16_t* kv = p.data + ((size_t)a.layer * 2 * p.n_kv_heads + hk) * tile + (size_t)lane * 8;
-    const size_t v_off = (size_t)p.n_kv_heads * tile;
-    const int* table = p.table + (size_t)max(seq, 0) * p.max_pages;
 
-    f32x16 o[NI];
-#pragma unroll
-    for (int ib = 0; ib < NI; ++ib)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    // pages of the next 64 tiles, one per lane (an index out of range reads page 0: the table is the caller's)
-    int ids = 0;
-    auto load_ids = [&](int kt) {
-      const int at = kt + lane * step;
-      ids = at < t1 ? table[at] : 0;
-      if ((unsigned)ids >= (unsigned)p.n_pages) {
-        ids = 0;
-        report(p, PAGES_BAD_ENTRY);
+    // The steps of this wave: every wk-th of the part's shared pages, then of its own pages (which go on where the shared ones
+    // stopped, so that the waves' numbers of steps differ by one at most).  A lane holds one step.
+    const int own_at = ld_scalar(im->own_at + bw), own_n = idle ? 0 : ld_scalar(im->own_n + bw);
+    const int s0 = (int)((long long)part * shared / parts), s1 = (int)((long long)(part + 1) * shared / parts);
+    const int o0 = (int)((long long)part * own_n / parts), o1 = (int)((long long)(part + 1) * own_n / parts);
+    const int sh0 = s0 + phase, ow0 = o0 + ((phase - (s1 - s0)) & (wk - 1));
+    const int n_shared = idle || sh0 >= s1 ? 0 : (s1 - sh0 + wk - 1) / wk;
+    const int n_steps = n_shared + (ow0 >= o1 ? 0 : (o1 - ow0 + wk - 1) / wk);
+    int st_page = 0, st_what = 0;  // page | valid positions << 24, tile | entry << 16 (an own page's)
+    auto load_steps = [&](int first) {
+      const int i = first + lane;
+      st_what = 0;
+      if (i < n_shared) {
+        st_page = p.table[(size_t)lead * p.max_pages + sh0 + i * wk];
+        if ((unsigned)st_page >= (unsigned)p.n_pages) {  // (the table is the caller's)
+          st_page = 0;
+          report(p, PAGES_BAD_ENTRY);
+        }
+      } else if (i < n_steps) {
+        const Own x = a.own[own_at + ow0 + (i - n_shared) * wk];
+        st_page = (int)x.page;
+        st_what = (int)x.what;
       }
     };
+
+    const bf16_t* kv = p.data + ((size_t)a.layer * 2 * p.n_kv_heads + hk) * tile + (size_t)lane * 8;
+    const size_t v_off = (size_t)p.n_kv_heads * tile;
     uint4 kf[NC];
-    auto tile_of = [&](int n) { return kv + (size_t)__builtin_amdgcn_readlane(ids, n) * page; };
+    auto tile_of = [&](int i) { return kv + (size_t)(__builtin_amdgcn_readlane(st_page, i) & 0xffffff) * page; };
     auto load_k = [&](const bf16_t* t) {
 #pragma unroll
       for (int x = 0; x < NC; ++x) kf[x] = *(const uint4*)(t + x * 512);
     };
-    const bf16_t* now = nullptr;
-    if (t0 < t1) {
-      load_ids(t0);
-      now = tile_of(0);
-      load_k(now);
-    }
-    int n_at = 0;
-    bool odd = false;
-    for (int kt = t0; kt < t1; kt += step) {
-      f32x16 s;
+    f32x16 o[NI];
+    float m, l;
+    bool odd;
+    // Once as a rule.  Where a column comes out infinite or NaN once more with care: V of a position may hold that, columns
+    // that do not see the position have weight 0 there, and 0 x NaN is not 0.
+    for (int care = 0; care < 2; ++care) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      for (int ib = 0; ib < NI; ++ib)
 #pragma unroll
-      for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
-      __builtin_amdgcn_sched_barrier(0);
-      uint4 vf[NI * 2];
+        for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
+      m = -INFINITY;
+      l = 0.f;
+      odd = false;
+      // 64 steps at a time, and no branch around a load inside (the compiler would wait for all loads behind it): the last step
+      // asks for its own K again
+      for (int first = 0; first < n_steps; first += 64) {
+       load_steps(first);
+       const bf16_t* now = tile_of(0);
+       load_k(now);
+       const int n64 = min(n_steps - first, 64);
+       for (int i = 0; i < n64; ++i) {
+        const bool own = first + i >= n_shared;
+        const int what = __builtin_amdgcn_readlane(st_what, i), kt = what & 0xffff;
+        const int held = __builtin_amdgcn_readlane(st_page, i) >> 24;  // positions of an own page that hold a token
+        uint4 vf[NI * 2];
 #pragma unroll
-      for (int t = 0; t < NI * 2; ++t) vf[t] = *(const uint4*)(now + v_off + t * 512);
-      if (kt + step < t1) {
-        if (++n_at == 64) {
-          load_ids(kt + step);
-          n_at = 0;
-        }
-        now = tile_of(n_at);
+        for (int t = 0; t < NI * 2; ++t) vf[t] = *(const uint4*)(now + v_off + t * 512);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+        for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
+        __builtin_amdgcn_sched_barrier(0);
+        now = tile_of(min(i + 1, n64 - 1));
         load_k(now);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      // register 4*q4 + e of a lane is key 32*kt + 8*q4 + 4*g + e
-      float tmax = -INFINITY;
+        __builtin_amdgcn_sched_barrier(0);
+        // register 4*q4 + e of a lane is key 32*kt + 8*q4 + 4*g + e
+        float tmax = -INFINITY;
+        if (own) {
+          const int see = ei == what >> 16 ? last - 32 * kt - 4 * g : -1;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int kp = 32 * kt + 8 * (i >> 2) + 4 * g + (i & 3);
-        s[i] = (!masked || kp <= last) ? s[i] * a.scale_log2e : -INFINITY;
-        tmax = fmaxf(tmax, s[i]);
-      }
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
-      const float m_new = fmaxf(m, tmax);
-      const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-      const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-      m = m_new;
-      float psum = 0.f;
+          for (int x = 0; x < 16; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] * a.scale_log2e : -INFINITY;
+        } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(s[i] - m_use);
-        psum += s[i];
-      }
-      l = l * alpha + psum;
-      uint4 pb[2];
+          for (int x = 0; x < 16; ++x) s[x] *= a.scale_log2e;
+        }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        pb[t].x = pack2<F16>(s[8 * t + 0], s[8 * t + 1]);
-        pb[t].y = pack2<F16>(s[8 * t + 2], s[8 * t + 3]);
-        pb[t].z = pack2<F16>(s[8 * t + 4], s[8 * t + 5]);
-        pb[t].w = pack2<F16>(s[8 * t + 6], s[8 * t + 7]);
-      }
-      if (masked && 32 * kt + 31 > pos) {
-        // V of positions that hold no token may be anything, NaN among it, and 0 x NaN is not 0.  Positions behind the
-        // first query are seen by some columns only: what is not finite there is left for behind the loop.
+        for (int x = 0; x < 16; ++x) tmax = fmaxf(tmax, s[x]);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+        const float m_new = fmaxf(m, tmax);
+        const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
+        m = m_new;
+        float psum = 0.f;
 #pragma unroll
-        for (int t = 0; t < NI * 2; ++t) {
-          uint32_t* x = (uint32_t*)&vf[t];
+        for (int x = 0; x < 16; ++x) {
+          s[x] = __builtin_amdgcn_exp2f(s[x] - m_use);
+          psum += s[x];
+        }
+        l = l * alpha + psum;
+        uint4 pb[2];
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int kp = 32 * kt + 16 * (t & 1) + 8 * (d >> 1) + 4 * g + 2 * (d & 1);
-            const uint32_t far = far_values<F16>(x[d], kp > pos, kp + 1 > pos);
-            const uint32_t seen = kp + 1 < end ? ~0u : kp < end ? 0xffffu : 0u;
-            odd |= (far & seen) != 0;
-            x[d] &= seen & ~far;
+        for (int t = 0; t < 2; ++t) {
+          pb[t].x = pack2<F16>(s[8 * t + 0], s[8 * t + 1]);
+          pb[t].y = pack2<F16>(s[8 * t + 2], s[8 * t + 3]);
+          pb[t].z = pack2<F16>(s[8 * t + 4], s[8 * t + 5]);
+          pb[t].w = pack2<F16>(s[8 * t + 6], s[8 * t + 7]);
+        }
+        if (own && (care || held < kPage)) {
+          // V of positions that hold no token may be anything
+#pragma unroll
+          for (int t = 0; t < NI * 2; ++t) {
+            uint32_t* x = (uint32_t*)&vf[t];
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const int kp = 16 * (t & 1) + 8 * (d >> 1) + 4 * g + 2 * (d & 1);
+              const uint32_t far = far_values<F16>(x[d], care, care);
+              const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
+              odd |= (far & seen) != 0;
+              x[d] &= seen & ~far;
+            }
           }
         }
+#pragma unroll
+        for (int ib = 0; ib < NI; ++ib) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[ib][x] *= alpha;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) o[ib] = mfma32<F16>(vf[ib * 2 + t], pb[t], o[ib]);
+        }
+       }
       }
+      if (care) break;
+      float worst = 0.f;  // (0 x infinity and 0 x NaN are NaN, and stay it)
 #pragma unroll
-      for (int ib = 0; ib < NI; ++ib) {
+      for (int ib = 0; ib < NI; ++ib)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[ib][i] *= alpha;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) o[ib] = mfma32<F16>(vf[ib * 2 + t], pb[t], o[ib]);
-      }
+        for (int x = 0; x < 16; ++x) worst = fmaf(o[ib][x], 0.f, worst);
+      if (!__any(worst != 0.f)) break;
     }
     l += __shfl_xor(l, 32);
-    if (masked && __any(odd)) {
-      // infinities and NaN of V where some columns see them and some do not: key by key, added where they are seen
-      for (int kt = t0; kt < t1; kt += step) {
-        if (32 * kt + 31 <= pos) continue;
-        const int pg = table[kt];
-        const bf16_t* at = kv + (size_t)((unsigned)pg < (unsigned)p.n_pages ? pg : 0) * page;
+    if (__builtin_expect(__any(odd), 0)) {
+      // key by key, added where it is seen
+      for (int i = n_shared; i < n_steps; ++i) {
+        const int at64 = (i - n_shared) & 63;
+        if (at64 == 0) load_steps(i);
+        const int what = __builtin_amdgcn_readlane(st_what, at64), kt = what & 0xffff, held = __builtin_amdgcn_readlane(st_page, at64) >> 24;
+        const int see = ei == what >> 16 ? last - 32 * kt : -1;  // this column's last key of the tile
+        const bf16_t* at = tile_of(at64);
         load_k(at);
         f32x16 s;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int x = 0; x < 16; ++x) s[x] = 0.f;
 #pragma unroll
         for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int kp = 32 * kt + 8 * (i >> 2) + 4 * g + (i & 3);
-          s[i] = kp <= last ? __builtin_amdgcn_exp2f(s[i] * a.scale_log2e - (m == -INFINITY ? 0.f : m)) : 0.f;
-        }
+        for (int x = 0; x < 16; ++x)
+          s[x] = 8 * (x >> 2) + 4 * g + (x & 3) <= see ? __builtin_amdgcn_exp2f(s[x] * a.scale_log2e - (m == -INFINITY ? 0.f : m)) : 0.f;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const uint4 pb = {pack2<F16>(s[8 * t], s[8 * t + 1]), pack2<F16>(s[8 * t + 2], s[8 * t + 3]),
@@ -524,8 +605,8 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
           for (int ib = 0; ib < NI; ++ib) {
             const uint4 v = *(const uint4*)(at + v_off + (ib * 2 + t) * 512);
             const uint32_t* x = (const uint32_t*)&v;
-            for (int k = max(pos + 1 - 32 * kt - 16 * t, 0); k < min(end - 32 * kt - 16 * t, 16); ++k) {
-              const bool here = g == (k >> 2 & 1), sees = 32 * kt + 16 * t + k <= last;
+            for (int k = 0; k < min(held - 16 * t, 16); ++k) {
+              const bool here = g == (k >> 2 & 1);
               uint4 only;
               uint32_t* y = (uint32_t*)&only;
 #pragma unroll
@@ -533,30 +614,20 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
                 y[d] = here && d == 2 * (k >> 3) + (k >> 1 & 1) ? x[d] & far_values<F16>(x[d], !(k & 1), k & 1) : 0u;
               f32x16 z;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) z[i] = 0.f;
+              for (int r = 0; r < 16; ++r) z[r] = 0.f;
               z = mfma32<F16>(only, pb, z);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[ib][i] += sees ? z[i] : 0.f;
+              for (int r = 0; r < 16; ++r) o[ib][r] += 16 * t + k <= see ? z[r] : 0.f;
             }
           }
         }
       }
     }
 
-    auto store = [&](int ib, const f32x16& x) {
-      float* d = a.o + (size_t)(base + c) * HD + 32 * ib + 4 * g;
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *(float4*)(d + 8 * q4) = make_float4(x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]);
-    };
-    if (what == 2 || wk == 1) {
-      if (!idle && c < cols) {
-#pragma unroll
-        for (int ib = 0; ib < NI; ++ib) store(ib, o[ib]);
-        if (g == 0) a.ml[base + c] = make_float2(m, l);
-      }
-    } else {
-      // the waves of a column block meet in LDS, a share of the feature blocks each, in the order of the waves
+    // The waves of a block meet in LDS, a share of the sums each, in the order of the waves; then the result, or the part.
+    auto meet = [&](auto count) {
+      constexpr int R = decltype(count)::value;
+      constexpr int WK = REGS / R;
       park[w][0][lane] = m;
       park[w][1][lane] = l;
 #pragma unroll
@@ -564,76 +635,93 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) park[w][2 + ib * 16 + i][lane] = o[ib][i];
       __syncthreads();
-      const int w0 = w & (wc - 1), share = w / wc;
-      float M = -INFINITY;
-      for (int x = 0; x < wk; ++x) M = fmaxf(M, park[w0 + x * wc][0][lane]);
+      const int r0 = phase * R;
+      float M = -INFINITY, L = 0.f, x[R];
+#pragma unroll
+      for (int y = 0; y < WK; ++y) M = fmaxf(M, park[bw + y * wc][0][lane]);
       const float m_use = M == -INFINITY ? 0.f : M;
-      float L = 0.f, f[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        f[x] = x < wk ? __builtin_amdgcn_exp2f(park[w0 + x * wc][0][lane] - m_use) : 0.f;
-        if (x < wk) L = fmaf(f[x], park[w0 + x * wc][1][lane], L);
+      for (int r = 0; r < R; ++r) x[r] = 0.f;
+#pragma unroll
+      for (int y = 0; y < WK; ++y) {
+        const float f = __builtin_amdgcn_exp2f(park[bw + y * wc][0][lane] - m_use);
+        L = fmaf(f, park[bw + y * wc][1][lane], L);
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = fmaf(f, park[bw + y * wc][2 + r0 + r][lane], x[r]);
       }
-      if (!idle && c < cols) {
-        for (int ib = share; ib < NI; ib += wk) {
-          f32x16 x;
+      if (!idle) {
+        if (parts > 1) {
+          const size_t at = (size_t)tile0 + bw * parts + part;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = 0.f;
+          for (int r = 0; r < R; r += 4)
+            a.o[(at * (REGS / 4) + (r0 + r) / 4) * 64 + lane] = make_float4(x[r], x[r + 1], x[r + 2], x[r + 3]);
+          if (r0 == 0) a.ml[at * 64 + lane] = make_float2(M, L);
+        } else if (c < cols) {
+          const float inv = 1.f / L;
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (y < wk) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = fmaf(f[y], park[w0 + y * wc][2 + ib * 16 + i][lane], x[i]);
-            }
-          store(ib, x);
+          for (int r = 0; r < R; r += 4)
+            store_out<HD, F16>(a, row, h, (r0 + r) / 4, g, make_float4(x[r], x[r + 1], x[r + 2], x[r + 3]), inv, valid);
         }
-        if (share == 0 && g == 0) a.ml[base + c] = make_float2(M, L);
       }
-      __syncthreads();
-    }
+      __syncthreads();  // (the next item parks here)
+    };
+    if (wc == 1) meet(std::integral_constant<int, REGS / 8>{});
+    else if (wc == 2) meet(std::integral_constant<int, REGS / 4>{});
+    else meet(std::integral_constant<int, REGS / 2>{});
   }
 }
 
-// A wave per row: the parts of its segments, shared ones first, in their order
+// Joins the parts.  The items of a (head, column blocks) deal its sums among themselves: a wave takes four sums of a block's
+// lanes, over all parts.
 template <int HD, bool F16>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+  constexpr int QUADS = HD / 8;
   const PoolView& p = a.p;
-  const int lane = threadIdx.x & 63;
-  const long long rh = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (rh >= (long long)a.n * a.tokens * a.n_q_heads) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
-  const int row = (int)(rh / a.n_q_heads), h = (int)(rh - (long long)row * a.n_q_heads);
-  const int i = row / a.tokens, t = row - i * a.tokens, hk = h / grp, ci = t * grp + h - hk * grp;
-  const Ent* e = a.ent + i;
-  const bool valid = ld_scalar(&e->seq) >= 0;
-  const int sp = valid ? ld_scalar(&e->sh_parts) : 0, op = valid ? ld_scalar(&e->own_parts) : 0;
-  const int cols = ld_scalar(&e->cols);
-  const size_t sh = ld_scalar(&e->sh_base) + (size_t)hk * sp * cols + ld_scalar(&e->c0) + ci;
-  const size_t ow = ld_scalar(&e->own_base) + (size_t)hk * op * per_entry + ci;
-  float2 s = make_float2(-INFINITY, 0.f), w = make_float2(-INFINITY, 0.f);
-  if (lane < sp) s = a.ml[sh + (size_t)lane * cols];
-  if (lane < op) w = a.ml[ow + (size_t)lane * per_entry];
-  float M = fmaxf(s.x, w.x);
+  const int n_items = ld_scalar(a.head);
+  for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+    const Item* im = a.item + it;
+    const int parts = ld_scalar(&im->parts), part = ld_scalar(&im->part), wc = ld_scalar(&im->waves_c), cols = ld_scalar(&im->cols);
+    const int e0 = ld_scalar(&im->e0), hk = ld_scalar(&im->head), block0 = ld_scalar(&im->block0), tile0 = ld_scalar(&im->tile);
+    if (parts < 2) continue;
+    for (int u = part + w * parts; u < wc * QUADS; u += 4 * parts) {
+      const int bw = u / QUADS, quad = u - bw * QUADS, block = block0 + bw;
+      if (block * 32 >= cols) continue;
+      const size_t at = (size_t)tile0 + bw * parts;
+      float M = -INFINITY, L = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s0 = 0; s0 < parts; s0 += 8) {  // eight parts in flight
+        float2 y[8];
+        float4 z[8];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
-  const float m_use = M == -INFINITY ? 0.f : M;
-  const float fs = __builtin_amdgcn_exp2f(s.x - m_use), fw = __builtin_amdgcn_exp2f(w.x - m_use);
-  float L = fs * s.y + fw * w.y;
+        for (int s = 0; s < 8; ++s) {
+          const size_t t = at + min(s0 + s, parts - 1);
+          y[s] = a.ml[t * 64 + lane];
+          z[s] = a.o[(t * QUADS + quad) * 64 + lane];
+        }
+        float top = M;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
-  constexpr int PER = HD / 64;
-  float acc[PER] = {};
-  auto add = [&](size_t col, float f) {
-    const float* o = a.o + col * HD + lane * PER;
+        for (int s = 0; s < 8; ++s) top = fmaxf(top, y[s].x);
+        const float m_use = top == -INFINITY ? 0.f : top, back = __builtin_amdgcn_exp2f(M - m_use);
+        M = top;
+        L *= back;
+        x.x *= back; x.y *= back; x.z *= back; x.w *= back;
 #pragma unroll
-    for (int x = 0; x < PER; ++x) acc[x] = fmaf(f, o[x], acc[x]);
-  };
-  for (int x = 0; x < sp; ++x) add(sh + (size_t)x * cols, __shfl(fs, x));
-  for (int x = 0; x < op; ++x) add(ow + (size_t)x * per_entry, __shfl(fw, x));
-  const float inv = valid ? 1.f / L : 0.f;
-  bf16_t* d = a.kc_out > 0 ? a.out + frag_off(row, h * HD + lane * PER, a.kc_out) : a.out + (size_t)rh * HD + lane * PER;
-  if (PER == 2) *(uint32_t*)d = pack2<F16>(acc[0] * inv, acc[PER - 1] * inv);
-  else *d = (bf16_t)pack2<F16>(acc[0] * inv, 0.f);
+        for (int s = 0; s < 8; ++s) {
+          const float f = s0 + s < parts ? __builtin_amdgcn_exp2f(y[s].x - m_use) : 0.f;
+          if (s0 + s < parts) {
+            L = fmaf(f, y[s].y, L);
+            x.x = fmaf(f, z[s].x, x.x); x.y = fmaf(f, z[s].y, x.y); x.z = fmaf(f, z[s].z, x.z); x.w = fmaf(f, z[s].w, x.w);
+          }
+        }
+      }
+      const int c = block * 32 + j;
+      if (c >= cols) continue;
+      const int ei = c / per_entry, ci = c - ei * per_entry, ti = ci / grp;
+      store_out<HD, F16>(a, (e0 + ei) * a.tokens + ti, hk * grp + ci - ti * grp, quad, g, x, 1.f / L, a.ent[e0 + ei].seq >= 0);
+    }
+  }
 }
 
 bool sizes_ok(const vlac_pages* p, int n, int tokens, int n_q_heads) {
@@ -654,35 +742,35 @@ int check_attend(const vlac_pages* pages, int n, int tokens, int n_q_heads, cons
 
 }  // namespace
 
-// 0: more partial columns than an int counts
 size_t attend_workspace(const PoolView& p, int n, int tokens, int n_q_heads) {
-  const Layout l = layout_of(n > 0 ? n : 1, tokens, n_q_heads, p.n_kv_heads, p.head_dim);
-  return l.max_cols > 0x7fffffffu || l.max_items > 0x7fffffffu ? 0 : l.total;
+  return layout_of(p, n > 0 ? n : 1, tokens, n_q_heads).total;
 }
 
 void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
                         const int* group, void* ws, hipStream_t st) {
-  const Layout l = layout_of(n, tokens, n_q_heads, p.n_kv_heads, p.head_dim);
+  const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const PlanArgs a = {p, seqs, pos, group, add, n, tokens, n_q_heads, l.split_shared, l.split_own, (int)l.max_items,
-                      (int*)b, (Ent*)(b + l.ent), (Item*)(b + l.item)};
-  hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlan), 0, st, a);
+  const PlanArgs a = {p, seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
+                      (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
+  // (one token of 2 candidates: 8.1 us with 4 waves, 9.8 with 16; 48 candidates with tables of 1027 pages: 40 and 20)
+  if (n <= 128 && (long long)n * p.max_pages <= 4096)
+    hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(1), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((attend_plan_kernel<1024, VLAC_PAGES_MAX_LIST>), dim3(1), dim3(1024), 0, st, a);
 }
 
 void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, int n_q_heads, const AttendIo& io, void* ws,
                    hipStream_t st) {
-  const Layout l = layout_of(n, tokens, n_q_heads, p.n_kv_heads, p.head_dim);
+  const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const AttendArgs a = {p, (const int*)b, (const Ent*)(b + l.ent), (const Item*)(b + l.item), (float2*)(b + l.ml), (float*)(b + l.o),
-                        io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens, n_q_heads,
-                        1.4426950408889634f / sqrtf((float)p.head_dim)};
-  const dim3 grid((unsigned)std::min<size_t>(l.max_items, 2 * kSlots));
-  const long long rows = (long long)n * tokens * n_q_heads;
-  const dim3 join((unsigned)((rows + 3) / 4));
-#define VLAC_ATTEND(HD_, F16_)                                                             \
-  {                                                                                        \
-    hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(256), 0, st, a);             \
-    hipLaunchKernelGGL((attend_join_kernel<HD_, F16_>), join, dim3(256), 0, st, a);        \
+  const AttendArgs a = {p, (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
+                        (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
+                        n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
+  const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
+#define VLAC_ATTEND(HD_, F16_)                                                                        \
+  {                                                                                                   \
+    hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);                \
+    if (l.parts) hipLaunchKernelGGL((attend_join_kernel<HD_, F16_>), join, dim3(256), 0, st, a);      \
   }
   if (p.head_dim == 128) {
     if (f16) VLAC_ATTEND(128, true) else VLAC_ATTEND(128, false)
