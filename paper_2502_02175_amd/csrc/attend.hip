@@ -47,7 +47,7 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   const size_t least = (cols + 31) / 32 * p.n_kv_heads, max_blocks = least + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
   // Parts where the column blocks do not fill the chip by themselves and the tables have room for lists that are long
   // for 8 waves (that decides whether the second kernel is launched: 2.5 us where it finds nothing to join)
-  l.parts = least < 2 * kCus && p.max_pages > 48;
+  l.parts = least < 2 * kCus && p.max_pages > 24;
   l.part_tiles = l.parts ? (int)std::min<size_t>(kPartTiles, max_blocks * kMaxParts) : 0;
   l.max_items = max_blocks + l.part_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -287,14 +287,16 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     if (most == 1) {
       steps = s_longest;
     } else if (n_groups <= 64) {
-      int items = 0;
+      int items = 0, most_steps = 0;  // (the steps that come of it: parts are bounded)
       bool joined = false;
       for (int g = 0; g < n_groups; ++g) {
+        const Cut x = cut_of(group_cols(g), log_most);
         const int parts = parts_of(g, steps);
-        items += hkv * cut_of(group_cols(g), log_most).chunks * parts;
+        items += hkv * x.chunks * parts;
+        most_steps = max(most_steps, (g_own[g] + parts * x.wk - 1) / (parts * x.wk));
         joined |= parts > 1;
       }
-      const float cost = (float)((items + kCus - 1) / kCus) * (float)(steps + 3) + (joined ? 3.f : 0.f);
+      const float cost = (float)((items + kCus - 1) / kCus) * (float)(most_steps + 3) + (joined ? 3.f : 0.f);
       best = (int)fminf(cost, 1e9f);  // (ties: the fewest parts)
       int who = lane;
 #pragma unroll
@@ -479,97 +481,110 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
       for (int x = 0; x < NC; ++x) kf[x] = *(const uint4*)(t + x * 512);
     };
     f32x16 o[NI];
-    float m, l;
-    bool odd;
-    // Once as a rule.  Where a column comes out infinite or NaN once more with care: V of a position may hold that, columns
-    // that do not see the position have weight 0 there, and 0 x NaN is not 0.
+#pragma unroll
+    for (int ib = 0; ib < NI; ++ib)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    // Scores (minus infinity: not seen) -> the weights as the second product's operand, and the sums so far in their units.  Register 4*q4 + e of a lane is key 8*q4 + 4*g + e of the tile.  The reference point of a column's
+    // exponentials follows its maximum only when that has grown by more than 8 (weights stay below 256): then the rescaling of
+    // the sums is rare.  (The decision is the column's own: its result does not depend on its neighbours.)
+    auto weigh = [&](f32x16& s, uint4(&pb)[2]) {
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) tmax = fmaxf(tmax, s[x]);
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * a.scale_log2e;  // (m is in units of log2)
+      float alpha = 1.f;
+      if (tmax > m + 8.f) {
+        alpha = __builtin_amdgcn_exp2f(m - tmax);  // (the first time 2^-inf = 0)
+        m = tmax;
+      }
+      const float m_use = m == -INFINITY ? 0.f : m;
+      float psum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -m_use));
+        psum += s[x];
+      }
+      l = fmaf(l, alpha, psum);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        pb[t].x = pack2<F16>(s[8 * t + 0], s[8 * t + 1]);
+        pb[t].y = pack2<F16>(s[8 * t + 2], s[8 * t + 3]);
+        pb[t].z = pack2<F16>(s[8 * t + 4], s[8 * t + 5]);
+        pb[t].w = pack2<F16>(s[8 * t + 6], s[8 * t + 7]);
+      }
+      if (__any(alpha != 1.f)) {
+#pragma unroll
+        for (int ib = 0; ib < NI; ++ib)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[ib][x] *= alpha;
+      }
+    };
+
+    bool odd = false;
+    // Once as a rule.  Where a column comes out infinite or NaN once more, from the beginning and with care: V of a position may
+    // hold that, columns that do not see the position have weight 0 there, and 0 x NaN is not 0.
     for (int care = 0; care < 2; ++care) {
+      if (care) {
 #pragma unroll
-      for (int ib = 0; ib < NI; ++ib)
+        for (int ib = 0; ib < NI; ++ib)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
-      m = -INFINITY;
-      l = 0.f;
-      odd = false;
+          for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
+      }
       // 64 steps at a time, and no branch around a load inside (the compiler would wait for all loads behind it): the last step
       // asks for its own K again
       for (int first = 0; first < n_steps; first += 64) {
-       load_steps(first);
-       const bf16_t* now = tile_of(0);
-       load_k(now);
-       const int n64 = min(n_steps - first, 64);
-       for (int i = 0; i < n64; ++i) {
-        const bool own = first + i >= n_shared;
-        const int what = __builtin_amdgcn_readlane(st_what, i), kt = what & 0xffff;
-        const int held = __builtin_amdgcn_readlane(st_page, i) >> 24;  // positions of an own page that hold a token
-        uint4 vf[NI * 2];
-#pragma unroll
-        for (int t = 0; t < NI * 2; ++t) vf[t] = *(const uint4*)(now + v_off + t * 512);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x16 s;
-#pragma unroll
-        for (int x = 0; x < 16; ++x) s[x] = 0.f;
-#pragma unroll
-        for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
-        __builtin_amdgcn_sched_barrier(0);
-        now = tile_of(min(i + 1, n64 - 1));
+        load_steps(first);
+        const bf16_t* now = tile_of(0);
         load_k(now);
-        __builtin_amdgcn_sched_barrier(0);
-        // register 4*q4 + e of a lane is key 32*kt + 8*q4 + 4*g + e
-        float tmax = -INFINITY;
-        if (own) {
-          const int see = ei == what >> 16 ? last - 32 * kt - 4 * g : -1;
+        const int n64 = min(n_steps - first, 64);
+        for (int i = 0; i < n64; ++i) {
+          const bool own = first + i >= n_shared;
+          const int what = __builtin_amdgcn_readlane(st_what, i), kt = what & 0xffff;
+          const int held = __builtin_amdgcn_readlane(st_page, i) >> 24;  // positions of an own page that hold a token
+          uint4 vf[NI * 2];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] * a.scale_log2e : -INFINITY;
-        } else {
+          for (int t = 0; t < NI * 2; ++t) vf[t] = *(const uint4*)(now + v_off + t * 512);
+          __builtin_amdgcn_sched_barrier(0);
+          f32x16 s;
 #pragma unroll
-          for (int x = 0; x < 16; ++x) s[x] *= a.scale_log2e;
-        }
+          for (int x = 0; x < 16; ++x) s[x] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) tmax = fmaxf(tmax, s[x]);
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
-        const float m_new = fmaxf(m, tmax);
-        const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-        m = m_new;
-        float psum = 0.f;
+          for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
+          __builtin_amdgcn_sched_barrier(0);
+          now = tile_of(min(i + 1, n64 - 1));
+          load_k(now);
+          __builtin_amdgcn_sched_barrier(0);
+          if (own) {
+            const int see = ei == what >> 16 ? last - 32 * kt - 4 * g : -1;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          s[x] = __builtin_amdgcn_exp2f(s[x] - m_use);
-          psum += s[x];
-        }
-        l = l * alpha + psum;
-        uint4 pb[2];
+            for (int x = 0; x < 16; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+          }
+          uint4 pb[2];
+          weigh(s, pb);
+          if (own && (care || held < kPage)) {
+            // V of positions that hold no token may be anything
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          pb[t].x = pack2<F16>(s[8 * t + 0], s[8 * t + 1]);
-          pb[t].y = pack2<F16>(s[8 * t + 2], s[8 * t + 3]);
-          pb[t].z = pack2<F16>(s[8 * t + 4], s[8 * t + 5]);
-          pb[t].w = pack2<F16>(s[8 * t + 6], s[8 * t + 7]);
-        }
-        if (own && (care || held < kPage)) {
-          // V of positions that hold no token may be anything
+            for (int t = 0; t < NI * 2; ++t) {
+              uint32_t* x = (uint32_t*)&vf[t];
 #pragma unroll
-          for (int t = 0; t < NI * 2; ++t) {
-            uint32_t* x = (uint32_t*)&vf[t];
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              const int kp = 16 * (t & 1) + 8 * (d >> 1) + 4 * g + 2 * (d & 1);
-              const uint32_t far = far_values<F16>(x[d], care, care);
-              const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
-              odd |= (far & seen) != 0;
-              x[d] &= seen & ~far;
+              for (int d = 0; d < 4; ++d) {
+                const int kp = 16 * (t & 1) + 8 * (d >> 1) + 4 * g + 2 * (d & 1);
+                const uint32_t far = far_values<F16>(x[d], care, care);
+                const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
+                odd |= (far & seen) != 0;
+                x[d] &= seen & ~far;
+              }
             }
           }
+#pragma unroll
+          for (int ib = 0; ib < NI; ++ib)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) o[ib] = mfma32<F16>(vf[ib * 2 + t], pb[t], o[ib]);
         }
-#pragma unroll
-        for (int ib = 0; ib < NI; ++ib) {
-#pragma unroll
-          for (int x = 0; x < 16; ++x) o[ib][x] *= alpha;
-#pragma unroll
-          for (int t = 0; t < 2; ++t) o[ib] = mfma32<F16>(vf[ib * 2 + t], pb[t], o[ib]);
-        }
-       }
       }
       if (care) break;
       float worst = 0.f;  // (0 x infinity and 0 x NaN are NaN, and stay it)
@@ -596,7 +611,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
         for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
 #pragma unroll
         for (int x = 0; x < 16; ++x)
-          s[x] = 8 * (x >> 2) + 4 * g + (x & 3) <= see ? __builtin_amdgcn_exp2f(s[x] * a.scale_log2e - (m == -INFINITY ? 0.f : m)) : 0.f;
+          s[x] = 8 * (x >> 2) + 4 * g + (x & 3) <= see ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const uint4 pb = {pack2<F16>(s[8 * t], s[8 * t + 1]), pack2<F16>(s[8 * t + 2], s[8 * t + 3]),
