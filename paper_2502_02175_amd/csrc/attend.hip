@@ -28,10 +28,10 @@ struct Ent { int seq, pos; };
 // A step over a page of an entry's own: page | valid positions of it << 24, tile | entry of the group << 16
 struct Own { uint32_t page, what; };
 // A work item: column blocks block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry e0, part `part` of
-// `parts` of their key tiles: the shared pages of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
+// `parts` of their key tiles: pages s0 .. s1 - 1 of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
 // tile: where block0's parts lie.
 struct Item {
-  int e0, seq, head, block0, waves_c, part, parts, cols, shared, tile, pad[2], own_at[4], own_n[4];
+  int e0, seq, head, block0, waves_c, part, parts, cols, s0, s1, tile, pad, own_at[4], own_n[4];
 };
 static_assert(sizeof(Item) == 80, "read as five 16-byte words");
 
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     int longest = 0;
     for (int g = tid; g < n_groups; g += NT) {
       const Cut x = cut_of(group_cols(g), log_most);
-      const int tiles = g_shared[g] + (int)(((long long)g_own[g] * entry_blocks + x.blocks - 1) / x.blocks);
+      const int tiles = g_shared[g] + (int)ceilf((float)g_own[g] * (float)entry_blocks / (float)max(x.blocks, 1));
       g_own[g] = tiles;  // (from here on: of the whole list of a block)
       work += (unsigned long long)x.blocks * tiles * hkv;
       longest = max(longest, (tiles + x.wk - 1) / x.wk);
@@ -347,23 +347,24 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     // (heads fastest: workgroup id % 8, the XCD, is then the same for all chunks of a head where there are 8 heads or a
     // multiple of them, and its pages come into one L2 only)
     const int r = it - g_item[g], h = r % hkv, r1 = r / hkv, part = r1 % parts, chunk = r1 / parts;
-    Item im = {};
-    im.e0 = g_start[g]; im.seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im.head = h;
-    im.block0 = chunk * x.waves_c; im.waves_c = x.waves_c; im.part = part; im.parts = parts; im.cols = c;
-    im.shared = g_shared[g];
-    im.tile = g_tile[g] + (h * x.blocks + chunk * x.waves_c) * parts;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    const int e0 = g_start[g], shared = g_shared[g], block0 = chunk * x.waves_c;
+    Item* im = a.item + it;
+    im->e0 = e0; im->seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im->head = h;
+    im->block0 = block0; im->waves_c = x.waves_c; im->part = part; im->parts = parts; im->cols = c;
+    im->s0 = part * shared / parts; im->s1 = (part + 1) * shared / parts;
+    im->tile = g_tile[g] + (h * x.blocks + block0) * parts;
+#pragma unroll 1
+    for (int k = 0; k < x.waves_c; ++k) {
       // the own pages of the block's entries, one behind the other; of the last entry those that its tokens of
-      // the block see
-      const int block = im.block0 + k, last_col = min(block * 32 + 31, c - 1);
-      if (k >= x.waves_c || block >= x.blocks) break;
-      const int lo = im.e0 + (block * 32) / per_entry, e = last_col / per_entry, hi = im.e0 + e;
-      const int seen = l_seq[hi] < 0 ? 0 : (l_pos[hi] + (last_col - e * per_entry) / grp) / kPage + 1 - g_shared[g];
-      im.own_at[k] = l_own[lo];
-      im.own_n[k] = l_own[hi] + seen - l_own[lo];
+      // the block see; and the part's share of them
+      const int block = block0 + k, last_col = min(block * 32 + 31, c - 1);
+      if (block >= x.blocks) break;
+      const int lo = e0 + (block * 32) / per_entry, e = last_col / per_entry, hi = e0 + e;
+      const int seen = l_seq[hi] < 0 ? 0 : (l_pos[hi] + (last_col - e * per_entry) / grp) / kPage + 1 - shared;
+      const int all = l_own[hi] + seen - l_own[lo], o0 = part * all / parts;
+      im->own_at[k] = l_own[lo] + o0;
+      im->own_n[k] = (part + 1) * all / parts - o0;
     }
-    a.item[it] = im;
   }
 }
 
@@ -424,10 +425,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
     const Item* im = a.item + it;
     const int e0 = ld_scalar(&im->e0), lead = ld_scalar(&im->seq), hk = ld_scalar(&im->head), wc = ld_scalar(&im->waves_c);
-    const int part = ld_scalar(&im->part), parts = ld_scalar(&im->parts), cols = ld_scalar(&im->cols), shared = ld_scalar(&im->shared);
+    const int part = ld_scalar(&im->part), parts = ld_scalar(&im->parts), cols = ld_scalar(&im->cols);
     const int tile0 = ld_scalar(&im->tile);
     // this wave's block and its place among the block's waves (neighbours, on SIMDs of their own, read the same page)
-    const int wk = kWaves / wc, bw = w & (wc - 1), phase = w / wc;
+    const int wc_log = wc >> 1, wk_log = 3 - wc_log, wk = 1 << wk_log, bw = w & (wc - 1), phase = w >> wc_log;  // (wc: 1, 2 or 4)
     const int block = ld_scalar(&im->block0) + bw;
     const bool idle = block * 32 >= cols;
 
@@ -450,11 +451,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     // The steps of this wave: every wk-th of the part's shared pages, then of its own pages (which go on where the shared ones
     // stopped, so that the waves' numbers of steps differ by one at most).  A lane holds one step.
     const int own_at = ld_scalar(im->own_at + bw), own_n = idle ? 0 : ld_scalar(im->own_n + bw);
-    const int s0 = (int)((long long)part * shared / parts), s1 = (int)((long long)(part + 1) * shared / parts);
-    const int o0 = (int)((long long)part * own_n / parts), o1 = (int)((long long)(part + 1) * own_n / parts);
-    const int sh0 = s0 + phase, ow0 = o0 + ((phase - (s1 - s0)) & (wk - 1));
-    const int n_shared = idle || sh0 >= s1 ? 0 : (s1 - sh0 + wk - 1) / wk;
-    const int n_steps = n_shared + (ow0 >= o1 ? 0 : (o1 - ow0 + wk - 1) / wk);
+    const int s0 = ld_scalar(&im->s0), s1 = ld_scalar(&im->s1);
+    const int sh0 = s0 + phase, ow0 = (phase - (s1 - s0)) & (wk - 1);
+    const int n_shared = idle || sh0 >= s1 ? 0 : (s1 - sh0 + wk - 1) >> wk_log;
+    const int n_steps = n_shared + (ow0 >= own_n ? 0 : (own_n - ow0 + wk - 1) >> wk_log);
     int st_page = 0, st_what = 0;  // page | valid positions << 24, tile | entry << 16 (an own page's)
     auto load_steps = [&](int first) {
       const int i = first + lane;

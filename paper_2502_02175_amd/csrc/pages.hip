@@ -85,140 +85,134 @@ struct PlanArgs {
   int* out_pos;
 };
 
-// What entry i asks for.  dst < 0: the entry is ignored.
-struct Entry {
-  int dst, src, held, pages, fresh, len;  // pages it holds before (and loses), pages after, fresh ones, length of the source
-};
+// What an entry asks for: the sequence that changes (-1: the entry is ignored) and its source, pages it holds before (and
+// loses, but for EXTEND), pages after, fresh ones, length of the source, first fresh page (in copy_dst)
+constexpr int kMost = VLAC_PAGES_MAX_LIST;
+struct Entries { int dst[kMost], src[kMost], held[kMost], pages[kMost], len[kMost], first[kMost + 1]; };
 
-template <int MODE>
-__device__ Entry entry_of(const PlanArgs& a, int i) {
-  const PoolView& p = a.p;
-  Entry e = {-1, 0, 0, 0, 0, 0};
-  const int d = a.dst[i];
-  const int ld = checked_len(p, d);
-  if (ld < 0 || ld_agent(p.is_dst() + d) != a.n - i) return e;  // (only the first entry of a sequence counts)
-  if (MODE == FORK) {
-    e.src = a.src[i];
-    e.len = checked_len(p, e.src);
-    if (e.len < 0 || ld_agent(p.is_src() + d) != 0) return e;
-    e.held = pages_of(ld);
-    e.pages = pages_of(e.len);
-    e.fresh = a.deep ? e.pages : (e.len % kPage != 0);
-  } else if (MODE == EXTEND) {
-    if ((long long)ld + a.tokens > (long long)p.max_pages * kPage || (a.want_len >= 0 && ld != a.want_len)) return e;
-    e.len = ld;
-    e.held = pages_of(ld);
-    e.pages = pages_of(ld + a.tokens);
-    e.fresh = e.pages - e.held;
-  } else {
-    e.len = a.tokens;
-    e.held = pages_of(ld);
-    e.pages = e.fresh = pages_of(a.tokens);
-  }
-  e.dst = d;
-  return e;
-}
-
-// One workgroup.  Everything or nothing: the destinations' pages are released, the fresh pages looked for, and if
-// they do not suffice the release is taken back.
+// One workgroup, which looks every entry up once and keeps it in LDS.  Everything or nothing: the destinations' pages are
+// released, the fresh pages looked for, and if they do not suffice the release is taken back.
 template <int MODE>
 __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
   __shared__ int sums[kPlan / 64 + 1];
-  __shared__ int first[kPlan];  // first fresh page (in copy_dst) of the entries of a round
+  __shared__ Entries es;
+  __shared__ int s_flags;  // 1: an entry is ignored, 2: pages are released
   const PoolView& p = a.p;
+  read_args(a.src, a.dst, a.n, a.tokens, a.deep, a.want_len, a.out_pos, p.refs, p.table, p.len, p.scratch, p.n_pages, p.max_seqs,
+            p.max_pages);
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   int* const fresh_pages = p.copy_dst();
+  if (tid == 0) s_flags = 0;
 
+  // Only the first entry of a sequence counts, and none whose sequence is a source.  Short lists are compared in LDS, long ones
+  // by marks in the scratch (a round trip more, but no square of the length).
+  const bool marks = a.n > 256;
   for (int i = tid; i < a.n; i += kPlan) {
-    const int d = a.dst[i];
-    if ((unsigned)d < (unsigned)p.max_seqs) atomicMax(p.is_dst() + d, a.n - i);
-    if (MODE == FORK) {
-      const int s = a.src[i];
-      if ((unsigned)s < (unsigned)p.max_seqs) atomicOr(p.is_src() + s, 1);
+    const int d = a.dst[i], s = MODE == FORK ? a.src[i] : 0;
+    es.dst[i] = d;
+    es.src[i] = s;
+    if (marks) {
+      if ((unsigned)d < (unsigned)p.max_seqs) atomicMax(p.is_dst() + d, a.n - i);
+      if (MODE == FORK && (unsigned)s < (unsigned)p.max_seqs) atomicOr(p.is_src() + s, 1);
     }
   }
-  meet();
-
+  if (marks) meet();
+  else __syncthreads();
   int need = 0;
-  bool bad = false;
-  for (int i = tid; i < a.n; i += kPlan) {
-    const Entry e = entry_of<MODE>(a, i);
-    bad |= e.dst < 0;
-    need += e.fresh;
+  for (int base = 0; base < a.n; base += kPlan) {
+    const int i = base + tid;
+    int fresh = 0, d = -1;
+    if (i < a.n) {
+      d = es.dst[i];
+      const int s = es.src[i];
+      const int ld = checked_len(p, d), ls = MODE == FORK ? checked_len(p, s) : 0;
+      bool ok = ld >= 0 && ls >= 0;
+      if (marks) {
+        ok = ok && ld_agent(p.is_dst() + d) == a.n - i && (MODE != FORK || ld_agent(p.is_src() + d) == 0);
+      } else {
+        for (int k = 0; k < a.n; ++k) ok = ok && !(k < i && es.dst[k] == d) && !(MODE == FORK && es.src[k] == d);
+      }
+      if (MODE == EXTEND)
+        ok = ok && (long long)ld + a.tokens <= (long long)p.max_pages * kPage && (a.want_len < 0 || ld == a.want_len);
+      const int len = MODE == FORK ? ls : MODE == EXTEND ? ld : a.tokens;
+      const int held = ok ? pages_of(ld) : 0, pages = ok ? pages_of(MODE == EXTEND ? ld + a.tokens : len) : 0;
+      if (ok) fresh = MODE == EXTEND ? pages - held : MODE == IMPORT || a.deep ? pages : (len % kPage != 0);
+      es.held[i] = held;
+      es.pages[i] = pages;
+      es.len[i] = len;
+      if (!ok) atomicOr(&s_flags, 1);
+      else if (MODE != EXTEND && held > 0) atomicOr(&s_flags, 2);
+      d = ok ? d : -1;
+    }
+    int total;
+    const int before = scan_before(fresh, sums, &total);  // (everybody is through with es.dst of others here)
+    if (i < a.n) {
+      es.first[i] = need + before;
+      if (!marks) es.dst[i] = d;
+    }
+    if (marks && i < a.n) es.dst[i] = d;
+    need += total;
   }
-  if (bad) report(p, PAGES_BAD_ENTRY);
+  __syncthreads();
+  if (tid == 0 && (s_flags & 1)) report(p, PAGES_BAD_ENTRY);
+  const bool releases = (s_flags & 2) != 0;
   // (by `by` = -1 released, by +1 taken back)
   auto release = [&](int by) {
     for (int i = w; i < a.n; i += kPlan / 64) {
-      const Entry e = entry_of<MODE>(a, i);
-      if (e.dst < 0) continue;
-      for (int j = lane; j < e.held; j += 64) {
-        const int pg = p.table[(size_t)e.dst * p.max_pages + j];
+      const int d = es.dst[i];
+      if (d < 0) continue;
+      for (int j = lane; j < es.held[i]; j += 64) {
+        const int pg = p.table[(size_t)d * p.max_pages + j];
         if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, by);
       }
     }
   };
-  if (MODE != EXTEND) release(-1);
+  if (releases) {
+    release(-1);
+    meet();
+  }
+  const int found = need > 0 ? lowest_free(p, min(need, p.n_pages), fresh_pages, sums) : 0;
   meet();
-  int want;
-  (void)scan_before(need, sums, &want);
-  const int found = want > 0 ? lowest_free(p, min(want, p.n_pages), fresh_pages, sums) : 0;
-  meet();
-  const bool room = found >= want;
+  const bool room = found >= need;
   if (!room) {
-    if (MODE != EXTEND) release(1);
+    if (releases) release(1);
     if (tid == 0) report(p, PAGES_NO_ROOM);
   }
-  if (tid == 0) p.scratch[PG_COPIES] = room && MODE != EXTEND ? want : 0;
-
-  int given = 0;
-  for (int base = 0; base < a.n; base += kPlan) {
-    const int i = base + tid;
-    Entry e = {-1, 0, 0, 0, 0, 0};
-    if (i < a.n) e = entry_of<MODE>(a, i);
-    int total;
-    first[tid] = given + scan_before(e.fresh, sums, &total);
-    given += total;
-    if (MODE == EXTEND && i < a.n) a.out_pos[i] = room && e.dst >= 0 ? e.len : -1;
-    __syncthreads();
-    if (room) {
-      const int end = min(kPlan, a.n - base);
-      for (int k = w; k < end; k += kPlan / 64) {
-        const Entry e = entry_of<MODE>(a, base + k);
-        if (e.dst < 0) continue;
-        int* const row = p.table + (size_t)e.dst * p.max_pages;
-        const int* const from = p.table + (size_t)e.src * p.max_pages;
-        const int whole = MODE == FORK && !a.deep ? e.len / kPage : 0;  // pages shared with the source
-        for (int j = (MODE == EXTEND ? e.held : 0) + lane; j < max(e.held, e.pages); j += 64) {
-          int pg = -1;
-          if (j < e.pages) {
-            if (j < whole) {
-              pg = from[j];
-            } else {
-              const int f = first[k] + j - (MODE == EXTEND ? e.held : whole);
-              pg = fresh_pages[f];
-              if (MODE == FORK) p.copy_src()[f] = from[j];
-              if (MODE == IMPORT) p.copy_src()[f] = ((base + k) << 16) | j;
-            }
-            if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, 1);
+  if (tid == 0) p.scratch[PG_COPIES] = room && MODE != EXTEND ? need : 0;
+  if (MODE == EXTEND)
+    for (int i = tid; i < a.n; i += kPlan) a.out_pos[i] = room && es.dst[i] >= 0 ? es.len[i] : -1;
+  if (room) {
+    for (int i = w; i < a.n; i += kPlan / 64) {
+      const int d = es.dst[i];
+      if (d < 0) continue;
+      const int held = es.held[i], pages = es.pages[i], len = es.len[i], first = es.first[i];
+      int* const row = p.table + (size_t)d * p.max_pages;
+      const int* const from = p.table + (size_t)es.src[i] * p.max_pages;
+      const int kept = MODE == EXTEND ? held : MODE == FORK && !a.deep ? len / kPage : 0;  // pages that are not fresh
+      for (int j = (MODE == EXTEND ? held : 0) + lane; j < max(held, pages); j += 64) {
+        int pg = -1;
+        if (j < pages) {
+          if (j < kept) {
+            pg = from[j];
+          } else {
+            const int f = first + j - kept;
+            pg = fresh_pages[f];
+            if (MODE == FORK) p.copy_src()[f] = from[j];
+            if (MODE == IMPORT) p.copy_src()[f] = i << 16 | j;
           }
-          row[j] = pg;
+          if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, 1);
         }
+        row[j] = pg;
       }
-      __syncthreads();  // (len is what entry_of reads; it changes when every wave is through)
-      if (e.dst >= 0) p.len[e.dst] = MODE == EXTEND ? e.len + a.tokens : e.len;
+      if (lane == 0) p.len[d] = MODE == EXTEND ? len + a.tokens : len;
     }
-    __syncthreads();
   }
-  meet();
-  for (int i = tid; i < a.n; i += kPlan) {
-    const int d = a.dst[i];
-    if ((unsigned)d < (unsigned)p.max_seqs) p.is_dst()[d] = 0;
-    if (MODE == FORK) {
-      const int s = a.src[i];
+  if (marks)
+    for (int i = tid; i < a.n; i += kPlan) {
+      const int d = a.dst[i], s = MODE == FORK ? a.src[i] : -1;
+      if ((unsigned)d < (unsigned)p.max_seqs) p.is_dst()[d] = 0;
       if ((unsigned)s < (unsigned)p.max_seqs) p.is_src()[s] = 0;
     }
-  }
 }
 
 // copy_src -> copy_dst, whole pages; how many of them only the device knows.  A workgroup takes 16 KiB at a time, four
@@ -305,23 +299,45 @@ __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* 
   }
 }
 
-// One workgroup: counts the pages in use, then pairs those at or beyond the count with the free ones below it
+// One workgroup: counts the pages in use, then pairs those at or beyond the count with the free ones below it.  A thread
+// takes 8 pages side by side, all of them asked for at once.
 __global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* out_live) {
   __shared__ int sums[kPlan / 64 + 1];
+  constexpr int PER = 8, ROUND = PER * kPlan;
+  read_args(p.refs, p.scratch, p.n_pages, out_live);
   const int tid = threadIdx.x;
+  int used = 0;  // bits of this thread's pages (of the last round)
+  auto look = [&](int base) {
+    int r[PER];
+    const int at = base + PER * tid;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) r[e] = at + e < p.n_pages ? p.refs[at + e] : 0;
+    used = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) used |= (r[e] > 0) << e;
+  };
   int mine = 0;
-  for (int i = tid; i < p.n_pages; i += kPlan) mine += p.refs[i] > 0;
+  for (int base = 0; base < p.n_pages; base += ROUND) {
+    look(base);
+    mine += __popc(used);
+  }
   int live;
   (void)scan_before(mine, sums, &live);
   int holes = 0, moves = 0;  // (equal in the end)
-  for (int base = 0; base < p.n_pages; base += kPlan) {
-    const int i = base + tid;
-    const bool in = i < p.n_pages, used = in && p.refs[i] > 0;
-    const bool hole = in && i < live && !used, move = in && i >= live && used;
+  for (int base = 0; base < p.n_pages; base += ROUND) {
+    if (p.n_pages > ROUND) look(base);
+    const int at = base + PER * tid;
+    const int below = live <= at ? 0 : live >= at + PER ? (1 << PER) - 1 : (1 << (live - at)) - 1;
+    const int in = p.n_pages >= at + PER ? (1 << PER) - 1 : p.n_pages <= at ? 0 : (1 << (p.n_pages - at)) - 1;
+    const int hole = ~used & below & in, move = used & ~below;
     int total;
-    const int rank = scan_before((hole ? 1 << 16 : 0) + (move ? 1 : 0), sums, &total);
-    if (hole) p.copy_dst()[holes + (rank >> 16)] = i;
-    if (move) p.copy_src()[moves + (rank & 0xffff)] = i;
+    const int before = scan_before(__popc(hole) << 16 | __popc(move), sums, &total);
+    int to = holes + (before >> 16), from = moves + (before & 0xffff);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      if (hole >> e & 1) p.copy_dst()[to++] = at + e;
+      if (move >> e & 1) p.copy_src()[from++] = at + e;
+    }
     holes += total >> 16;
     moves += total & 0xffff;
   }
@@ -339,55 +355,84 @@ __global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* o
   }
 }
 
-// K and V of new tokens.  A thread takes 8 features of one row: 16 bytes of a K tile, 8 values of a V tile
-// 16 bytes apart.  TILES: the rows come from tiles (one token per entry), else from rows.
+// K and V of new tokens.  A wave takes 64 features of a head at 8 positions that lie side by side in a page (so that what is
+// asked of the tables is one page, by scalar loads, and a K store of 8 lanes is a line): 16 bytes of a row per lane for
+// K, and for V, whose 4 neighbouring positions lie side by side, turned round in LDS, a feature per lane.
+// TILES: the rows come from tiles (one token per entry), else from rows.
 struct AppendArgs {
   PoolView p;
-  int layer, n, tokens, add;
+  int layer, n, tokens, add, blocks;  // blocks: of 8 positions that an entry's tokens may touch
   const int *seqs, *pos;
   const bf16_t *k, *v;
   long long row_stride;
 };
 template <bool TILES>
 __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
+  __shared__ uint4 turn[4][64];
   const PoolView& p = a.p;
-  const int c8 = p.head_dim / 8, per_row = p.n_kv_heads * c8;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long row = at / per_row;
-  if (row >= (long long)a.n * a.tokens) return;
-  const int x = (int)(at - row * per_row), h = x / c8, f = (x - h * c8) * 8;
-  const int i = (int)(row / a.tokens), t = (int)(row - (long long)i * a.tokens);
-  const int p0 = a.pos[i], s = a.seqs[i];
+  read_args(a.layer, a.n, a.tokens, a.add, a.blocks, a.seqs, a.pos, a.k, a.v, a.row_stride, p.data, p.refs, p.table, p.len, p.n_pages,
+            p.max_seqs, p.max_pages, p.n_layers, p.n_kv_heads, p.head_dim);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7, r8 = lane >> 3;
+  const int per_block = p.n_kv_heads * (p.head_dim >> 6);  // waves for a block of positions
+  const int u = blockIdx.x * 4 + w, ib = u / per_block, hf = u - ib * per_block, i = ib / a.blocks, blk = ib - i * a.blocks;
+  if (i >= a.n) return;
+  const int h = hf / (p.head_dim >> 6), f0 = (hf - h * (p.head_dim >> 6)) * 64;
+  const int p0 = ld_scalar(a.pos + i), s = ld_scalar(a.seqs + i);
   if (p0 < 0) return;
-  const int l = checked_len(p, s);
-  const long long at_pos = (long long)p0 + a.add + t;
-  int pg = -1;
-  if (l >= 0 && at_pos < l) pg = p.table[(size_t)s * p.max_pages + at_pos / kPage];
-  if ((unsigned)pg >= (unsigned)p.n_pages || p.refs[pg] != 1) {
-    report(p, PAGES_BAD_ENTRY);
+  const long long first = (long long)p0 + a.add, at8 = (first / 8 + blk) * 8;  // the block's first position
+  if (at8 >= first + a.tokens) return;
+  const int t = (int)(at8 + r8 - first);  // this lane's token
+  const bool mine = t >= 0 && t < a.tokens;
+  // (the values are asked for before it is known whether they have a place)
+  uint4 k8 = make_uint4(0, 0, 0, 0), v8 = k8;
+  if (!TILES && mine) {
+    const size_t src = ((size_t)i * a.tokens + t) * a.row_stride + (size_t)h * p.head_dim + f0 + 8 * c;
+    k8 = *(const uint4*)(a.k + src);
+    v8 = *(const uint4*)(a.v + src);
+  }
+  const bool known = (unsigned)s < (unsigned)p.max_seqs;
+  const int l = known ? ld_scalar(p.len + s) : -1;
+  const long long j = at8 / kPage;
+  int pg = known && j < p.max_pages ? ld_scalar(p.table + (size_t)s * p.max_pages + j) : -1;
+  const bool whole = l >= 0 && l <= p.max_pages * kPage && min(at8 + 8, first + a.tokens) <= l;  // (all of the block's tokens lie inside)
+  if ((unsigned)pg >= (unsigned)p.n_pages || ld_scalar(p.refs + pg) != 1) pg = -1;
+  if (lane == 0 && (pg < 0 || !whole)) report(p, PAGES_BAD_ENTRY);
+  if (pg < 0 || l < 0 || l > p.max_pages * kPage) return;
+  const bool store = mine && at8 + r8 < l;
+  const int r = ((int)at8 & 31) + r8;
+  const size_t tile = p.tile();
+  bf16_t* kd = p.data + (size_t)pg * p.page() + ((size_t)a.layer * 2 * p.n_kv_heads + h) * tile + (size_t)f0 * 32;
+  bf16_t* vd = kd + p.n_kv_heads * tile;
+  const size_t k_at = (size_t)(c >> 1) * 512 + (c & 1) * 256 + r * 8;  // (f0: 64 features are 2048 values of either tile)
+  // feature f0 + lane at position (at8 & 31) + 4 g of the V tile
+  auto v_at = [&](int g) { return (size_t)(lane >> 5) * 1024 + (((int)at8 & 31) >> 4) * 512 + g * 256 + (lane & 31) * 8 + (((int)at8 >> 3) & 1) * 4; };
+  if (TILES) {
+    const bf16_t* ks = a.k + ((size_t)i * 2 * p.n_kv_heads + h) * tile + (size_t)f0 * 32;
+    const bf16_t* vs = ks + p.n_kv_heads * tile;
+    if (store) *(uint4*)(kd + k_at) = *(const uint4*)(ks + k_at);
+    const int one = (int)(first - at8);  // the token's place among the 8 positions (inside: checked above)
+    const size_t x = v_at(one >> 2) + (one & 3);
+    if (first < l) vd[x] = vs[x];
     return;
   }
-  const int r = (int)at_pos & 31;
-  const size_t tile = p.tile();
-  bf16_t* kd = p.data + (size_t)pg * p.page() + ((size_t)a.layer * 2 * p.n_kv_heads + h) * tile;
-  bf16_t* vd = kd + p.n_kv_heads * tile;
-  const size_t k_at = (size_t)(f >> 4) * 512 + (size_t)((f >> 3) & 1) * 256 + r * 8;
-  const size_t v_at = (size_t)(f >> 5) * 1024 + (r >> 4) * 512 + ((r >> 2) & 1) * 256 + (f & 31) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
-  if (TILES) {
-    const bf16_t* ks = a.k + ((size_t)i * 2 * p.n_kv_heads + h) * tile;
-    const bf16_t* vs = ks + p.n_kv_heads * tile;
-    *(uint4*)(kd + k_at) = *(const uint4*)(ks + k_at);
+  if (store) *(uint4*)(kd + k_at) = k8;
+  turn[w][lane] = v8;  // [position][64 features]
+  asm volatile("" ::: "memory");  // (read as another type below: the order is the wave's own, if the compiler keeps it)
+  const bf16_t* rows = (const bf16_t*)turn[w] + lane;
+  const unsigned long long places = __ballot(store);  // (8 lanes each)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vd[v_at + e * 8] = vs[v_at + e * 8];
-  } else {
-    const size_t src = (size_t)row * a.row_stride + (size_t)h * p.head_dim + f;
-    *(uint4*)(kd + k_at) = *(const uint4*)(a.k + src);
-    const uint4 v8 = *(const uint4*)(a.v + src);
-    const uint32_t two[4] = {v8.x, v8.y, v8.z, v8.w};
+  for (int g = 0; g < 2; ++g) {
+    uint32_t y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      vd[v_at + e * 16] = (bf16_t)two[e];
-      vd[v_at + e * 16 + 8] = (bf16_t)(two[e] >> 16);
+    for (int e = 0; e < 4; ++e) y[e] = rows[(4 * g + e) * 64];
+    bf16_t* d = vd + v_at(g);
+    const uint32_t four = (uint32_t)(places >> (32 * g));
+    if (four == 0xffffffffu) {
+      *(uint2*)d = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (four >> (8 * e) & 1) d[e] = (bf16_t)y[e];
     }
   }
 }
@@ -427,16 +472,17 @@ void launch_extend(const PoolView& p, const int* seqs, int n, int tokens, int wa
   hipLaunchKernelGGL(pages_plan_kernel<EXTEND>, dim3(1), dim3(kPlan), 0, st, a);
 }
 
-static void launch_append(bool tiles, const AppendArgs& a, hipStream_t st) {
-  const long long threads = (long long)a.n * a.tokens * a.p.n_kv_heads * (a.p.head_dim / 8);
-  const dim3 grid((unsigned)((threads + 255) / 256));
+static void launch_append(bool tiles, AppendArgs a, hipStream_t st) {
+  a.blocks = (a.tokens + 14) / 8;
+  const long long waves = (long long)a.n * a.blocks * a.p.n_kv_heads * (a.p.head_dim / 64);
+  const dim3 grid((unsigned)((waves + 3) / 4));
   if (tiles) hipLaunchKernelGGL(pages_append_kernel<true>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(pages_append_kernel<false>, grid, dim3(256), 0, st, a);
 }
 
 void launch_append_tiles(const PoolView& p, int layer, const int* seqs, const int* pos, int add, int n,
                          const bf16_t* tiles, hipStream_t st) {
-  const AppendArgs a = {p, layer, n, 1, add, seqs, pos, tiles, nullptr, 0};
+  const AppendArgs a = {p, layer, n, 1, add, 0, seqs, pos, tiles, nullptr, 0};
   launch_append(true, a, st);
 }
 
@@ -528,7 +574,7 @@ int vlac_pages_append(const vlac_pages* pages, int layer, const int32_t* seqs, c
   if (n == 0) return VLAC_OK;
   if (!seqs || !pos || !k || !v) return VLAC_E_NULL;
   if ((uintptr_t)k % 16 || (uintptr_t)v % 16) return VLAC_E_SHAPE;
-  const AppendArgs a = {pool_view(pages), layer, n, tokens, 0, seqs, pos, (const bf16_t*)k, (const bf16_t*)v, row_stride};
+  const AppendArgs a = {pool_view(pages), layer, n, tokens, 0, 0, seqs, pos, (const bf16_t*)k, (const bf16_t*)v, row_stride};
   launch_append(false, a, (hipStream_t)stream);
   return launched();
 }
