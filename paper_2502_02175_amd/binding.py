@@ -382,6 +382,8 @@ def pages(n_layers, n_kv_heads, head_dim, operand_dtype, data, refs, table, leng
     p.tensors = (data, refs, table, length, scratch)
     p.index = refs.get_device()
     p.torch = torch
+    p.i32 = torch.int32
+    p.raw_stream = torch._C._cuda_getCurrentRawStream
     p.rows_dtype = torch.bfloat16 if operand_dtype == OPERAND_BF16 else torch.float16
     p.data = _at(p, data, None, 0, "data")
     p.refs, p.table = _at(p, refs, torch.int32, 0, "refs"), _at(p, table, torch.int32, 0, "table")
@@ -408,19 +410,19 @@ def _at(p, x, dtype, n, name):
     """Address of a contiguous tensor of at least n values on the pool's device (an address or None as it is)."""
     if x is None or isinstance(x, int):
         return x
+    if x.get_device() == p.index >= 0 and (dtype is None or x.dtype is dtype) and x.numel() >= n and x.is_contiguous():
+        return x.data_ptr()
     if x.get_device() != p.index or p.index < 0:
         raise ValueError("%s lies on %s, the pool on GPU %d" % (name, x.device, p.index))
     if dtype is not None and x.dtype != dtype:
         raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, dtype))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if x.numel() < n:
-        raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
-    return x.data_ptr()
+    raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
 
 
 def _list(p, x, n, name):
-    return _at(p, x, p.torch.int32, n, name)
+    return _at(p, x, p.i32, n, name)
 
 
 def _rows(p, x, count, width, name):
@@ -442,15 +444,16 @@ def _rows(p, x, count, width, name):
 
 def _call(p, name, stream, check, *args):
     """One library call on the pool's device."""
-    fn, index = getattr(lib(), name), getattr(p, "index", -1)
+    fn, index = getattr(_LIB or lib(), name), getattr(p, "index", -1)
     if index < 0:                      # (no pool, or one of bare addresses: the current device's)
         return _ret(fn(*args, _stream(stream)), name, check)
-    cuda = p.torch.cuda
-    raw = p.torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
-    if cuda.current_device() == index:
-        return _ret(fn(*args, raw), name, check)
-    with cuda.device(index):
-        return _ret(fn(*args, raw), name, check)
+    raw = p.raw_stream(index) if stream is None else _stream(stream)
+    if p.torch.cuda.current_device() == index:
+        status = fn(*args, raw)
+    else:
+        with p.torch.cuda.device(index):
+            status = fn(*args, raw)
+    return status if status == VLAC_OK else _ret(status, name, check)
 
 
 def _ref(p):
