@@ -389,12 +389,14 @@ int vlac_pages_compact(const vlac_pages* pages, int32_t* out_live, void* stream)
  *
  * vlac_attend_plan looks at the tables once (for all layers of a pass) and leaves in the workspace how the work is cut;
  * vlac_attend_shared runs one layer with it.  Between the two, and while passes on a workspace run, nothing else may
- * use that workspace, and the sequences' tables must stay.
+ * use that workspace (two graphs that share one must not run at once), and the sequences' tables must stay.  A workspace
+ * whose plan is for another pool, n, tokens or n_q_heads, or that holds none, is not used: out stays as it is, and
+ * vlac_pages_check reports it.
  * An entry whose pos is negative, or that does not fit (reported), gets rows of zeros.
  * n <= VLAC_PAGES_MAX_LIST, tokens <= 65536, n * tokens <= 2^20; n_q_heads is a multiple of n_kv_heads, at most 1024.
  * q: device, row (i, t) at element (i * tokens + t) * q_stride, in it [n_q_heads][head_dim] values of the pool's type;
  * q_stride >= n_q_heads * head_dim and a multiple of 8.  out: device [n, tokens, n_q_heads, head_dim], same type.
- * workspace: device, vlac_attend_workspace_bytes (0 if the arguments are not allowed), 16-byte aligned. */
+ * out 8-byte aligned.  workspace: device, vlac_attend_workspace_bytes (0 if the arguments are not allowed), 16-byte aligned. */
 size_t vlac_attend_workspace_bytes(const vlac_pages* pages, int n, int tokens, int n_q_heads);
 int vlac_attend_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens,
                      int n_q_heads, const int32_t* group, void* workspace, size_t workspace_bytes,

@@ -60,11 +60,27 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   return l;
 }
 
+// What a plan was made for, behind the number of items in the workspace: a workspace that holds another plan, or none, is
+// not read any further.
+struct Made { int v[15]; };
+inline Made made_for(const PoolView& p, int n, int tokens, int n_q_heads) {
+  const uint64_t d = (uint64_t)(uintptr_t)p.data, t = (uint64_t)(uintptr_t)p.table;
+  return {{0x564c4150, n, tokens, n_q_heads, p.n_layers, p.n_kv_heads, p.head_dim, p.n_pages, p.max_seqs, p.max_pages, (int)d,
+           (int)(d >> 32), (int)t, (int)(t >> 32), kWaves}};
+}
+__device__ inline bool is_made_for(const int* head, const Made& m) {
+  int differ = 0;
+#pragma unroll
+  for (int i = 0; i < 15; ++i) differ |= ld_scalar(head + 1 + i) ^ m.v[i];
+  return differ == 0;
+}
+
 struct PlanArgs {
   PoolView p;
+  Made made;
   const int *seqs, *pos, *group;
   int add, n, tokens, n_q_heads, part_tiles, max_items;
-  int* head;  // [0] number of items
+  int* head;  // [0] number of items, then what it was made for
   Ent* ent;
   Own* own;
   Item* item;
@@ -333,7 +349,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     tiles += total.b;
   }
   items = min(items, a.max_items);
-  if (tid == 0) a.head[0] = items;
+  if (tid < 16) a.head[tid] = tid == 0 ? items : a.made.v[tid - 1];
   __syncthreads();
   for (int it = tid; it < items; it += NT) {
     int g = 0, hi = n_groups;  // the last group that begins at or before this item
@@ -370,6 +386,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
 
 struct AttendArgs {
   PoolView p;
+  Made made;
   const int* head;
   const Ent* ent;
   const Own* own;
@@ -420,6 +437,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
+  if (!is_made_for(a.head, a.made)) {
+    if (blockIdx.x == 0 && tid == 0) report(p, PAGES_BAD_ENTRY);
+    return;
+  }
   const int n_items = ld_scalar(a.head);
   const size_t tile = (size_t)kPage * HD, page = (size_t)p.n_layers * 2 * p.n_kv_heads * tile;
   for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
@@ -486,9 +507,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-    // Scores (minus infinity: not seen) -> the weights as the second product's operand, and the sums so far in their units.  Register 4*q4 + e of a lane is key 8*q4 + 4*g + e of the tile.  The reference point of a column's
-    // exponentials follows its maximum only when that has grown by more than 8 (weights stay below 256): then the rescaling of
-    // the sums is rare.  (The decision is the column's own: its result does not depend on its neighbours.)
+    // Scores (minus infinity: not seen) -> the weights as the second product's operand, and the sums so far in their units.
+    // Register 4*q4 + e of a lane is key 8*q4 + 4*g + e of the tile.  The reference point of a column's exponentials follows its
+    // maximum only when that has grown by more than 8 (weights stay below 256): then the rescaling of the sums is rare.  (The
+    // decision is the column's own: its result does not depend on its neighbours.)
     auto weigh = [&](f32x16& s, uint4(&pb)[2]) {
       float tmax = -INFINITY;
 #pragma unroll
@@ -694,6 +716,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const PoolView& p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
+  if (!is_made_for(a.head, a.made)) return;
   const int n_items = ld_scalar(a.head);
   for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
     const Item* im = a.item + it;
@@ -765,7 +788,7 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
                         const int* group, void* ws, hipStream_t st) {
   const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const PlanArgs a = {p, seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
+  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
                       (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
   // (one token of 2 candidates: 8.1 us with 4 waves, 9.8 with 16; 48 candidates with tables of 1027 pages: 40 and 20)
   if (n <= 128 && (long long)n * p.max_pages <= 4096)
@@ -778,7 +801,7 @@ void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, in
                    hipStream_t st) {
   const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const AttendArgs a = {p, (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
+  const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
                         (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
                         n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
   const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
@@ -818,7 +841,7 @@ int vlac_attend_shared(const vlac_pages* pages, int layer, int n, int tokens, in
   if (layer < 0 || layer >= pages->n_layers) return VLAC_E_RANGE;
   if (n == 0) return VLAC_OK;
   if (!q || !out) return VLAC_E_NULL;
-  if (q_stride < (int64_t)n_q_heads * pages->head_dim || q_stride % 8 || q_stride > 1 << 30 || (uintptr_t)q % 16 || (uintptr_t)out % 4)
+  if (q_stride < (int64_t)n_q_heads * pages->head_dim || q_stride % 8 || q_stride > 1 << 30 || (uintptr_t)q % 16 || (uintptr_t)out % 8)
     return VLAC_E_SHAPE;
   const AttendIo io = {(const bf16_t*)q, q_stride, (bf16_t*)out, 0};
   launch_attend(pool_view(pages), pages_f16(pages), layer, n, tokens, n_q_heads, io, workspace, (hipStream_t)stream);

@@ -349,3 +349,33 @@ def test_pages_beyond_32_bit_offsets():
     assert table[2].tolist() == [1, 2, 3, -1]
     got2 = run(p, c, [2], [89], q, None, layers - 1)
     assert bool((got2 == got).all())
+
+
+def test_a_workspace_without_its_plan_is_not_used():
+    import torch
+    c = Cache(2, 64, 1, seed=11, layers=2)
+    base = [c._new(PAGE) for _ in range(2)]
+    pos = [70, 75, 66]
+    seqs = [c.sequence(x + 2, base) for x in pos]
+    p, other = c.pool(), c.pool(seed=1)
+    q = queries(c, 3, 2, 4)
+    ws = torch.full((V.vlac_attend_workspace_bytes(p, 64, 2, 4),), 0xA5, dtype=torch.uint8, device=DEV)
+    out = torch.full((3, 2, 4, 64), 7.0, dtype=c.dt, device=DEV)
+
+    def attend(pool=p, n=3, tokens=2, hq=4):
+        rows = n * tokens * hq * 64
+        V.vlac_attend_shared(pool, 0, n, tokens, hq, q.view(-1)[:rows].view(n, tokens, hq, 64),
+                             out.view(-1)[:rows].view(n, tokens, hq, 64), ws)
+        return V.vlac_pages_check(pool, check=False)
+
+    assert attend() == E_RANGE                                  # never planned
+    V.vlac_attend_plan(p, i32(seqs), i32(pos), 3, 2, 4, None, ws)
+    assert attend(pool=other) == E_RANGE and attend(n=2) == E_RANGE and attend(tokens=1) == E_RANGE and attend(hq=2) == E_RANGE
+    assert bool((out == 7.0).all())
+    assert attend() == OK
+    want, tol = definition(c, seqs, pos, q)
+    assert bool(((out.double() - want).abs() <= tol).all())
+    V.vlac_attend_plan(other, i32(seqs), i32(pos), 3, 2, 4, None, ws)
+    out.fill_(7.0)
+    assert attend() == E_RANGE and bool((out == 7.0).all())
+    assert attend(pool=other) == OK and bool(((out.double() - want).abs() <= tol).all())

@@ -164,3 +164,43 @@ def test_refusals_and_reports():
         assert V.vlac_pages_check(tight, check=False) == E_NOMEM and tight.tensors[3].tolist() == [40, 40, 40, 40, 40, 0]
     finally:
         gm.close()
+
+
+def test_decoding_captured_in_a_graph():
+    """Fork and decode in one graph, replayed between eager decodes of the streams on the same context."""
+    import torch
+    cfg, L, n_new, n = synth.CONFIGS["tiny"], 60, 5, 6
+    gm = GpuModel(cfg, seed=5, max_batch=n, max_seq=96, std=0.05)
+    try:
+        rng = np.random.default_rng(1)
+        got = gm.prefill(synth.round_bf16(rng.standard_normal((2, L, cfg.d_model))), 48)
+        pool = V.new_pages(cfg.n_layers, cfg.n_kv_heads, cfg.head_dim, 1, 24, 2 + n, 3, DEV)
+        V.vlac_pages_import(gm.ctx, gm.kv, 2, L, pool, i32([0, 1]))
+        src, seqs, first = i32([0, 0, 0, 1, 1, 1]), i32(range(2, 2 + n)), i32([3, 9, 27, 81, 243, 11])
+        toks = torch.zeros((n, n_new), dtype=torch.int32, device=DEV)
+        logits = torch.zeros((n, n_new, cfg.vocab), device=DEV)
+        ws = torch.empty(V.vlac_candidates_workspace_bytes(gm.ctx, pool, n), dtype=torch.uint8, device=DEV)
+
+        def work():
+            V.vlac_pages_fork(pool, src, seqs, n)
+            V.vlac_decode_candidates(gm.ctx, pool, seqs, n, L, src, n_new, first, toks, logits, ws)
+
+        work()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            work()
+        for r in range(3):
+            first.copy_(torch.randint(0, cfg.vocab, (n,), device=DEV).int())
+            work()
+            torch.cuda.synchronize()
+            want = toks.clone(), logits.clone()
+            toks.fill_(-7)
+            logits.zero_()
+            gm.decode(2, L, n_new, got["token"])                # (the context's buffers hold other rows)
+            g.replay()
+            torch.cuda.synchronize()
+            assert bool((toks == want[0]).all()) and bool((logits == want[1]).all()), r
+        assert V.vlac_pages_check(pool, check=False) == OK
+    finally:
+        gm.close()
