@@ -4,7 +4,7 @@
 // read once for all its columns (candidates x tokens x query heads of the kv head), 32 of them to a matrix product, where
 // one pass per sequence reads them once for each; the pages behind them are each sequence's own.
 //
-// A column is a query (entry, token, head of the kv head's group); 32 columns are a column block, whose work is a list of key
+// A column is a query (entry, token, head of the kv head's group); up to 32 columns are a column block, whose work is a list of key
 // tiles: the shared pages, then the own pages of its entries, which only the entry's columns see.  S^T = K Q^T and O^T += V^T P^T
 // as in the attention over the stream cache: a page's tiles are the operands as they lie, a lane owns a column.
 // A workgroup of 8 waves takes an item: 1, 2 or 4 column blocks side by side (they share the pages) and the key tiles dealt
@@ -27,11 +27,11 @@ constexpr int kPartTiles = 2048;     // column blocks x parts that the workspace
 struct Ent { int seq, pos; };
 // A step over a page of an entry's own: page | valid positions of it << 24, tile | entry of the group << 16
 struct Own { uint32_t page, what; };
-// A work item: column blocks block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry e0, part `part` of
+// A work item: column blocks (of `width` columns) block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry e0, part `part` of
 // `parts` of their key tiles: pages s0 .. s1 - 1 of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
 // tile: where block0's parts lie.
 struct Item {
-  int e0, seq, head, block0, waves_c, part, parts, cols, s0, s1, tile, pad, own_at[4], own_n[4];
+  int e0, seq, head, block0, waves_c, part, parts, cols, s0, s1, tile, width, own_at[4], own_n[4];
 };
 static_assert(sizeof(Item) == 80, "read as five 16-byte words");
 
@@ -115,9 +115,9 @@ __device__ inline Two scan_before(Two x, Two* sums, Two* total) {
 
 // How a group is cut: column blocks, of which `waves_c` are side by side in an item
 struct Cut { int blocks, waves_c, chunks, wk; };
-__device__ inline Cut cut_of(int cols, int log_most) {
+__device__ inline Cut cut_of(int cols, int log_most, int width) {
   Cut x;
-  x.blocks = (cols + 31) >> 5;
+  x.blocks = (int)((unsigned)(cols + width - 1) / (unsigned)width);
   const int log = min(x.blocks >= 3 ? 2 : x.blocks >> 1, log_most);
   x.waves_c = 1 << log;
   x.chunks = (x.blocks + x.waves_c - 1) >> log;
@@ -255,7 +255,6 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       }
     }
   }
-  const int entry_blocks = (per_entry + 31) / 32;
   // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
   // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
   {
@@ -267,12 +266,28 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
   const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
+  // fewer own pages are in its list then (32 groups of up to 8 candidates, 6 columns each: 11.7 us with blocks of 32
+  // columns, 5 and a third entries, XXX with blocks of 12).
+  if (w == 0) {
+    int cols_best = 32;
+    if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
+      const int each = lane + 1;  // entries of a block that this lane tries
+      int blocks = 0;
+      for (int g = 0; g < n_groups; ++g) blocks += (g_start[g + 1] - g_start[g] + each - 1) / each;
+      const unsigned long long fits = __ballot(each * per_entry <= 32 && blocks * hkv <= kCus);
+      if (fits) cols_best = __ffsll((long long)fits) * per_entry;
+    }
+    if (lane == 0) s_width = cols_best;
+  }
+  __syncthreads();
+  const int block_cols = s_width, entry_blocks = (per_entry + block_cols - 1) / block_cols;
   // tiles of the list of a group's block
   {
     unsigned long long work = 0;
     int longest = 0;
     for (int g = tid; g < n_groups; g += NT) {
-      const Cut x = cut_of(group_cols(g), log_most);
+      const Cut x = cut_of(group_cols(g), log_most, block_cols);
       const int tiles = g_shared[g] + (int)ceilf((float)g_own[g] * (float)entry_blocks / (float)max(x.blocks, 1));
       g_own[g] = tiles;  // (from here on: of the whole list of a block)
       work += (unsigned long long)x.blocks * tiles * hkv;
@@ -295,7 +310,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   if (tid == 0 && s_bad == 2) report(p, PAGES_BAD_ENTRY);
   const int most = max(1, a.part_tiles / max(s_blocks, 1));  // parts that the workspace has room for
   auto parts_of = [&](int g, int steps) {
-    const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most).wk;
+    const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most, block_cols).wk;
     return max(1, min(min(most, kMaxParts), (int)((g_own[g] + per_item - 1) / per_item)));
   };
   if (w == 0) {
@@ -306,7 +321,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       int items = 0, most_steps = 0;  // (the steps that come of it: parts are bounded)
       bool joined = false;
       for (int g = 0; g < n_groups; ++g) {
-        const Cut x = cut_of(group_cols(g), log_most);
+        const Cut x = cut_of(group_cols(g), log_most, block_cols);
         const int parts = parts_of(g, steps);
         items += hkv * x.chunks * parts;
         most_steps = max(most_steps, (g_own[g] + parts * x.wk - 1) / (parts * x.wk));
@@ -335,7 +350,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     const int g = base + tid;
     Two mine = {0, 0};
     if (g < n_groups) {
-      const Cut x = cut_of(group_cols(g), log_most);
+      const Cut x = cut_of(group_cols(g), log_most, block_cols);
       const int parts = parts_of(g, steps);
       mine = {hkv * x.chunks * parts, parts > 1 ? hkv * x.blocks * parts : 0};
     }
@@ -359,23 +374,23 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       else hi = mid;
     }
     const int c = group_cols(g), parts = parts_of(g, steps);
-    const Cut x = cut_of(c, log_most);
+    const Cut x = cut_of(c, log_most, block_cols);
     // (heads fastest: workgroup id % 8, the XCD, is then the same for all chunks of a head where there are 8 heads or a
     // multiple of them, and its pages come into one L2 only)
     const int r = it - g_item[g], h = r % hkv, r1 = r / hkv, part = r1 % parts, chunk = r1 / parts;
     const int e0 = g_start[g], shared = g_shared[g], block0 = chunk * x.waves_c;
     Item* im = a.item + it;
     im->e0 = e0; im->seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im->head = h;
-    im->block0 = block0; im->waves_c = x.waves_c; im->part = part; im->parts = parts; im->cols = c;
+    im->block0 = block0; im->waves_c = x.waves_c; im->part = part; im->parts = parts; im->cols = c; im->width = block_cols;
     im->s0 = part * shared / parts; im->s1 = (part + 1) * shared / parts;
     im->tile = g_tile[g] + (h * x.blocks + block0) * parts;
 #pragma unroll 1
     for (int k = 0; k < x.waves_c; ++k) {
       // the own pages of the block's entries, one behind the other; of the last entry those that its tokens of
       // the block see; and the part's share of them
-      const int block = block0 + k, last_col = min(block * 32 + 31, c - 1);
+      const int block = block0 + k, last_col = min(block * block_cols + block_cols - 1, c - 1);
       if (block >= x.blocks) break;
-      const int lo = e0 + (block * 32) / per_entry, e = last_col / per_entry, hi = e0 + e;
+      const int lo = e0 + (block * block_cols) / per_entry, e = last_col / per_entry, hi = e0 + e;
       const int seen = l_seq[hi] < 0 ? 0 : (l_pos[hi] + (last_col - e * per_entry) / grp) / kPage + 1 - shared;
       const int all = l_own[hi] + seen - l_own[lo], o0 = part * all / parts;
       im->own_at[k] = l_own[lo] + o0;
@@ -451,15 +466,16 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     // this wave's block and its place among the block's waves (neighbours, on SIMDs of their own, read the same page)
     const int wc_log = wc >> 1, wk_log = 3 - wc_log, wk = 1 << wk_log, bw = w & (wc - 1), phase = w >> wc_log;  // (wc: 1, 2 or 4)
     const int block = ld_scalar(&im->block0) + bw;
-    const bool idle = block * 32 >= cols;
+    const int width = ld_scalar(&im->width), cols_end = min(block * width + width, cols);
+    const bool idle = block * width >= cols;
 
     // this lane's column
-    const int c = block * 32 + j, cc = min(c, cols - 1);
+    const int c = block * width + j, cc = min(c, cols_end - 1);
     const int ei = cc / per_entry, ci = cc - ei * per_entry, ti = ci / grp, row = (e0 + ei) * a.tokens + ti;
     const int h = hk * grp + ci - ti * grp;
     const Ent mine = a.ent[e0 + ei];
     const int last = mine.pos + ti;  // its last visible position
-    const bool valid = c < cols && mine.seq >= 0;
+    const bool valid = c < cols_end && mine.seq >= 0;
     uint4 qf[NC];
     {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)NC * 512 + (size_t)(((row & 31) + 32 * g) << 3)
@@ -693,7 +709,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
           for (int r = 0; r < R; r += 4)
             a.o[(at * (REGS / 4) + (r0 + r) / 4) * 64 + lane] = make_float4(x[r], x[r + 1], x[r + 2], x[r + 3]);
           if (r0 == 0) a.ml[at * 64 + lane] = make_float2(M, L);
-        } else if (c < cols) {
+        } else if (c < cols_end) {
           const float inv = 1.f / L;
 #pragma unroll
           for (int r = 0; r < R; r += 4)
@@ -722,10 +738,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     const Item* im = a.item + it;
     const int parts = ld_scalar(&im->parts), part = ld_scalar(&im->part), wc = ld_scalar(&im->waves_c), cols = ld_scalar(&im->cols);
     const int e0 = ld_scalar(&im->e0), hk = ld_scalar(&im->head), block0 = ld_scalar(&im->block0), tile0 = ld_scalar(&im->tile);
+    const int width = ld_scalar(&im->width);
     if (parts < 2) continue;
     for (int u = part + w * parts; u < wc * QUADS; u += 4 * parts) {
       const int bw = u / QUADS, quad = u - bw * QUADS, block = block0 + bw;
-      if (block * 32 >= cols) continue;
+      if (block * width >= cols) continue;
       const size_t at = (size_t)tile0 + bw * parts;
       float M = -INFINITY, L = 0.f;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -754,8 +771,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
           }
         }
       }
-      const int c = block * 32 + j;
-      if (c >= cols) continue;
+      const int c = block * width + j;
+      if (j >= width || c >= cols) continue;
       const int ei = c / per_entry, ci = c - ei * per_entry, ti = ci / grp;
       store_out<HD, F16>(a, (e0 + ei) * a.tokens + ti, hk * grp + ci - ti * grp, quad, g, x, 1.f / L, a.ent[e0 + ei].seq >= 0);
     }
