@@ -80,7 +80,7 @@ struct PlanArgs {
   Made made;
   const int *seqs, *pos, *group;
   int add, n, tokens, n_q_heads, part_tiles, max_items;
-  int* head;  // [0] number of items, then what it was made for
+  int* head;  // [0] number of items, [1] what it was made for, [16] and [24] an XCD's items, [32] how far apart they are
   Ent* ent;
   Own* own;
   Item* item;
@@ -131,9 +131,9 @@ __device__ inline Cut cut_of(int cols, int log_most, int width) {
 template <int NT, int N>
 __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __shared__ Two sums[NT / 64];
-  __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_own[N], g_item[N + 1], g_tile[N], l_seq[N], l_pos[N], l_own[N + 1];
+  __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_own[N], q_item[N + 1], g_tile[N], l_seq[N], l_pos[N], l_own[N + 1];
   __shared__ unsigned short l_group[N];
-  __shared__ int s_bad, s_width, s_steps, s_longest, s_blocks, s_own;
+  __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_own, s_cols;
   __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -182,8 +182,40 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) widest = max(widest, __shfl_xor(widest, d));
-  if (lane == 0) atomicMax(&s_width, widest);
+  auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
+  int blocks32 = 0;  // blocks of 32 columns
+  for (int g = tid; g < n_groups; g += NT) blocks32 += (group_cols(g) + 31) / 32 * hkv;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) blocks32 += __shfl_xor(blocks32, d);
+  if (lane == 0) {
+    atomicMax(&s_width, widest);
+    atomicAdd(&s_blocks, blocks32);
+  }
   __syncthreads();
+  // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
+  // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
+  const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
+  // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
+  // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each).
+  if (w == NT / 64 - 1) {
+    int each = 0;  // entries of a block (0: 32 columns, whatever they are)
+    if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
+      int lo = 1, hi = 32 / per_entry + 1;  // the least that fits, by halving (hi: none does)
+      while (lo < hi) {
+        const int k = (lo + hi) >> 1;
+        const float per = 1.f / (float)k;
+        int blocks = 0;
+        for (int g = lane; g < n_groups; g += 64) blocks += (int)(((float)(g_start[g + 1] - g_start[g] + k - 1) + 0.5f) * per);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
+        if (blocks * hkv <= kCus) hi = k;
+        else lo = k + 1;
+      }
+      each = lo * per_entry <= 32 ? lo : 0;
+    }
+    if (lane == 0) s_cols = each > 0 ? each * per_entry : 32;
+  }
   // The common pages: every entry's against its group's first.  A wave takes an entry's next 512 pages or, where tables
   // are short, as many entries as they leave lanes for; all of a turn's pages are asked for at once.
   const int width = s_width;
@@ -213,12 +245,10 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
 
-  // Work in steps of a wave: a key tile of a column block.  (An entry's own tiles are dealt to its blocks as if each
-  // had them all; a block of tokens before the last sees fewer.)
-  auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
   for (int g = tid; g < n_groups; g += NT)
     if (g_lead[g] == 0x7fffffff) g_shared[g] = 0;
   __syncthreads();
+  const int block_cols = s_cols, entry_blocks = (per_entry + block_cols - 1) / block_cols;
   // own pages of every entry, and where they begin in the list of all of them
   int owned = 0;
   for (int base = 0; base < a.n; base += NT) {
@@ -229,10 +259,13 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       a.ent[i] = {seq, pos};
       if (seq >= 0) {
         own = pages_of(pos + a.tokens) - g_shared[g];
-        atomicAdd(&g_own[g], own);
-        atomicMax(&s_own, own);
+        if (a.part_tiles > 0) atomicAdd(&g_own[g], own);
       }
     }
+    int longest = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) longest = max(longest, __shfl_xor(longest, d));
+    if (lane == 0) atomicMax(&s_own, longest);
     Two total;
     const Two before = scan_before<NT>({own, 0}, sums, &total);
     if (i < a.n) l_own[i] = owned + before.a;
@@ -248,42 +281,16 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
         int pg = p.table[(size_t)l_seq[i] * p.max_pages + shared + t];
         if ((unsigned)pg >= (unsigned)p.n_pages) {  // (the table is the caller's)
           pg = 0;
-          s_bad = 2;
+          report(p, PAGES_BAD_ENTRY);
         }
         const int valid = min(l_pos[i] + a.tokens - kPage * (shared + t), kPage);
         a.own[l_own[i] + t] = {(uint32_t)pg | (uint32_t)valid << 24, (uint32_t)(shared + t) | (uint32_t)(i - g_start[l_group[i]]) << 16};
       }
     }
   }
-  // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
-  // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
-  {
-    int blocks = 0;
-    for (int g = tid; g < n_groups; g += NT) blocks += (group_cols(g) + 31) / 32 * hkv;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
-    if (lane == 0) atomicAdd(&s_blocks, blocks);
-  }
-  __syncthreads();
-  const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
-  // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
-  // fewer own pages are in its list then (32 groups of up to 8 candidates, 6 columns each: 11.7 us with blocks of 32
-  // columns, 5 and a third entries, XXX with blocks of 12).
-  if (w == 0) {
-    int cols_best = 32;
-    if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
-      const int each = lane + 1;  // entries of a block that this lane tries
-      int blocks = 0;
-      for (int g = 0; g < n_groups; ++g) blocks += (g_start[g + 1] - g_start[g] + each - 1) / each;
-      const unsigned long long fits = __ballot(each * per_entry <= 32 && blocks * hkv <= kCus);
-      if (fits) cols_best = __ffsll((long long)fits) * per_entry;
-    }
-    if (lane == 0) s_width = cols_best;
-  }
-  __syncthreads();
-  const int block_cols = s_width, entry_blocks = (per_entry + block_cols - 1) / block_cols;
-  // tiles of the list of a group's block
-  {
+  // Work in steps of a wave, a key tile of a column block: tiles of the list of a group's block.  (An entry's own tiles are dealt
+  // to its blocks as if each had them all; a block of tokens before the last sees fewer.)
+  if (a.part_tiles > 0) {
     unsigned long long work = 0;
     int longest = 0;
     for (int g = tid; g < n_groups; g += NT) {
@@ -302,22 +309,20 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       atomicAdd(&s_work, work);
       atomicMax(&s_longest, longest);
     }
+    __syncthreads();
   }
-  __syncthreads();
   // Steps of a wave per item: the lanes of the first wave try the longest list in 1, 2, ... 64 parts, and take what
   // ends first: rounds of one item per CU x (steps + 3 for an item's start and end), + 3 for parts that have to be joined.
   // With many groups the chip is full anyhow, and the work per wave is the measure.
-  if (tid == 0 && s_bad == 2) report(p, PAGES_BAD_ENTRY);
   const int most = max(1, a.part_tiles / max(s_blocks, 1));  // parts that the workspace has room for
   auto parts_of = [&](int g, int steps) {
+    if (most == 1) return 1;
     const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most, block_cols).wk;
     return max(1, min(min(most, kMaxParts), (int)((g_own[g] + per_item - 1) / per_item)));
   };
-  if (w == 0) {
+  if (most > 1 && w == 0) {
     int steps = max((s_longest + lane) / (lane + 1), 1), best;
-    if (most == 1) {
-      steps = s_longest;
-    } else if (n_groups <= 64) {
+    if (n_groups <= 64) {
       int items = 0, most_steps = 0;  // (the steps that come of it: parts are bounded)
       bool joined = false;
       for (int g = 0; g < n_groups; ++g) {
@@ -341,45 +346,71 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
     if (lane == 0) s_steps = steps;
   }
-  __syncthreads();
+  if (most > 1) __syncthreads();
   const int steps = s_steps;
 
-  // first item and first partial tile of every group
+  // First item (per kv head) and first partial tile of every group.  Workgroup id % 8 is the XCD, and items that read the same
+  // pages belong into one L2.  With 8 kv heads or a multiple of them it is enough that the heads are the fastest index.  With 1, 2
+  // or 4 of them the groups are taken residue by residue (mod 8 / heads), and every XCD has a run of items of its own, if
+  // the longest run takes no more rounds than the items dealt one by one.
+  const int m = hkv < 8 && 8 % hkv == 0 ? 8 / hkv : 1, whole = n_groups / m, rest = n_groups - whole * m;
+  auto group_at = [&](int q, int* residue) {  // the q-th group in that order
+    const bool longer = q < rest * (whole + 1);
+    const int r = longer ? q / (whole + 1) : rest + (q - rest * (whole + 1)) / max(whole, 1);
+    *residue = r;
+    return (q - r * whole - min(r, rest)) * m + r;
+  };
   int items = 0, tiles = 0;
   for (int base = 0; base < n_groups; base += NT) {
-    const int g = base + tid;
+    const int q = base + tid;
+    int g = 0, residue = 0;
     Two mine = {0, 0};
-    if (g < n_groups) {
+    if (q < n_groups) {
+      g = group_at(q, &residue);
       const Cut x = cut_of(group_cols(g), log_most, block_cols);
       const int parts = parts_of(g, steps);
-      mine = {hkv * x.chunks * parts, parts > 1 ? hkv * x.blocks * parts : 0};
+      mine = {x.chunks * parts, parts > 1 ? hkv * x.blocks * parts : 0};
     }
     Two total;
     const Two before = scan_before<NT>(mine, sums, &total);
-    if (g < n_groups) {
-      g_item[g] = items + before.a;
+    if (q < n_groups) {
+      q_item[q] = items + before.a;
       g_tile[g] = tiles + before.b;
+      if (g < m) s_run[residue] = items + before.a;  // (the first group of a residue)
     }
     items += total.a;
     tiles += total.b;
   }
+  if (tid == 0)
+    for (int r = min(m, n_groups); r <= m; ++r) s_run[r] = items;
+  __syncthreads();
+  int longest_run = 0;
+  for (int r = 0; r < m; ++r) longest_run = max(longest_run, s_run[r + 1] - s_run[r]);
+  const bool runs = m > 1 && (longest_run + kCus / 8 - 1) / (kCus / 8) <= (items * hkv + kCus - 1) / kCus && 2 * longest_run * m <= 3 * items;
+  items *= hkv;
   items = min(items, a.max_items);
   if (tid < 16) a.head[tid] = tid == 0 ? items : a.made.v[tid - 1];
-  __syncthreads();
+  if (tid < 8) {  // an XCD's items: from .. to, and how far apart they are
+    const int r = tid / hkv, len = runs ? s_run[r + 1] - s_run[r] : 0;
+    const int from = runs ? hkv * s_run[r] + (tid - r * hkv) * len : tid;
+    a.head[16 + tid] = from;
+    a.head[24 + tid] = runs ? from + len : items;
+    if (tid == 0) a.head[32] = runs ? 1 : 8;
+  }
   for (int it = tid; it < items; it += NT) {
-    int g = 0, hi = n_groups;  // the last group that begins at or before this item
-    while (hi - g > 1) {
-      const int mid = (g + hi) >> 1;
-      if (g_item[mid] <= it) g = mid;
+    const int u = it / hkv, h = it - u * hkv;
+    int q = 0, hi = n_groups;  // the last group that begins at or before this item
+    while (hi - q > 1) {
+      const int mid = (q + hi) >> 1;
+      if (q_item[mid] <= u) q = mid;
       else hi = mid;
     }
-    const int c = group_cols(g), parts = parts_of(g, steps);
+    int residue;
+    const int g = group_at(q, &residue), c = group_cols(g), parts = parts_of(g, steps);
     const Cut x = cut_of(c, log_most, block_cols);
-    // (heads fastest: workgroup id % 8, the XCD, is then the same for all chunks of a head where there are 8 heads or a
-    // multiple of them, and its pages come into one L2 only)
-    const int r = it - g_item[g], h = r % hkv, r1 = r / hkv, part = r1 % parts, chunk = r1 / parts;
+    const int r1 = u - q_item[q], part = r1 % parts, chunk = r1 / parts, run = s_run[residue];
+    Item* im = a.item + (runs ? hkv * run + h * (s_run[residue + 1] - run) + u - run : it);
     const int e0 = g_start[g], shared = g_shared[g], block0 = chunk * x.waves_c;
-    Item* im = a.item + it;
     im->e0 = e0; im->seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im->head = h;
     im->block0 = block0; im->waves_c = x.waves_c; im->part = part; im->parts = parts; im->cols = c; im->width = block_cols;
     im->s0 = part * shared / parts; im->s1 = (part + 1) * shared / parts;
@@ -458,7 +489,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   }
   const int n_items = ld_scalar(a.head);
   const size_t tile = (size_t)kPage * HD, page = (size_t)p.n_layers * 2 * p.n_kv_heads * tile;
-  for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+  const int xcd = blockIdx.x & 7, apart = ld_scalar(a.head + 32), end = min(ld_scalar(a.head + 24 + xcd), n_items);
+  for (int it = ld_scalar(a.head + 16 + xcd) + (int)(blockIdx.x >> 3) * apart; it < end; it += (int)(gridDim.x >> 3) * apart) {
     const Item* im = a.item + it;
     const int e0 = ld_scalar(&im->e0), lead = ld_scalar(&im->seq), hk = ld_scalar(&im->head), wc = ld_scalar(&im->waves_c);
     const int part = ld_scalar(&im->part), parts = ld_scalar(&im->parts), cols = ld_scalar(&im->cols);
@@ -573,7 +605,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
         l = 0.f;
       }
       // 64 steps at a time, and no branch around a load inside (the compiler would wait for all loads behind it): the last step
-      // asks for its own K again
+      // asks for a few words that are never used.  (Its own keys again instead: what a CU fetches is what bounds a list of few steps.)
       for (int first = 0; first < n_steps; first += 64) {
         load_steps(first);
         const bf16_t* now = tile_of(0);
@@ -593,7 +625,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 #pragma unroll
           for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
           __builtin_amdgcn_sched_barrier(0);
-          now = tile_of(min(i + 1, n64 - 1));
+          now = i + 1 < n64 ? tile_of(min(i + 1, n64 - 1)) : p.data;
           load_k(now);
           __builtin_amdgcn_sched_barrier(0);
           if (own) {
@@ -807,7 +839,8 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
   char* b = (char*)ws;
   const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
                       (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
-  // (one token of 2 candidates: 8.1 us with 4 waves, 9.8 with 16; 48 candidates with tables of 1027 pages: 40 and 20)
+  // (4 waves and 128 entries: one token of 2 candidates 8.1 us with 4 waves, 9.8 with 16; 48 candidates with tables of 1027 pages:
+  // 40 and 20; 32 groups of up to 8 candidates over short tables: 15.4 and 15.1)
   if (n <= 128 && (long long)n * p.max_pages <= 4096)
     hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(1), dim3(256), 0, st, a);
   else
@@ -821,7 +854,7 @@ void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, in
   const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
                         (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
                         n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
-  const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
+  const dim3 grid((unsigned)std::min<size_t>((l.max_items + 7) / 8 * 8, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
 #define VLAC_ATTEND(HD_, F16_)                                                                        \
   {                                                                                                   \
     hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);                \
