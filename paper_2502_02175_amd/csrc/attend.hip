@@ -90,25 +90,18 @@ struct PlanArgs {
 struct Two { int a, b; };
 template <int NT>
 __device__ inline Two scan_before(Two x, Two* sums, Two* total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  Two run = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int ya = __shfl_up(run.a, d), yb = __shfl_up(run.b, d);
-    if (lane >= d) { run.a += ya; run.b += yb; }
-  }
+  static_assert(NT <= 1024, "the waves' sums are a row of lanes");
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Two run = {wave_sums(x.a), wave_sums(x.b)};
   if (lane == 63) sums[w] = run;
   __syncthreads();
-  // (every wave adds the sums of all 16 for itself: no second meeting)
-  const Two mine = lane < NT / 64 ? sums[lane] : Two{0, 0};
-  Two s = mine;
-#pragma unroll
-  for (int d = 1; d < NT / 64; d <<= 1) {
-    const int ya = __shfl_up(s.a, d), yb = __shfl_up(s.b, d);
-    if (lane >= d) { s.a += ya; s.b += yb; }
-  }
-  *total = {__builtin_amdgcn_readlane(s.a, NT / 64 - 1), __builtin_amdgcn_readlane(s.b, NT / 64 - 1)};
-  const Two before = {__shfl(s.a - mine.a, w) + run.a - x.a, __shfl(s.b - mine.b, w) + run.b - x.b};
+  // (every wave adds the sums of all of them for itself: no second meeting)
+  const Two mine = (lane & 15) < NT / 64 ? sums[lane & 15] : Two{0, 0};
+  const Two s = {row_sums(mine.a), row_sums(mine.b)};
+  *total = {__builtin_amdgcn_readlane(s.a, 15), __builtin_amdgcn_readlane(s.b, 15)};
+  const int last = max(w - 1, 0);
+  const Two before = {(w > 0 ? __builtin_amdgcn_readlane(s.a, last) : 0) + run.a - x.a,
+                      (w > 0 ? __builtin_amdgcn_readlane(s.b, last) : 0) + run.b - x.b};
   __syncthreads();
   return before;
 }
@@ -180,14 +173,12 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       atomicMin(&g_shared[l_group[i]], l_pos[i] / kPage);
       widest = max(widest, l_pos[i] / kPage);
     }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) widest = max(widest, __shfl_xor(widest, d));
+  widest = wave_max(widest);
   auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
   int blocks32 = 0;  // blocks of 32 columns
   for (int g = tid; g < n_groups; g += NT) blocks32 += (group_cols(g) + 31) / 32 * hkv;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) blocks32 += __shfl_xor(blocks32, d);
-  if (lane == 0) {
+  blocks32 = wave_sums(blocks32);
+  if (lane == 63) {
     atomicMax(&s_width, widest);
     atomicAdd(&s_blocks, blocks32);
   }
@@ -207,8 +198,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
         const float per = 1.f / (float)k;
         int blocks = 0;
         for (int g = lane; g < n_groups; g += 64) blocks += (int)(((float)(g_start[g + 1] - g_start[g] + k - 1) + 0.5f) * per);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
+        blocks = __builtin_amdgcn_readlane(wave_sums(blocks), 63);
         if (blocks * hkv <= kCus) hi = k;
         else lo = k + 1;
       }
@@ -262,9 +252,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
         if (a.part_tiles > 0) atomicAdd(&g_own[g], own);
       }
     }
-    int longest = own;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) longest = max(longest, __shfl_xor(longest, d));
+    const int longest = wave_max(own);
     if (lane == 0) atomicMax(&s_own, longest);
     Two total;
     const Two before = scan_before<NT>({own, 0}, sums, &total);
@@ -301,10 +289,8 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       longest = max(longest, (tiles + x.wk - 1) / x.wk);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      work += __shfl_xor(work, d);
-      longest = max(longest, __shfl_xor(longest, d));
-    }
+    for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+    longest = wave_max(longest);
     if (lane == 0) {
       atomicAdd(&s_work, work);
       atomicMax(&s_longest, longest);
@@ -355,6 +341,8 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   // the longest run takes no more rounds than the items dealt one by one.
   const int m = hkv < 8 && 8 % hkv == 0 ? 8 / hkv : 1, whole = n_groups / m, rest = n_groups - whole * m;
   auto group_at = [&](int q, int* residue) {  // the q-th group in that order
+    *residue = 0;
+    if (m == 1) return q;
     const bool longer = q < rest * (whole + 1);
     const int r = longer ? q / (whole + 1) : rest + (q - rest * (whole + 1)) / max(whole, 1);
     *residue = r;
@@ -408,7 +396,12 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     int residue;
     const int g = group_at(q, &residue), c = group_cols(g), parts = parts_of(g, steps);
     const Cut x = cut_of(c, log_most, block_cols);
-    const int r1 = u - q_item[q], part = r1 % parts, chunk = r1 / parts, run = s_run[residue];
+    const int r1 = u - q_item[q], run = s_run[residue];
+    int part = 0, chunk = r1;
+    if (most > 1) {
+      chunk = r1 / parts;
+      part = r1 - chunk * parts;
+    }
     Item* im = a.item + (runs ? hkv * run + h * (s_run[residue + 1] - run) + u - run : it);
     const int e0 = g_start[g], shared = g_shared[g], block0 = chunk * x.waves_c;
     im->e0 = e0; im->seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im->head = h;

@@ -47,6 +47,32 @@ __device__ inline int checked_len(const PoolView& p, int s) {
   return l < 0 || l > p.max_pages * kPage ? -1 : l;
 }
 __device__ inline void report(const PoolView& p, int bit) { atomicOr(p.scratch + PG_STATUS, bit); }
+
+// Sums over the lanes up to this one, and a maximum over all, by moves between lanes inside the vector ALU (shifts within rows
+// of 16 lanes, then the last lane of a row into the next, and of the first half into the second): 6 dependent instructions where
+// shuffles through LDS take 6 round trips, and the planning kernels, which are chains of such sums, 1 to 3 us less.
+template <int HOW, int ROWS>
+__device__ inline int lanes_moved(int x) { return __builtin_amdgcn_update_dpp(0, x, HOW, ROWS, 0xf, false); }
+__device__ inline int row_sums(int x) {  // (of 16 lanes)
+  x += lanes_moved<0x111, 0xf>(x);
+  x += lanes_moved<0x112, 0xf>(x);
+  x += lanes_moved<0x114, 0xf>(x);
+  return x + lanes_moved<0x118, 0xf>(x);
+}
+__device__ inline int wave_sums(int x) {
+  x = row_sums(x);
+  x += lanes_moved<0x142, 0xa>(x);
+  return x + lanes_moved<0x143, 0xc>(x);
+}
+__device__ inline int wave_max(int x) {  // (x >= 0)
+  x = max(x, lanes_moved<0x111, 0xf>(x));
+  x = max(x, lanes_moved<0x112, 0xf>(x));
+  x = max(x, lanes_moved<0x114, 0xf>(x));
+  x = max(x, lanes_moved<0x118, 0xf>(x));
+  x = max(x, lanes_moved<0x142, 0xa>(x));
+  x = max(x, lanes_moved<0x143, 0xc>(x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 #endif
 
 // pages.hip

@@ -22,33 +22,17 @@ __device__ inline void meet() {
   __syncthreads();
 }
 
-// Sum over the workgroup's threads before this one; *total: over all of them.  sums: [kPlan / 64 + 1] words of LDS
+// Sum over the workgroup's threads before this one; *total: over all of them.  sums: [kPlan / 64] words of LDS
 __device__ inline int scan_before(int x, int* sums, int* total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int run = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(run, d);
-    if (lane >= d) run += y;
-  }
+  static_assert(kPlan / 64 == 16, "the waves' sums are a row of lanes");
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, run = wave_sums(x);
   if (lane == 63) sums[w] = run;
   __syncthreads();
-  if (threadIdx.x < 64) {
-    int s = lane < kPlan / 64 ? sums[lane] : 0;
-    const int mine = s;
-#pragma unroll
-    for (int d = 1; d < kPlan / 64; d <<= 1) {
-      const int y = __shfl_up(s, d);
-      if (lane >= d) s += y;
-    }
-    if (lane < kPlan / 64) sums[lane] = s - mine;
-    if (lane == kPlan / 64 - 1) sums[kPlan / 64] = s;
-  }
-  __syncthreads();
-  const int before = sums[w] + run - x;
-  *total = sums[kPlan / 64];
-  __syncthreads();
-  return before;
+  const int s = row_sums(sums[lane & 15]);  // (every wave adds them for itself: no second meeting)
+  *total = __builtin_amdgcn_readlane(s, 15);
+  const int before = w > 0 ? __builtin_amdgcn_readlane(s, __builtin_amdgcn_readfirstlane(max(w - 1, 0))) : 0;
+  __syncthreads();  // (sums are written again)
+  return before + run - x;
 }
 
 // The free pages of lowest index, ascending, to out[0 .. most): -> how many there are (at most `most` are looked for)
@@ -94,7 +78,7 @@ struct Entries { int dst[kMost], src[kMost], held[kMost], pages[kMost], len[kMos
 // released, the fresh pages looked for, and if they do not suffice the release is taken back.
 template <int MODE>
 __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
-  __shared__ int sums[kPlan / 64 + 1];
+  __shared__ int sums[kPlan / 64];
   __shared__ Entries es;
   __shared__ int s_flags;  // 1: an entry is ignored, 2: pages are released
   const PoolView& p = a.p;
@@ -305,7 +289,7 @@ __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* 
 // One workgroup: counts the pages in use, then pairs those at or beyond the count with the free ones below it.  A thread
 // takes 8 pages side by side, all of them asked for at once.
 __global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* out_live) {
-  __shared__ int sums[kPlan / 64 + 1];
+  __shared__ int sums[kPlan / 64];
   constexpr int PER = 8, ROUND = PER * kPlan;
   read_args(p.refs, p.scratch, p.n_pages, out_live);
   const int tid = threadIdx.x;
