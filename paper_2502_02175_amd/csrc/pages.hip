@@ -88,20 +88,31 @@ __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
   int* const fresh_pages = p.copy_dst();
   if (tid == 0) s_flags = 0;
 
-  // Only the first entry of a sequence counts, and none whose sequence is a source.  Short lists are compared in LDS, long ones
-  // by marks in the scratch (a round trip more, but no square of the length).
+  // Only the first entry of a sequence counts, and none whose sequence is a source.  Short lists are compared in LDS, 32 lanes
+  // per entry, long ones by marks in the scratch (a round trip more, but no square of the length).
   const bool marks = a.n > 256;
   for (int i = tid; i < a.n; i += kPlan) {
     const int d = a.dst[i], s = MODE == FORK ? a.src[i] : 0;
     es.dst[i] = d;
     es.src[i] = s;
+    es.first[i] = 0;  // (until then: 1 if the entry does not count)
     if (marks) {
       if ((unsigned)d < (unsigned)p.max_seqs) atomicMax(p.is_dst() + d, a.n - i);
       if (MODE == FORK && (unsigned)s < (unsigned)p.max_seqs) atomicOr(p.is_src() + s, 1);
     }
   }
-  if (marks) meet();
-  else __syncthreads();
+  if (marks) {
+    meet();
+  } else {
+    __syncthreads();
+    for (int i = tid >> 5; i < a.n; i += kPlan / 32) {
+      const int d = es.dst[i];
+      bool out = false;
+      for (int k = lane & 31; k < a.n; k += 32) out |= (k < i && es.dst[k] == d) || (MODE == FORK && es.src[k] == d);
+      if (out) es.first[i] = 1;
+    }
+    __syncthreads();
+  }
   int need = 0;
   for (int base = 0; base < a.n; base += kPlan) {
     const int i = base + tid;
@@ -114,7 +125,7 @@ __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
       if (marks) {
         ok = ok && ld_agent(p.is_dst() + d) == a.n - i && (MODE != FORK || ld_agent(p.is_src() + d) == 0);
       } else {
-        for (int k = 0; k < a.n; ++k) ok = ok && !(k < i && es.dst[k] == d) && !(MODE == FORK && es.src[k] == d);
+        ok = ok && es.first[i] == 0;
       }
       if (MODE == EXTEND)
         ok = ok && (long long)ld + a.tokens <= (long long)p.max_pages * kPage && (a.want_len < 0 || ld == a.want_len);
@@ -129,12 +140,11 @@ __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
       d = ok ? d : -1;
     }
     int total;
-    const int before = scan_before(fresh, sums, &total);  // (everybody is through with es.dst of others here)
+    const int before = scan_before(fresh, sums, &total);
     if (i < a.n) {
       es.first[i] = need + before;
-      if (!marks) es.dst[i] = d;
+      es.dst[i] = d;
     }
-    if (marks && i < a.n) es.dst[i] = d;
     need += total;
   }
   __syncthreads();
