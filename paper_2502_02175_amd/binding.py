@@ -383,7 +383,7 @@ def pages(n_layers, n_kv_heads, head_dim, operand_dtype, data, refs, table, leng
     p.index = refs.get_device()
     p.torch = torch
     p.i32 = torch.int32
-    p.raw_stream = torch._C._cuda_getCurrentRawStream
+    p.raw_stream, p.current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     p.rows_dtype = torch.bfloat16 if operand_dtype == OPERAND_BF16 else torch.float16
     p.data = _at(p, data, None, 0, "data")
     p.refs, p.table = _at(p, refs, torch.int32, 0, "refs"), _at(p, table, torch.int32, 0, "table")
@@ -448,7 +448,7 @@ def _call(p, name, stream, check, *args):
     if index < 0:                      # (no pool, or one of bare addresses: the current device's)
         return _ret(fn(*args, _stream(stream)), name, check)
     raw = p.raw_stream(index) if stream is None else _stream(stream)
-    if p.torch.cuda.current_device() == index:
+    if p.current() == index:
         status = fn(*args, raw)
     else:
         with p.torch.cuda.device(index):
