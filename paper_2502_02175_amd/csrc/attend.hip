@@ -11,6 +11,17 @@
 // to the waves of a block, which meet in LDS.  Where that leaves the chip empty the list is cut into parts, one item each,
 // which leave (max, sum, output) in fp32, and a second kernel joins them in the order of the parts:
 //   M = max m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i   (scores in units of log2).
+//
+// What bounds it, and what it takes (32 query and kv heads of 128, fp16, if not said otherwise):
+// * long lists: memory.  48 candidates over 32801 shared positions (554 MB of K and V) 105 to 110 us, 5.2 TB/s, and 5.5 us to join.
+// * many columns: what a CU moves into registers, 64 bytes per clock.  Every wave reads the K and V of a tile (16 KiB) for
+//   its 32 columns: 16 candidates x 56 tokens over 1057 positions (16 GFLOP) 35 us, that path busy 73 % of the time, the matrix
+//   cores 27 %.  (Pages staged in LDS for all blocks of an item: 35 us as against 32 then, the meetings of the waves cost what the
+//   reads save; two column blocks per wave in 4 waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two
+//   per wave in 8 waves, queries in LDS: 46, the registers that would let LDS reads run ahead are not there.)
+// * short lists: the chain launch arguments - item - tables - pages, 2.6 us to the first product, then 1.4 us for every tile of
+//   a wave (2 or 3 of them), 1.5 us to meet and store: 12 query heads on 2 kv heads, 32 groups of up to 8 candidates over 304
+//   positions, bf16, 13 MB: 10 us; two candidates over 80 positions, 4 heads of 64: 6 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,8 +38,8 @@ constexpr int kPartTiles = 2048;     // column blocks x parts that the workspace
 struct Ent { int seq, pos; };
 // A step over a page of an entry's own: page | valid positions of it << 24, tile | entry of the group << 16
 struct Own { uint32_t page, what; };
-// A work item: column blocks (of `width` columns) block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry e0, part `part` of
-// `parts` of their key tiles: pages s0 .. s1 - 1 of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
+// A work item: column blocks (of `width` columns) block0 .. block0 + waves_c - 1 of head `head` of the group that begins at entry
+// e0, part `part` of `parts` of their key tiles: pages s0 .. s1 - 1 of sequence seq, and own_n[i] steps from own_at[i] on for block0 + i.
 // tile: where block0's parts lie.
 struct Item {
   int e0, seq, head, block0, waves_c, part, parts, cols, s0, s1, tile, width, own_at[4], own_n[4];
@@ -119,7 +130,8 @@ __device__ inline Cut cut_of(int cols, int log_most, int width) {
 }
 
 // One workgroup.  Groups and their common pages, then the cut, then the items.  Memory is asked for in three rounds
-// (lists, lengths, tables), all else is in LDS.
+// (lists, lengths, tables), all else is in LDS.  Bound by latency: two candidates 7.3 us, 32 groups of up to 8 candidates 9.2, 48
+// entries of 1027 pages 20 to 23 (9 of them the comparison of the tables).
 // (NT threads and room for N entries: a workgroup of 4 waves meets sooner than one of 16)
 template <int NT, int N>
 __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
@@ -188,7 +200,8 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
-  // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each).
+  // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
+  // XCD's runs, below).
   if (w == NT / 64 - 1) {
     int each = 0;  // entries of a block (0: 32 columns, whatever they are)
     if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
@@ -549,6 +562,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
       for (int i = 0; i < 16; ++i) o[ib][i] = 0.f;
     float m = -INFINITY, l = 0.f;
     // Scores (minus infinity: not seen) -> the weights as the second product's operand, and the sums so far in their units.
+    // (The weights are rounded to the type of the cache, half a step each: it is what the matrix core takes at its full rate, and
+    // V has no more bits.  Their sum is that of the weights in fp32.)
     // Register 4*q4 + e of a lane is key 8*q4 + 4*g + e of the tile.  The reference point of a column's exponentials follows its
     // maximum only when that has grown by more than 8 (weights stay below 256): then the rescaling of the sums is rare.  (The
     // decision is the column's own: its result does not depend on its neighbours.)
@@ -832,8 +847,8 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
   char* b = (char*)ws;
   const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
                       (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
-  // (4 waves and 128 entries: one token of 2 candidates 8.1 us with 4 waves, 9.8 with 16; 48 candidates with tables of 1027 pages:
-  // 40 and 20; 32 groups of up to 8 candidates over short tables: 15.4 and 15.1)
+  // (4 waves or 16: one token of 2 candidates 7.3 and 8.2 us, 16 candidates x 56 tokens over 1057 positions 8.0 and 8.6; 48
+  // candidates with tables of 1027 pages 40 and 20 when both were tried.  More entries than 128 are a second round for 4 waves.)
   if (n <= 128 && (long long)n * p.max_pages <= 4096)
     hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(1), dim3(256), 0, st, a);
   else

@@ -75,7 +75,9 @@ constexpr int kMost = VLAC_PAGES_MAX_LIST;
 struct Entries { int dst[kMost], src[kMost], held[kMost], pages[kMost], len[kMost], first[kMost + 1]; };
 
 // One workgroup, which looks every entry up once and keeps it in LDS.  Everything or nothing: the destinations' pages are
-// released, the fresh pages looked for, and if they do not suffice the release is taken back.
+// released, the fresh pages looked for, and if they do not suffice the release is taken back.  A chain of reads (list, lengths,
+// tables of what is released, refs, tables of the sources), about 1 us each: fork of 16 entries 5.5 to 6.8 us, extend 2.8 (4
+// entries) to 4.8 (16).
 template <int MODE>
 __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
   __shared__ int sums[kPlan / 64];
@@ -250,7 +252,8 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PoolView p, long long p
   }
 }
 
-// Tiles of the streams' cache into fresh pages: work item = (page, layer, K or V, kv head)
+// Tiles of the streams' cache into fresh pages: work item = (page, layer, K or V, kv head); a tile of 4 or 8 KiB is the
+// longest piece that lies together on both sides.  Bound by memory: 34 pages of 4 MiB (285 MB read and written) in 48 us.
 __global__ __launch_bounds__(256) void pages_import_kernel(PoolView p, const uint4* cache, long long stream16, int max_seq) {
   const int n = ld_scalar(p.scratch + PG_COPIES);
   const int tile16 = (int)(p.tile() / 8), heads = p.n_layers * 2 * p.n_kv_heads;
@@ -273,7 +276,8 @@ __global__ __launch_bounds__(256) void pages_reset_kernel(PoolView p, int scratc
   for (long long i = at; i < scratch_words; i += step) p.scratch[i] = 0;
 }
 
-// One workgroup per entry; whoever takes the length of a sequence first releases its pages
+// One workgroup per entry; whoever takes the length of a sequence first releases its pages.  (2.5 us: the exchange of the
+// length, the row, the counts, one behind the other.)
 __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* __restrict__ seqs) {
   __shared__ int s_len;
   const int s = seqs[blockIdx.x];
@@ -297,7 +301,7 @@ __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* 
 }
 
 // One workgroup: counts the pages in use, then pairs those at or beyond the count with the free ones below it.  A thread
-// takes 8 pages side by side, all of them asked for at once.
+// takes 8 pages side by side, all of them asked for at once (301 pages 4.6 us, 5003 pages 5.5).
 __global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* out_live) {
   __shared__ int sums[kPlan / 64];
   constexpr int PER = 8, ROUND = PER * kPlan;
@@ -354,7 +358,9 @@ __global__ __launch_bounds__(kPlan) void pages_compact_kernel(PoolView p, int* o
 
 // K and V of new tokens.  A wave takes 64 features of a head at 8 positions that lie side by side in a page (so that what is
 // asked of the tables is one page, by scalar loads, and a K store of 8 lanes is a line): 16 bytes of a row per lane for
-// K, and for V, whose 4 neighbouring positions lie side by side, turned round in LDS, a feature per lane.
+// K, and for V, whose 4 neighbouring positions lie side by side, turned round in LDS, a feature per lane.  Bound by the latency
+// of the table (list and position, then length, table and count of the page, then the stores): 8 tokens of 32 heads of 128 in 3.3 us,
+// 32 entries x 56 tokens of 2 heads (3.7 MB) in 3.7.
 // TILES: the rows come from tiles (one token per entry), else from rows.
 struct AppendArgs {
   PoolView p;
