@@ -429,6 +429,8 @@ def _rows(p, x, count, width, name):
     """Address and row stride of `count` rows of `width` dense values, equally far apart, of the pool's type."""
     if x is None or isinstance(x, int):
         return x, width
+    if x.is_contiguous() and x.numel() == count * width and x.dtype is p.rows_dtype and x.get_device() == p.index >= 0:
+        return x.data_ptr(), width
     if x.numel() != count * width:
         raise ValueError("%s holds %d values, expected %d rows of %d" % (name, x.numel(), count, width))
     if x.is_contiguous():
@@ -444,16 +446,15 @@ def _rows(p, x, count, width, name):
 
 def _call(p, name, stream, check, *args):
     """One library call on the pool's device."""
-    fn, index = getattr(_LIB or lib(), name), getattr(p, "index", -1)
-    if index < 0:                      # (no pool, or one of bare addresses: the current device's)
+    index = getattr(p, "index", -1)
+    if index >= 0 and stream is None and p.current() == index:
+        status = getattr(_LIB or lib(), name)(*args, p.raw_stream(index))
+        return status if status == VLAC_OK else _ret(status, name, check)
+    fn = getattr(lib(), name)
+    if index < 0 or p.current() == index:   # (no pool, or one of bare addresses: the current device's)
         return _ret(fn(*args, _stream(stream)), name, check)
-    raw = p.raw_stream(index) if stream is None else _stream(stream)
-    if p.current() == index:
-        status = fn(*args, raw)
-    else:
-        with p.torch.cuda.device(index):
-            status = fn(*args, raw)
-    return status if status == VLAC_OK else _ret(status, name, check)
+    with p.torch.cuda.device(index):
+        return _ret(fn(*args, p.raw_stream(index) if stream is None else _stream(stream)), name, check)
 
 
 def _ref(p):
