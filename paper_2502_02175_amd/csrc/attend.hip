@@ -44,7 +44,19 @@ struct Own { uint32_t page, what; };
 struct Item {
   int e0, seq, head, block0, waves_c, part, parts, cols, s0, s1, tile, width, own_at[4], own_n[4];
 };
-static_assert(sizeof(Item) == 80, "read as five 16-byte words");
+static_assert(sizeof(Item) == 80, "read as twenty words");
+__device__ inline Item load_item(const Item* at) {
+  Item x;
+  x.e0 = ld_scalar(&at->e0); x.seq = ld_scalar(&at->seq); x.head = ld_scalar(&at->head); x.block0 = ld_scalar(&at->block0);
+  x.waves_c = ld_scalar(&at->waves_c); x.part = ld_scalar(&at->part); x.parts = ld_scalar(&at->parts); x.cols = ld_scalar(&at->cols);
+  x.s0 = ld_scalar(&at->s0); x.s1 = ld_scalar(&at->s1); x.tile = ld_scalar(&at->tile); x.width = ld_scalar(&at->width);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    x.own_at[k] = ld_scalar(at->own_at + k);
+    x.own_n[k] = ld_scalar(at->own_n + k);
+  }
+  return x;
+}
 
 struct Layout {
   size_t ent, own, item, ml, o, total;
@@ -61,6 +73,8 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   l.parts = least < 2 * kCus && p.max_pages > 24;
   l.part_tiles = l.parts ? (int)std::min<size_t>(kPartTiles, max_blocks * kMaxParts) : 0;
   l.max_items = max_blocks + l.part_tiles;
+  if (p.n_kv_heads < 8) l.max_items += l.max_items / 2;  // (runs of an XCD may leave places empty)
+  l.max_items = (l.max_items + 7) / 8 * 8;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   l.ent = 256;
   l.own = l.ent + up(sizeof(Ent) * n);
@@ -79,11 +93,11 @@ inline Made made_for(const PoolView& p, int n, int tokens, int n_q_heads) {
   return {{0x564c4150, n, tokens, n_q_heads, p.n_layers, p.n_kv_heads, p.head_dim, p.n_pages, p.max_seqs, p.max_pages, (int)d,
            (int)(d >> 32), (int)t, (int)(t >> 32), kWaves}};
 }
-__device__ inline bool is_made_for(const int* head, const Made& m) {
-  int differ = 0;
+__device__ inline int differs(const int* head, const Made& m) {
+  int x = 0;
 #pragma unroll
-  for (int i = 0; i < 15; ++i) differ |= ld_scalar(head + 1 + i) ^ m.v[i];
-  return differ == 0;
+  for (int i = 0; i < 15; ++i) x |= ld_scalar(head + 1 + i) ^ m.v[i];
+  return x;
 }
 
 struct PlanArgs {
@@ -91,7 +105,7 @@ struct PlanArgs {
   Made made;
   const int *seqs, *pos, *group;
   int add, n, tokens, n_q_heads, part_tiles, max_items;
-  int* head;  // [0] number of items, [1] what it was made for, [16] and [24] an XCD's items, [32] how far apart they are
+  int* head;  // [0] places for items, [1] what it was made for
   Ent* ent;
   Own* own;
   Item* item;
@@ -389,15 +403,18 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   for (int r = 0; r < m; ++r) longest_run = max(longest_run, s_run[r + 1] - s_run[r]);
   const bool runs = m > 1 && (longest_run + kCus / 8 - 1) / (kCus / 8) <= (items * hkv + kCus - 1) / kCus && 2 * longest_run * m <= 3 * items;
   items *= hkv;
+  // Workgroup i takes the items at i, i + grid, ..., so a place is its XCD + 8 x its number there.
+  const int places = min(runs ? 8 * longest_run : items, a.max_items);
   items = min(items, a.max_items);
-  if (tid < 16) a.head[tid] = tid == 0 ? items : a.made.v[tid - 1];
-  if (tid < 8) {  // an XCD's items: from .. to, and how far apart they are
-    const int r = tid / hkv, len = runs ? s_run[r + 1] - s_run[r] : 0;
-    const int from = runs ? hkv * s_run[r] + (tid - r * hkv) * len : tid;
-    a.head[16 + tid] = from;
-    a.head[24 + tid] = runs ? from + len : items;
-    if (tid == 0) a.head[32] = runs ? 1 : 8;
-  }
+  if (tid < 16) a.head[tid] = tid == 0 ? places : a.made.v[tid - 1];
+  if (runs)
+    for (int it = tid; it < places; it += NT) {
+      const int r = (it & 7) / hkv;
+      if (it >> 3 >= s_run[r + 1] - s_run[r]) {  // (nobody's)
+        a.item[it].cols = 0;
+        a.item[it].parts = 1;
+      }
+    }
   for (int it = tid; it < items; it += NT) {
     const int u = it / hkv, h = it - u * hkv;
     int q = 0, hi = n_groups;  // the last group that begins at or before this item
@@ -415,7 +432,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       chunk = r1 / parts;
       part = r1 - chunk * parts;
     }
-    Item* im = a.item + (runs ? hkv * run + h * (s_run[residue + 1] - run) + u - run : it);
+    Item* im = a.item + (runs ? residue * hkv + h + 8 * (u - run) : it);
     const int e0 = g_start[g], shared = g_shared[g], block0 = chunk * x.waves_c;
     im->e0 = e0; im->seq = g_lead[g] == 0x7fffffff ? 0 : l_seq[g_lead[g]]; im->head = h;
     im->block0 = block0; im->waves_c = x.waves_c; im->part = part; im->parts = parts; im->cols = c; im->width = block_cols;
@@ -489,22 +506,25 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
-  if (!is_made_for(a.head, a.made)) {
+  // (asked for together with what says whether there is such an item)
+  Item im = load_item(a.item + blockIdx.x);
+  const int n_items = ld_scalar(a.head), differ = differs(a.head, a.made);
+  read_args(n_items, differ, im.e0, im.seq, im.head, im.block0, im.waves_c, im.part, im.parts, im.cols, im.s0, im.s1, im.tile,
+            im.width, im.own_at[0], im.own_at[1], im.own_at[2], im.own_at[3], im.own_n[0], im.own_n[1], im.own_n[2], im.own_n[3]);
+  if (differ) {
     if (blockIdx.x == 0 && tid == 0) report(p, PAGES_BAD_ENTRY);
     return;
   }
-  const int n_items = ld_scalar(a.head);
   const size_t tile = (size_t)kPage * HD, page = (size_t)p.n_layers * 2 * p.n_kv_heads * tile;
-  const int xcd = blockIdx.x & 7, apart = ld_scalar(a.head + 32), end = min(ld_scalar(a.head + 24 + xcd), n_items);
-  for (int it = ld_scalar(a.head + 16 + xcd) + (int)(blockIdx.x >> 3) * apart; it < end; it += (int)(gridDim.x >> 3) * apart) {
-    const Item* im = a.item + it;
-    const int e0 = ld_scalar(&im->e0), lead = ld_scalar(&im->seq), hk = ld_scalar(&im->head), wc = ld_scalar(&im->waves_c);
-    const int part = ld_scalar(&im->part), parts = ld_scalar(&im->parts), cols = ld_scalar(&im->cols);
-    const int tile0 = ld_scalar(&im->tile);
+  for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+    if (it != (int)blockIdx.x) im = load_item(a.item + it);
+    const int e0 = im.e0, lead = im.seq, hk = im.head, wc = im.waves_c, part = im.part, parts = im.parts, cols = im.cols;
+    const int tile0 = im.tile;
+    if (cols == 0) continue;
     // this wave's block and its place among the block's waves (neighbours, on SIMDs of their own, read the same page)
     const int wc_log = wc >> 1, wk_log = 3 - wc_log, wk = 1 << wk_log, bw = w & (wc - 1), phase = w >> wc_log;  // (wc: 1, 2 or 4)
-    const int block = ld_scalar(&im->block0) + bw;
-    const int width = ld_scalar(&im->width), cols_end = min(block * width + width, cols);
+    const int block = im.block0 + bw;
+    const int width = im.width, cols_end = min(block * width + width, cols);
     const bool idle = block * width >= cols;
 
     // this lane's column
@@ -525,8 +545,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 
     // The steps of this wave: every wk-th of the part's shared pages, then of its own pages (which go on where the shared ones
     // stopped, so that the waves' numbers of steps differ by one at most).  A lane holds one step.
-    const int own_at = ld_scalar(im->own_at + bw), own_n = idle ? 0 : ld_scalar(im->own_n + bw);
-    const int s0 = ld_scalar(&im->s0), s1 = ld_scalar(&im->s1);
+    auto of_block = [&](int x0, int x1, int x2, int x3) { return bw < 2 ? (bw == 0 ? x0 : x1) : (bw == 2 ? x2 : x3); };
+    const int own_at = of_block(im.own_at[0], im.own_at[1], im.own_at[2], im.own_at[3]);
+    const int own_n = idle ? 0 : of_block(im.own_n[0], im.own_n[1], im.own_n[2], im.own_n[3]);
+    const int s0 = im.s0, s1 = im.s1;
     const int sh0 = s0 + phase, ow0 = (phase - (s1 - s0)) & (wk - 1);
     const int n_shared = idle || sh0 >= s1 ? 0 : (s1 - sh0 + wk - 1) >> wk_log;
     const int n_steps = n_shared + (ow0 >= own_n ? 0 : (own_n - ow0 + wk - 1) >> wk_log);
@@ -772,7 +794,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const PoolView& p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
   const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
-  if (!is_made_for(a.head, a.made)) return;
+  if (differs(a.head, a.made)) return;
   const int n_items = ld_scalar(a.head);
   for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
     const Item* im = a.item + it;
@@ -862,7 +884,7 @@ void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, in
   const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
                         (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
                         n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
-  const dim3 grid((unsigned)std::min<size_t>((l.max_items + 7) / 8 * 8, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
+  const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
 #define VLAC_ATTEND(HD_, F16_)                                                                        \
   {                                                                                                   \
     hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);                \
