@@ -622,6 +622,12 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
       }
     };
 
+    // Two blocks side by side read the same pages, each page by two waves: those keep step (by a barrier that orders no memory, once
+    // per shared step that every wave has), so that the second finds the page in this CU's L1.  48 candidates over 32801 positions
+    // 118 -> 112 us, 2 x 40 over 9000 83 -> 79, short lists as before.  With heads of 64 the pages of all waves fit into the L1 anyway
+    // (6 groups of 1 to 3 x 6 tokens over 18532 positions, 4 heads: 26.4 without, 28.0 with), and with four blocks the waves
+    // lose by it (grouped queries, 24 x 17009 positions: 32.9 and 37.0).
+    const int together = HD == 128 && wc == 2 && (im.block0 + 1) * width < cols ? (s1 - s0) >> wk_log : 0;
     bool odd = false;
     // Once as a rule.  Where a column comes out infinite or NaN once more, from the beginning and with care: V of a position may
     // hold that, columns that do not see the position have weight 0 there, and 0 x NaN is not 0.
@@ -642,6 +648,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
         load_k(now);
         const int n64 = min(n_steps - first, 64);
         for (int i = 0; i < n64; ++i) {
+          if (!care && first + i < together) __builtin_amdgcn_s_barrier();
           const bool own = first + i >= n_shared;
           const int what = __builtin_amdgcn_readlane(st_what, i), kt = what & 0xffff;
           const int held = __builtin_amdgcn_readlane(st_page, i) >> 24;  // positions of an own page that hold a token
