@@ -13,12 +13,13 @@
 //   M = max m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i   (scores in units of log2).
 //
 // What bounds it, and what it takes (32 query and kv heads of 128, fp16, if not said otherwise):
-// * long lists: memory.  48 candidates over 32801 shared positions (554 MB of K and V) 105 to 110 us, 5.2 TB/s, and 5.5 us to join.
+// * long lists: memory.  48 candidates over 32801 shared positions (554 MB of K and V) 99 to 102 us, 5.5 TB/s, and 5.5 us to join.
 // * many columns: what a CU moves into registers, 64 bytes per clock.  Every wave reads the K and V of a tile (16 KiB) for
-//   its 32 columns: 16 candidates x 56 tokens over 1057 positions (16 GFLOP) 35 us, that path busy 73 % of the time, the matrix
-//   cores 27 %.  (Pages staged in LDS for all blocks of an item: 35 us as against 32 then, the meetings of the waves cost what the
-//   reads save; two column blocks per wave in 4 waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two
-//   per wave in 8 waves, queries in LDS: 46, the registers that would let LDS reads run ahead are not there.)
+//   its 32 columns: 16 candidates x 56 tokens over 1057 positions (16 GFLOP) 34 to 35 us, that path busy 73 % of the time, the
+//   matrix cores 27 %, the softmax's instructions 37 %; two waves per SIMD overlap them in part.  (Pages staged in LDS for all
+//   blocks of an item: 35 us as against 32 then, the meetings of the waves cost what the reads save; two column blocks per wave in 4
+//   waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two per wave in 8 waves, queries in LDS: 36 to
+//   46, no registers are left for K and V to be asked for ahead.)
 // * short lists: the chain launch arguments - item - tables - pages, 2.6 us to the first product, then 1.4 us for every tile of
 //   a wave (2 or 3 of them), 1.5 us to meet and store: 12 query heads on 2 kv heads, 32 groups of up to 8 candidates over 304
 //   positions, bf16, 13 MB: 10 us; two candidates over 80 positions, 4 heads of 64: 6 us.
