@@ -64,14 +64,17 @@ struct Layout {
   size_t max_items;
   int part_tiles;
   bool parts;  // there may be parts to join
+  bool few;    // blocks of up to 16 columns
 };
 inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   Layout l;
   const size_t cols = (size_t)n * tokens * (n_q_heads / p.n_kv_heads);  // per kv head
-  const size_t least = (cols + 31) / 32 * p.n_kv_heads, max_blocks = least + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
+  const size_t least = (cols + 31) / 32 * p.n_kv_heads;
   // Parts where the column blocks do not fill the chip by themselves and the tables have room for lists that are long
   // for 8 waves (that decides whether the second kernel is launched: 2.5 us where it finds nothing to join)
   l.parts = least < 2 * kCus && p.max_pages > 24;
+  l.few = !l.parts && cols <= (size_t)16 * n && (cols + 15) / 16 * p.n_kv_heads <= kCus;
+  const size_t max_blocks = (l.few ? (cols + 15) / 16 * p.n_kv_heads : least) + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
   l.part_tiles = l.parts ? (int)std::min<size_t>(kPartTiles, max_blocks * kMaxParts) : 0;
   l.max_items = max_blocks + l.part_tiles;
   if (p.n_kv_heads < 8) l.max_items += l.max_items / 2;  // (runs of an XCD may leave places empty)
@@ -105,7 +108,7 @@ struct PlanArgs {
   PoolView p;
   Made made;
   const int *seqs, *pos, *group;
-  int add, n, tokens, n_q_heads, part_tiles, max_items;
+  int add, n, tokens, n_q_heads, part_tiles, max_items, width;
   int* head;  // [0] places for items, [1] what it was made for
   Ent* ent;
   Own* own;
@@ -202,25 +205,25 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
   widest = wave_max(widest);
   auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
-  int blocks32 = 0;  // blocks of 32 columns
-  for (int g = tid; g < n_groups; g += NT) blocks32 += (group_cols(g) + 31) / 32 * hkv;
-  blocks32 = wave_sums(blocks32);
+  int all_blocks = 0;  // (of full width)
+  for (int g = tid; g < n_groups; g += NT) all_blocks += (group_cols(g) + a.width - 1) / a.width * hkv;
+  all_blocks = wave_sums(all_blocks);
   if (lane == 63) {
     atomicMax(&s_width, widest);
-    atomicAdd(&s_blocks, blocks32);
+    atomicAdd(&s_blocks, all_blocks);
   }
   __syncthreads();
   // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
   // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
-  const int log_most = a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  const int log_most = a.width < 32 ? 0 : a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
   // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
   // XCD's runs, below).
   if (w == NT / 64 - 1) {
-    int each = 0;  // entries of a block (0: 32 columns, whatever they are)
+    int each = 0;  // entries of a block (0: full width, whatever they are)
     if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
-      int lo = 1, hi = 32 / per_entry + 1;  // the least that fits, by halving (hi: none does)
+      int lo = 1, hi = a.width / per_entry + 1;  // the least that fits, by halving (hi: none does)
       while (lo < hi) {
         const int k = (lo + hi) >> 1;
         const float per = 1.f / (float)k;
@@ -230,9 +233,9 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
         if (blocks * hkv <= kCus) hi = k;
         else lo = k + 1;
       }
-      each = lo * per_entry <= 32 ? lo : 0;
+      each = lo * per_entry <= a.width ? lo : 0;
     }
-    if (lane == 0) s_cols = each > 0 ? each * per_entry : 32;
+    if (lane == 0) s_cols = each > 0 ? each * per_entry : a.width;
   }
   // The common pages: every entry's against its group's first.  A wave takes an entry's next 512 pages or, where tables
   // are short, as many entries as they leave lanes for; all of a turn's pages are asked for at once.
@@ -489,13 +492,16 @@ __device__ inline uint32_t far_values(uint32_t x, bool lo, bool hi) {
   return (lo && (x & kExp) == kExp ? 0xffffu : 0u) | (hi && (x >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
 }
 
-// The result of a column: features 4 * quad' .. + 3 of 32 * ib + 8 * q4 + 4 * g from its sums 4 * quad .. + 3 (quad = 4 ib + q4)
+// The result of a column: features f .. f + 3 of its row
 template <int HD, bool F16>
-__device__ inline void store_out(const AttendArgs& a, int row, int h, int quad, int g, const float4& x, float inv, bool valid) {
-  const int f = h * HD + 32 * (quad >> 2) + 8 * (quad & 3) + 4 * g;
+__device__ inline void store_out(const AttendArgs& a, int row, int f, const float4& x, float inv, bool valid) {
   const uint2 y = valid ? make_uint2(pack2<F16>(x.x * inv, x.y * inv), pack2<F16>(x.z * inv, x.w * inv)) : make_uint2(0, 0);
   *(uint2*)(a.kc_out > 0 ? a.out + frag_off(row, f, a.kc_out) : a.out + (size_t)row * a.n_q_heads * HD + f) = y;
 }
+
+// the first feature of sums 4 * quad .. + 3 of head h: 32 * ib + 8 * q4 + 4 * g, quad = 4 ib + q4
+template <int HD>
+__device__ inline int feature_of(int h, int quad, int g) { return h * HD + 32 * (quad >> 2) + 8 * (quad & 3) + 4 * g; }
 
 template <int HD, bool F16>
 __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
@@ -783,7 +789,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
           const float inv = 1.f / L;
 #pragma unroll
           for (int r = 0; r < R; r += 4)
-            store_out<HD, F16>(a, row, h, (r0 + r) / 4, g, make_float4(x[r], x[r + 1], x[r + 2], x[r + 3]), inv, valid);
+            store_out<HD, F16>(a, row, feature_of<HD>(h, (r0 + r) / 4, g), make_float4(x[r], x[r + 1], x[r + 2], x[r + 3]), inv, valid);
         }
       }
       __syncthreads();  // (the next item parks here)
@@ -791,6 +797,253 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     if (wc == 1) meet(std::integral_constant<int, REGS / 8>{});
     else if (wc == 2) meet(std::integral_constant<int, REGS / 4>{});
     else meet(std::integral_constant<int, REGS / 2>{});
+  }
+}
+
+// The same for short lists of blocks of up to 16 columns, no parts: products of 16 x 16 x 32, half the registers per column
+// block, and so two tiles at a time per wave.  A row of K is the key that the second product wants there: the row m = 4 * q + e of
+// product rb is key 16 * (q >> 1) + 8 * rb + 4 * (q & 1) + e, so that the 8 scores of a lane are, in order, the 8 weights that it owes
+// as the second operand, for the 16 bytes of V that lie together in the page.
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
+  constexpr int NB = HD / 32, NF = HD / 16, U = 2;
+  __shared__ float park[kWaves][2 + 4 * NF][64];
+  const PoolView& p = a.p;
+  read_args(a.head, a.item, a.ent, a.q, a.q_stride, a.out, a.kc_out, a.layer, a.tokens, a.n_q_heads, a.scale_log2e, p.data, p.table,
+            p.n_pages, p.max_pages, p.n_layers, p.n_kv_heads, a.own);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = lane & 15, q4 = lane >> 4;
+  const int grp = a.n_q_heads / p.n_kv_heads, per_entry = a.tokens * grp;
+  // (asked for together with what says whether there is such an item)
+  Item im = load_item(a.item + blockIdx.x);
+  const int n_items = ld_scalar(a.head), differ = differs(a.head, a.made);
+  read_args(n_items, differ, im.e0, im.seq, im.head, im.block0, im.cols, im.s0, im.s1, im.width, im.own_at[0], im.own_n[0]);
+  if (differ) {
+    if (blockIdx.x == 0 && tid == 0) report(p, PAGES_BAD_ENTRY);
+    return;
+  }
+  const size_t tile = (size_t)kPage * HD, page = (size_t)p.n_layers * 2 * p.n_kv_heads * tile;
+  const int half = (q4 >> 1) * 512 + (q4 & 1) * 256;  // where 8 features, or 8 positions, of a lane lie
+  for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+    if (it != (int)blockIdx.x) im = load_item(a.item + it);
+    const int e0 = im.e0, lead = im.seq, hk = im.head, cols = im.cols, width = im.width;
+    if (cols == 0) continue;
+    const int c0 = im.block0 * width, cols_end = min(c0 + width, cols);
+
+    // this lane's column
+    const int c = c0 + j, cc = min(c, cols_end - 1);
+    const int ei = cc / per_entry, ci = cc - ei * per_entry, ti = ci / grp, row = (e0 + ei) * a.tokens + ti;
+    const int h = hk * grp + ci - ti * grp;
+    const Ent mine = a.ent[e0 + ei];
+    const int last = mine.pos + ti;  // its last visible position
+    const bool valid = c < cols_end && mine.seq >= 0;
+    uint4 qf[NB];
+    {
+      const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)(HD / 16) * 512 + (size_t)((row & 31) << 3) + half
+                                       : a.q + (size_t)row * a.q_stride + (size_t)h * HD + 8 * q4;
+      const int q_step = a.q_stride < 0 ? 1024 : 32;
+#pragma unroll
+      for (int x = 0; x < NB; ++x) qf[x] = *(const uint4*)(q + (size_t)x * q_step);
+    }
+
+    // The steps of this wave: every eighth of the shared pages, then of the block's own.  A lane holds one step.
+    const int own_at = im.own_at[0], own_n = im.own_n[0], s0 = im.s0, s1 = im.s1;
+    const int sh0 = s0 + w, ow0 = (w - (s1 - s0)) & (kWaves - 1);
+    const int n_shared = sh0 >= s1 ? 0 : (s1 - sh0 + kWaves - 1) / kWaves;
+    const int n_steps = n_shared + (ow0 >= own_n ? 0 : (own_n - ow0 + kWaves - 1) / kWaves);
+    int st_page = 0, st_what = 0;  // page | valid positions << 24, tile | entry << 16 (an own page's)
+    auto load_steps = [&](int first) {
+      const int i = first + lane;
+      st_what = 0;
+      if (i < n_shared) {
+        st_page = p.table[(size_t)lead * p.max_pages + sh0 + i * kWaves];
+        if ((unsigned)st_page >= (unsigned)p.n_pages) {  // (the table is the caller's)
+          st_page = 0;
+          report(p, PAGES_BAD_ENTRY);
+        }
+      } else if (i < n_steps) {
+        const Own x = a.own[own_at + ow0 + (i - n_shared) * kWaves];
+        st_page = (int)x.page;
+        st_what = (int)x.what;
+      }
+    };
+
+    const bf16_t* kv = p.data + ((size_t)a.layer * 2 * p.n_kv_heads + hk) * tile + half;
+    const size_t v_off = (size_t)p.n_kv_heads * tile + 8 * j;
+    const int k_off = 8 * (16 * (j >> 3) + (j & 7));
+    auto tile_of = [&](int i) { return kv + (size_t)(__builtin_amdgcn_readlane(st_page, i) & 0xffffff) * page; };
+    f32x4v o[NF];
+    float m, l;
+    auto clear = [&] {
+      m = -INFINITY;
+      l = 0.f;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) o[f] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    };
+    clear();
+    auto load_k = [&](uint4(&kf)[2 * NB], const bf16_t* t) {
+#pragma unroll
+      for (int x = 0; x < 2 * NB; ++x) kf[x] = *(const uint4*)(t + k_off + (x >> 1) * 1024 + (x & 1) * 64);
+    };
+    auto v_at = [&](const bf16_t* t, int f) { return t + v_off + (f >> 1) * 1024 + (f & 1) * 128; };
+    auto scores = [&](const uint4(&kf)[2 * NB], float(&s)[8]) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        f32x4v y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NB; ++x) y = mfma16<F16>(kf[2 * x + rb], qf[x], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * rb + e] = y[e];
+      }
+    };
+    // score 4 * rb + e is key first_key + 8 * rb + e of the tile
+    const int first_key = 16 * (q4 >> 1) + 4 * (q4 & 1);
+    auto weights = [&](const float(&s)[8]) {
+      return make_uint4(pack2<F16>(s[0], s[1]), pack2<F16>(s[2], s[3]), pack2<F16>(s[4], s[5]), pack2<F16>(s[6], s[7]));
+    };
+    bool odd = false;
+    for (int care = 0; care < 2; ++care) {  // (as above: twice only where a column comes out infinite or NaN)
+      if (care) clear();
+      for (int first = 0; first < n_steps; first += 64) {
+        load_steps(first);
+        const int n64 = min(n_steps - first, 64);
+        for (int i = 0; i < n64; i += U) {
+          uint4 kf[U][2 * NB], vf[U][NF];
+#pragma unroll
+          for (int u = 0; u < U; ++u) load_k(kf[u], i + u < n64 ? tile_of(min(i + u, n64 - 1)) : kv);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const bf16_t* t = i + u < n64 ? tile_of(min(i + u, n64 - 1)) : kv;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) vf[u][f] = *(const uint4*)v_at(t, f);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (i + u >= n64) break;
+            const bool own = first + i + u >= n_shared;
+            const int what = __builtin_amdgcn_readlane(st_what, min(i + u, 63)), kt = what & 0xffff;
+            const int held = __builtin_amdgcn_readlane(st_page, min(i + u, 63)) >> 24;  // positions of an own page that hold a token
+            float s[8];
+            scores(kf[u], s);
+            if (own) {
+              const int see = ei == what >> 16 ? last - 32 * kt - first_key : -1;
+#pragma unroll
+              for (int x = 0; x < 8; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+            }
+            // (the reference point as above)
+            float tmax = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
+            tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * a.scale_log2e;
+            float alpha = 1.f;
+            if (tmax > m + 8.f) {
+              alpha = __builtin_amdgcn_exp2f(m - tmax);
+              m = tmax;
+            }
+            const float m_use = m == -INFINITY ? 0.f : m;
+            float psum = 0.f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -m_use));
+              psum += s[x];
+            }
+            l = fmaf(l, alpha, psum);
+            const uint4 pb = weights(s);
+            if (__any(alpha != 1.f)) {
+#pragma unroll
+              for (int f = 0; f < NF; ++f) o[f] *= alpha;
+            }
+            if (own && (care || held < kPage)) {
+              // V of positions that hold no token may be anything
+#pragma unroll
+              for (int f = 0; f < NF; ++f) {
+                uint32_t* x = (uint32_t*)&vf[u][f];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                  const int kp = first_key + 8 * (d >> 1) + 2 * (d & 1);
+                  const uint32_t far = far_values<F16>(x[d], care, care);
+                  const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
+                  odd |= (far & seen) != 0;
+                  x[d] &= seen & ~far;
+                }
+              }
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f) o[f] = mfma16<F16>(vf[u][f], pb, o[f]);
+          }
+        }
+      }
+      if (care) break;
+      float worst = 0.f;  // (0 x infinity and 0 x NaN are NaN, and stay it)
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) worst = fmaf(o[f][e], 0.f, worst);
+      if (!__any(worst != 0.f)) break;
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (__builtin_expect(__any(odd), 0)) {
+      // key by key, added where it is seen
+      for (int i = n_shared; i < n_steps; ++i) {
+        const int at64 = (i - n_shared) & 63;
+        if (at64 == 0) load_steps(i);
+        const int what = __builtin_amdgcn_readlane(st_what, at64), kt = what & 0xffff, held = __builtin_amdgcn_readlane(st_page, at64) >> 24;
+        const int see = ei == what >> 16 ? last - 32 * kt : -1;  // this column's last key of the tile
+        const bf16_t* at = tile_of(at64);
+        uint4 kf[2 * NB];
+        load_k(kf, at);
+        float s[8];
+        scores(kf, s);
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          s[x] = first_key + 8 * (x >> 2) + (x & 3) <= see ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
+        const uint4 pb = weights(s);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const uint4 v = *(const uint4*)v_at(at, f);
+          const uint32_t* x = (const uint32_t*)&v;
+          for (int k = 0; k < held; ++k) {
+            const bool here = q4 == 2 * (k >> 4) + (k >> 2 & 1);
+            uint4 only;
+            uint32_t* y = (uint32_t*)&only;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+              y[d] = here && d == 2 * (k >> 3 & 1) + (k >> 1 & 1) ? x[d] & far_values<F16>(x[d], !(k & 1), k & 1) : 0u;
+            const f32x4v z = mfma16<F16>(only, pb, f32x4v{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[f][e] += k <= see ? z[e] : 0.f;
+          }
+        }
+      }
+    }
+
+    // The waves meet in LDS; four sums of a lane each, in the order of the waves.
+    park[w][0][lane] = m;
+    park[w][1][lane] = l;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) park[w][2 + 4 * f + e][lane] = o[f][e];
+    __syncthreads();
+    if (w < NF && c < cols_end) {
+      float M = -INFINITY, L = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) M = fmaxf(M, park[y][0][lane]);
+      const float m_use = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) {
+        const float f = __builtin_amdgcn_exp2f(park[y][0][lane] - m_use);
+        L = fmaf(f, park[y][1][lane], L);
+        x.x = fmaf(f, park[y][2 + 4 * w][lane], x.x);
+        x.y = fmaf(f, park[y][3 + 4 * w][lane], x.y);
+        x.z = fmaf(f, park[y][4 + 4 * w][lane], x.z);
+        x.w = fmaf(f, park[y][5 + 4 * w][lane], x.w);
+      }
+      store_out<HD, F16>(a, row, h * HD + 16 * w + 4 * q4, x, 1.f / L, valid);
+    }
+    __syncthreads();  // (the next item parks here)
   }
 }
 
@@ -844,7 +1097,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
       const int c = block * width + j;
       if (j >= width || c >= cols) continue;
       const int ei = c / per_entry, ci = c - ei * per_entry, ti = ci / grp;
-      store_out<HD, F16>(a, (e0 + ei) * a.tokens + ti, hk * grp + ci - ti * grp, quad, g, x, 1.f / L, a.ent[e0 + ei].seq >= 0);
+      store_out<HD, F16>(a, (e0 + ei) * a.tokens + ti, feature_of<HD>(hk * grp + ci - ti * grp, quad, g), x, 1.f / L, a.ent[e0 + ei].seq >= 0);
     }
   }
 }
@@ -875,7 +1128,7 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
                         const int* group, void* ws, hipStream_t st) {
   const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items,
+  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items, l.few ? 16 : 32,
                       (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
   // (4 waves or 16: one token of 2 candidates 7.3 and 8.2 us, 16 candidates x 56 tokens over 1057 positions 8.0 and 8.6; 48
   // candidates with tables of 1027 pages 40 and 20 when both were tried.  More entries than 128 are a second round for 4 waves.)
@@ -895,7 +1148,8 @@ void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, in
   const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
 #define VLAC_ATTEND(HD_, F16_)                                                                        \
   {                                                                                                   \
-    hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);                \
+    if (l.few) hipLaunchKernelGGL((attend_few_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a); \
+    else hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);           \
     if (l.parts) hipLaunchKernelGGL((attend_join_kernel<HD_, F16_>), join, dim3(256), 0, st, a);      \
   }
   if (p.head_dim == 128) {

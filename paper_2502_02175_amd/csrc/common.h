@@ -30,6 +30,7 @@ static inline int round_up(int x, int m) { return (x + m - 1) / m * m; }
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
 
 // fp32 -> bf16, round to nearest even, by the chip's own conversion of two values (the same bits as the
 // integer arithmetic it replaces for all 2^32 inputs, NaN and subnormals among them, in a seventh of
@@ -119,6 +120,14 @@ __device__ inline f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c)
   else
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                    __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// D[16x16] += A[16x32] . B[32x16]; a lane supplies 8 consecutive k (8 * (lane / 16) on) of row/col (lane % 16)
+template <bool F16>
+__device__ inline f32x4v mfma16(const uint4& a, const uint4& b, const f32x4v& c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 #endif
 
