@@ -21,8 +21,9 @@
 //   waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two per wave in 8 waves, queries in LDS: 36 to
 //   46, no registers are left for K and V to be asked for ahead.)
 // * short lists: the chain launch arguments - item - tables - pages, 2.6 us to the first product, then 1.4 us for every tile of
-//   a wave (2 or 3 of them), 1.5 us to meet and store: 12 query heads on 2 kv heads, 32 groups of up to 8 candidates over 304
-//   positions, bf16, 13 MB: 10 us; two candidates over 80 positions, 4 heads of 64: 6 us.
+//   a wave (one after the other here; two at a time in the kernel for few columns), 1.5 us to meet and store: 12 query heads on 2 kv
+//   heads, 32 groups of up to 8 candidates over 304 positions, bf16, 13 MB: 10 us, 8.5 with few columns; two candidates over 80
+//   positions, 4 heads of 64: 5.5 and 5.2.
 #include <algorithm>
 #include <type_traits>
 
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
   // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
-  // XCD's runs, below).
+  // XCD's runs, below; blocks of 16 for 32 heads: 2 groups of up to 16 over 288 positions 13.2 and 10.0).
   if (w == NT / 64 - 1) {
     int each = 0;  // entries of a block (0: full width, whatever they are)
     if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
@@ -806,7 +807,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 // The same for short lists of blocks of up to 16 columns, no parts: products of 16 x 16 x 32, half the registers per column
 // block, and so two tiles at a time per wave.  A row of K is the key that the second product wants there: the row m = 4 * q + e of
 // product rb is key 16 * (q >> 1) + 8 * rb + 4 * (q & 1) + e, so that the 8 scores of a lane are, in order, the 8 weights that it owes
-// as the second operand, for the 16 bytes of V that lie together in the page.
+// as the second operand, for the 16 bytes of V that lie together in the page.  Bound by latency, then by what a CU fetches: one
+// token of 8 candidates over 288 positions, 32 heads of 128, 6.8 us; 2 groups of up to 8 x 8 tokens over 601 (36 MB) 11.6.
 template <int HD, bool F16>
 __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
   constexpr int NB = HD / 32, NF = HD / 16, U = 2;
