@@ -33,6 +33,7 @@ namespace {
 
 constexpr int kWaves = 8;            // of a workgroup; one workgroup per CU (256 registers a wave)
 constexpr int kCus = 256;
+constexpr int kLong = 64;            // pages of a list from which on it may be cut
 constexpr int kMaxParts = 64;
 constexpr int kPartTiles = 2048;     // column blocks x parts that the workspace holds at most
 
@@ -73,7 +74,7 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   const size_t least = (cols + 31) / 32 * p.n_kv_heads;
   // Parts where the column blocks do not fill the chip by themselves and the tables have room for lists that are long
   // for 8 waves (that decides whether the second kernel is launched: 2.5 us where it finds nothing to join)
-  l.parts = least < 2 * kCus && p.max_pages > 24;
+  l.parts = least < 2 * kCus && p.max_pages > kLong;
   // Blocks of up to 16 columns where one round of the chip holds all of them: 8.1 -> 6.8 us for 8 candidates over 288 positions (32
   // heads of 128), 16.3 -> 14.7 for 60 over 300, 21.3 -> 19.2 for 100.  In more than a round the pages are read too often: 150 over
   // 300 28.1 -> 34.1, grouped queries, 120 groups of up to 8 over 304, 21.3 -> 24.7.
@@ -219,7 +220,8 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __syncthreads();
   // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
   // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
-  const int log_most = a.width < 32 ? 0 : a.part_tiles > 0 || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  const bool cut = a.part_tiles > 0 && s_width + (a.tokens + kPage - 1) / kPage + 1 > kLong;  // (lists are cut into parts)
+  const int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
   // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       a.ent[i] = {seq, pos};
       if (seq >= 0) {
         own = pages_of(pos + a.tokens) - g_shared[g];
-        if (a.part_tiles > 0) atomicAdd(&g_own[g], own);
+        if (cut) atomicAdd(&g_own[g], own);
       }
     }
     const int longest = wave_max(own);
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   }
   // Work in steps of a wave, a key tile of a column block: tiles of the list of a group's block.  (An entry's own tiles are dealt
   // to its blocks as if each had them all; a block of tokens before the last sees fewer.)
-  if (a.part_tiles > 0) {
+  if (cut) {
     unsigned long long work = 0;
     int longest = 0;
     for (int g = tid; g < n_groups; g += NT) {
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   // Steps of a wave per item: the lanes of the first wave try the longest list in 1, 2, ... 64 parts, and take what
   // ends first: rounds of one item per CU x (steps + 3 for an item's start and end), + 3 for parts that have to be joined.
   // With many groups the chip is full anyhow, and the work per wave is the measure.
-  const int most = max(1, a.part_tiles / max(s_blocks, 1));  // parts that the workspace has room for
+  const int most = cut ? max(1, a.part_tiles / max(s_blocks, 1)) : 1;  // parts that the workspace has room for
   auto parts_of = [&](int g, int steps) {
     if (most == 1) return 1;
     const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most, block_cols).wk;
