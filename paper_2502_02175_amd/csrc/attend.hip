@@ -161,7 +161,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __shared__ Two sums[NT / 64];
   __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_own[N], q_item[N + 1], g_tile[N], l_seq[N], l_pos[N], l_own[N + 1];
   __shared__ unsigned short l_group[N];
-  __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_own, s_cols;
+  __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_area, s_own, s_cols;
   __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
             a.item, p.table, p.len, p.max_seqs, p.max_pages, p.n_kv_heads);
   const int hkv = p.n_kv_heads, grp = a.n_q_heads / hkv, per_entry = a.tokens * grp;  // columns of an entry per kv head
   if (tid == 0) {
-    s_bad = s_width = s_longest = s_blocks = s_own = 0;
+    s_bad = s_width = s_longest = s_blocks = s_area = s_own = 0;
     s_work = 0;
   }
 
@@ -210,17 +210,31 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
   widest = wave_max(widest);
   auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
-  int all_blocks = 0;  // (of full width)
-  for (int g = tid; g < n_groups; g += NT) all_blocks += (group_cols(g) + a.width - 1) / a.width * hkv;
+  int all_blocks = 0, area = 0;  // (of full width; blocks x pages / 64)
+  for (int g = tid; g < n_groups; g += NT) {
+    const int blocks = (group_cols(g) + a.width - 1) / a.width * hkv;
+    all_blocks += blocks;
+    area += min(blocks, 512) * (l_pos[g_start[g]] / kPage) >> 6;
+  }
   all_blocks = wave_sums(all_blocks);
+  area = wave_sums(area);
   if (lane == 63) {
     atomicMax(&s_width, widest);
     atomicAdd(&s_blocks, all_blocks);
+    atomicAdd(&s_area, area);
   }
   __syncthreads();
   // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
   // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
-  const bool cut = a.part_tiles > 0 && s_width + (a.tokens + kPage - 1) / kPage + 1 > kLong;  // (lists are cut into parts)
+  // Lists are cut where they are long and the blocks would not fill the chip (half of it, up to 128 pages) while the longest runs:
+  // 4 blocks side by side and a second kernel, instead of many blocks that read the same pages from the L2.  Uncut and cut, us: 20 groups
+  // of up to 45 over 2300 positions (16 query heads on 4 of 64) 26 and 35, over 6000 55 and 61; 8 x 19 tokens over 2300 (32 heads of
+  // 128) 24 and 31; 24 groups of up to 51 over 6000 (8 on 1 of 128, not quite a chip full of blocks) 87 and 66; up to 64 pages: 8
+  // candidates over 1400 (32 heads) 12.4 and 14.9, over 2300 18.8 and 17.2.
+  const int pages_most = s_width + (a.tokens + kPage - 1) / kPage + 1;
+  const long long filled = 64ll * s_area;  // blocks that last as long as it, x its length
+  const bool cut = a.part_tiles > 0 && pages_most > kLong &&
+                   (filled < (long long)(kCus / 2) * s_width || (pages_most > 2 * kLong && filled < (long long)kCus * s_width));
   const int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks

@@ -1,4 +1,4 @@
-"""The cases of test_gpu_attend once more in pools with longer tables: with room for more than 24 pages per sequence a list may be cut
+"""The cases of test_gpu_attend once more in pools with longer tables: with room for more than 64 pages per sequence a list may be cut
 into parts, and another kernel (blocks of 32 columns) does what the short tables leave to the one for 16; with many more entries
 than columns fit in a round of the chip neither cuts."""
 import pytest
@@ -14,7 +14,7 @@ def long_tables(monkeypatch):
     short = V.new_pages
 
     def new_pages(n_layers, n_kv_heads, head_dim, operand, n_pages, max_seqs, max_pages, device="cuda"):
-        return short(n_layers, n_kv_heads, head_dim, operand, n_pages, max_seqs, max(max_pages, 27), device)
+        return short(n_layers, n_kv_heads, head_dim, operand, n_pages, max_seqs, max(max_pages, 70), device)
 
     monkeypatch.setattr(V, "new_pages", new_pages)
 
@@ -55,3 +55,30 @@ def test_around_one_round_of_the_chip(hq, hkv, hd, operand, n, tokens):
     order = sorted(range(n), key=lambda i: i % 3)
     seqs = [c.sequence(pos[i] + tokens, stems[i % 3]) for i in order]
     T.compare(c, c.pool(), seqs, [pos[i] for i in order], T.queries(c, n, tokens, hq), [i % 3 for i in order])
+
+
+@pytest.mark.parametrize("hq,hkv,hd,operand", [(4, 4, 64, 1), (12, 2, 128, 0)])
+@pytest.mark.parametrize("stem", [3, 90])
+def test_far_values_in_a_place_that_some_rows_see(hq, hkv, hd, operand, stem):
+    """An infinite and a NaN value of V at the second of three new tokens: the first row does not see it, the others' features
+    are what it makes of them; over a short list, and over one that is cut into parts."""
+    import torch
+    c = T.Cache(hkv, hd, operand, seed=stem)
+    base = [c._new(T.PAGE) for _ in range(stem)]
+    pos = [32 * stem + 4 + i for i in range(5)]
+    seqs = [c.sequence(x + 3, base) for x in pos]
+    at = pos[1] + 1
+    page = c.pages[c.seqs[seqs[1]][0][at // 32]]
+    page[0, 1, at % 32, 0, 5] = float("inf")
+    page[0, 1, at % 32, hkv - 1, 6] = float("nan")
+    q = T.queries(c, 5, 3, hq)
+    got = T.run(c.pool(), c, seqs, pos, q, [0] * 5).double()
+    g = hq // hkv
+    for i in range(5):
+        for t in range(3):
+            want, tol = T.definition(c, [seqs[i]], [pos[i] + t], q[i:i + 1, t:t + 1])
+            if i == 1 and t > 0:
+                assert bool((got[i, t, :g, 5] == float("inf")).all()) and bool(got[i, t, hq - g:, 6].isnan().all())
+            fine = want[0, 0].isfinite()
+            assert fine.sum() == hq * hd - (2 * g if i == 1 and t > 0 else 0)
+            assert bool(((got[i, t] - want[0, 0]).abs() <= tol[0, 0])[fine].all()), (i, t)
