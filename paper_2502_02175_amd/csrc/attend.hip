@@ -1149,8 +1149,8 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
                         const int* group, void* ws, hipStream_t st) {
   const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles, (int)l.max_items, l.few ? 16 : 32,
-                      (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
+  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles,
+                      (int)l.max_items, l.few ? 16 : 32, (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
   // (4 waves or 16: one token of 2 candidates 7.3 and 8.2 us, 16 candidates x 56 tokens over 1057 positions 8.0 and 8.6; 48
   // candidates with tables of 1027 pages 40 and 20 when both were tried.  More entries than 128 are a second round for 4 waves.)
   if (n <= 128 && (long long)n * p.max_pages <= 4096)
@@ -1163,7 +1163,8 @@ void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, in
                    hipStream_t st) {
   const Layout l = layout_of(p, n, tokens, n_q_heads);
   char* b = (char*)ws;
-  const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own), (const Item*)(b + l.item),
+  const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own),
+                        (const Item*)(b + l.item),
                         (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
                         n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
   const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));

@@ -408,7 +408,9 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
   bf16_t* vd = kd + p.n_kv_heads * tile;
   const size_t k_at = (size_t)(c >> 1) * 512 + (c & 1) * 256 + r * 8;  // (f0: 64 features are 2048 values of either tile)
   // feature f0 + lane at position (at8 & 31) + 4 g of the V tile
-  auto v_at = [&](int g) { return (size_t)(lane >> 5) * 1024 + (((int)at8 & 31) >> 4) * 512 + g * 256 + (lane & 31) * 8 + (((int)at8 >> 3) & 1) * 4; };
+  auto v_at = [&](int g) {
+    return (size_t)(lane >> 5) * 1024 + (((int)at8 & 31) >> 4) * 512 + g * 256 + (lane & 31) * 8 + (((int)at8 >> 3) & 1) * 4;
+  };
   if (TILES) {
     const bf16_t* ks = a.k + ((size_t)i * 2 * p.n_kv_heads + h) * tile + (size_t)f0 * 32;
     const bf16_t* vs = ks + p.n_kv_heads * tile;
