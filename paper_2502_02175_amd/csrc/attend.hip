@@ -505,6 +505,12 @@ __device__ inline uint32_t pack2(float lo, float hi) {
   }
 }
 
+// How far above a column's maximum (log2) the reference point of its exponentials stands.  In fp32 a sum of weights times values of
+// bf16 would pass 2^128 where V is near the end of the type: with weights of up to 2^(8 - 32) and at most 2^20 positions it
+// stays below 2^124 (and a weight loses no bits: bf16 has fp32's range).  fp16 values end at 2^16, and its weights need their bits.
+template <bool F16>
+constexpr float kAbove = F16 ? 0.f : 32.f;
+
 // Masks of the two values of a word that are infinite or NaN, where asked for
 template <bool F16>
 __device__ inline uint32_t far_values(uint32_t x, bool lo, bool hi) {
@@ -637,13 +643,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     // (The weights are rounded to the type of the cache, half a step each: it is what the matrix core takes at its full rate, and
     // V has no more bits.  Their sum is that of the weights in fp32.)
     // Register 4*q4 + e of a lane is key 8*q4 + 4*g + e of the tile.  The reference point of a column's exponentials follows its
-    // maximum only when that has grown by more than 8 (weights stay below 256): then the rescaling of the sums is rare.  (The
+    // maximum only when that has grown by more than 8 (weights stay below 256, or 2^-24): then the rescaling of the sums is rare.  (The
     // decision is the column's own: its result does not depend on its neighbours.)
     auto weigh = [&](f32x16& s, uint4(&pb)[2]) {
       float tmax = -INFINITY;
 #pragma unroll
       for (int x = 0; x < 16; ++x) tmax = fmaxf(tmax, s[x]);
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * a.scale_log2e;  // (m is in units of log2)
+      tmax = fmaf(fmaxf(tmax, __shfl_xor(tmax, 32)), a.scale_log2e, kAbove<F16>);  // (m is in units of log2)
       float alpha = 1.f;
       if (tmax > m + 8.f) {
         alpha = __builtin_amdgcn_exp2f(m - tmax);  // (the first time 2^-inf = 0)
@@ -977,7 +983,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
             // (the reference point as above)
             float tmax = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
             tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
-            tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * a.scale_log2e;
+            tmax = fmaf(fmaxf(tmax, __shfl_xor(tmax, 32)), a.scale_log2e, kAbove<F16>);
             float alpha = 1.f;
             if (tmax > m + 8.f) {
               alpha = __builtin_amdgcn_exp2f(m - tmax);

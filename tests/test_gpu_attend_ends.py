@@ -30,7 +30,7 @@ def of_one_value(hkv, hd, operand, pages, T, hq, n, value, top=9.0):
     return c, s, length - T, q
 
 
-TYPES = [1]  # (fp16)
+TYPES = [0, 1]
 CASES = [(8, 1, 64, 60, 1), (8, 8, 64, 30, 1), (12, 2, 128, 30, 3)]
 
 
