@@ -172,6 +172,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     s_bad = s_width = s_longest = s_blocks = s_area = s_own = 0;
     s_work = 0;
   }
+  for (int g = tid; g < a.n; g += NT) g_own[g] = 0;
 
   int n_groups = 0;
   for (int base = 0; base < a.n; base += NT) {
@@ -186,7 +187,6 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       const int g = n_groups + before.a;
       g_start[g] = i;
       g_lead[g] = g_shared[g] = 0x7fffffff;
-      g_own[g] = 0;
     }
     if (i < a.n) {
       const long long at = (long long)p0 + a.add;
@@ -194,7 +194,9 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       if (p0 >= 0 && !fits) s_bad = 1;
       l_seq[i] = fits ? s : -1;
       l_pos[i] = fits ? (int)at : 0;
-      l_group[i] = (unsigned short)(n_groups + before.a + (start ? 1 : 0) - 1);
+      const int g = n_groups + before.a + (start ? 1 : 0) - 1;
+      l_group[i] = (unsigned short)g;
+      if (fits) atomicMax(&g_own[g], (int)at / kPage);  // (for a while: pages before the group's farthest query)
     }
     n_groups += total.a;
   }
@@ -210,14 +212,16 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
   widest = wave_max(widest);
   auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
-  int all_blocks = 0, area = 0;  // (of full width; blocks x pages / 64)
+  int all_blocks = 0, area = 0;  // (of full width; blocks x pages: no more than the rule below asks for, so that no sum overflows)
+  constexpr int kFull = kCus << 15;
   for (int g = tid; g < n_groups; g += NT) {
     const int blocks = (group_cols(g) + a.width - 1) / a.width * hkv;
     all_blocks += blocks;
-    area += min(blocks, 512) * (l_pos[g_start[g]] / kPage) >> 6;
+    area = min(area + min(blocks, 2 * kCus) * g_own[g], kFull);
+    g_own[g] = 0;
   }
   all_blocks = wave_sums(all_blocks);
-  area = wave_sums(area);
+  area = min(wave_sums(area), kFull);  // (of the last lane: all of them)
   if (lane == 63) {
     atomicMax(&s_width, widest);
     atomicAdd(&s_blocks, all_blocks);
@@ -232,9 +236,9 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   // 128) 24 and 31; 24 groups of up to 51 over 6000 (8 on 1 of 128, not quite a chip full of blocks) 87 and 66; up to 64 pages: 8
   // candidates over 1400 (32 heads) 12.4 and 14.9, over 2300 18.8 and 17.2.
   const int pages_most = s_width + (a.tokens + kPage - 1) / kPage + 1;
-  const long long filled = 64ll * s_area;  // blocks that last as long as it, x its length
+  const int filled = s_area;  // blocks that last as long as it, x its length
   const bool cut = a.part_tiles > 0 && pages_most > kLong &&
-                   (filled < (long long)(kCus / 2) * s_width || (pages_most > 2 * kLong && filled < (long long)kCus * s_width));
+                   (filled < kCus / 2 * s_width || (pages_most > 2 * kLong && filled < kCus * s_width));
   const int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
