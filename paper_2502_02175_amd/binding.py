@@ -43,6 +43,7 @@ class Pages(C.Structure):
 
 _PATH = os.path.join(_HERE, "libvlac.so")
 _LOADED = {}
+_SIZES = {}   # of the contexts that vlac_create made here: handle -> (vocabulary, bytes of the cache)
 
 
 def lib_path():
@@ -202,10 +203,13 @@ def vlac_create(cfg, check=True):
     out = C.c_void_p()
     st = lib().vlac_create(C.byref(cfg) if cfg is not None else None, C.byref(out))
     _ret(st, "vlac_create", check)
+    if st == VLAC_OK:
+        _SIZES[out.value] = (cfg.vocab, vlac_kv_cache_bytes(cfg))
     return out.value if st == VLAC_OK else st
 
 
 def vlac_destroy(ctx, check=True):
+    _SIZES.pop(ctx, None)
     return _ret(lib().vlac_destroy(ctx), "vlac_destroy", check)
 
 
@@ -478,6 +482,9 @@ def vlac_pages_check(p, stream=None, check=True):
 
 
 def vlac_pages_import(ctx, kv_cache, B, L, p, seqs, stream=None, check=True):
+    need = _SIZES.get(ctx, (0, 0))[1]
+    if hasattr(kv_cache, "numel") and kv_cache.numel() * kv_cache.element_size() < need:
+        raise ValueError("kv_cache holds %d bytes, the context's has %d" % (kv_cache.numel() * kv_cache.element_size(), need))
     return _call(p, "vlac_pages_import", stream, check, ctx, _at(p, kv_cache, None, 0, "kv_cache"), B, L, _ref(p),
                  _list(p, seqs, B, "seqs"))
 
@@ -542,6 +549,8 @@ def vlac_candidates_workspace_bytes(ctx, p, n):
 def vlac_decode_candidates(ctx, p, seqs, n, L, group, n_new, first_token, out_tokens, out_logits, workspace, stream=None,
                            check=True):
     ws, size = _workspace(p, workspace)
+    vocab = _SIZES.get(ctx, (0, 0))[0]
     return _call(p, "vlac_decode_candidates", stream, check, ctx, _ref(p), _list(p, seqs, n, "seqs"), n, L,
                  _list(p, group, n, "group"), n_new, _list(p, first_token, n, "first_token"),
-                 _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, p.torch.float32, 0, "out_logits"), ws, size)
+                 _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, p.torch.float32, n * n_new * vocab, "out_logits"),
+                 ws, size)
