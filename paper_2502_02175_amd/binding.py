@@ -39,6 +39,15 @@ class Pages(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_kv_heads", "head_dim", "operand_dtype",
                                          "n_pages", "max_seqs", "max_pages")] + [
         (n, C.c_void_p) for n in ("data", "refs", "table", "len", "scratch")]
+    index = -1   # the pool's device (-1: filled in with bare addresses, the current one)
+
+    def __getattr__(self, name):
+        """(what `pages` sets, for a pool that it did not make)"""
+        if name not in ("torch", "i32", "rows_dtype"):
+            raise AttributeError(name)
+        import torch
+        return {"torch": torch, "i32": torch.int32,
+                "rows_dtype": torch.bfloat16 if self.operand_dtype == OPERAND_BF16 else torch.float16}[name]
 
 
 _PATH = os.path.join(_HERE, "libvlac.so")
@@ -414,9 +423,14 @@ def _at(p, x, dtype, n, name):
     """Address of a contiguous tensor of at least n values on the pool's device (an address or None as it is)."""
     if x is None or isinstance(x, int):
         return x
-    if x.get_device() == p.index >= 0 and (dtype is None or x.dtype is dtype) and x.numel() >= n and x.is_contiguous():
+    if p is None or p.index < 0:
+        at = _ptr(x, dtype, name)
+        if x.numel() < n:
+            raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
+        return at
+    if x.get_device() == p.index and (dtype is None or x.dtype is dtype) and x.numel() >= n and x.is_contiguous():
         return x.data_ptr()
-    if x.get_device() != p.index or p.index < 0:
+    if x.get_device() != p.index:
         raise ValueError("%s lies on %s, the pool on GPU %d" % (name, x.device, p.index))
     if dtype is not None and x.dtype != dtype:
         raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, dtype))
@@ -426,7 +440,7 @@ def _at(p, x, dtype, n, name):
 
 
 def _list(p, x, n, name):
-    return _at(p, x, p.i32, n, name)
+    return _at(p, x, p.i32 if p is not None else None, n, name)
 
 
 def _rows(p, x, count, width, name):
@@ -450,7 +464,7 @@ def _rows(p, x, count, width, name):
 
 def _call(p, name, stream, check, *args):
     """One library call on the pool's device."""
-    index = getattr(p, "index", -1)
+    index = p.index if p is not None else -1
     if index >= 0 and stream is None and p.current() == index:
         status = getattr(_LIB or lib(), name)(*args, p.raw_stream(index))
         return status if status == VLAC_OK else _ret(status, name, check)
