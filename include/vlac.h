@@ -308,9 +308,11 @@ int vlac_decode_action(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* fi
  * nothing of a pool between calls and allocates nothing for it, so every call but vlac_pages_check
  * may be captured into a graph.  Calls on one pool go to one stream or are ordered by the caller.
  * Lists (of sequences, positions) are device int32 with n <= VLAC_PAGES_MAX_LIST entries, n = 0 is
- * allowed and does nothing.  Entries that do not fit (index out of range, a sequence whose len or
- * pages are out of range, a sequence listed twice where it would be changed twice) are ignored and
- * reported by vlac_pages_check.
+ * allowed and does nothing.  Entries that do not fit (index out of range, a sequence whose len is out
+ * of range, a sequence listed twice where it would be changed twice) are ignored and reported by
+ * vlac_pages_check.  A place of a sequence's row that names no page of the pool is reported by the calls that
+ * look at it, and nothing is read or written through it (a fork takes it over as it is, attention
+ * takes another page's values there).
  * Fresh pages are the free ones of lowest index, given out in the order of the list and of the
  * positions.  A call that needs more than there are changes nothing and is reported by vlac_pages_check. */
 #define VLAC_PAGES_MAX_LIST 4096

@@ -160,6 +160,7 @@ __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
       for (int j = lane; j < es.held[i]; j += 64) {
         const int pg = p.table[(size_t)d * p.max_pages + j];
         if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, by);
+        else report(p, PAGES_BAD_ENTRY);
       }
     }
   };
@@ -193,10 +194,15 @@ __global__ __launch_bounds__(kPlan) void pages_plan_kernel(PlanArgs a) {
           } else {
             const int f = first + j - kept;
             pg = fresh_pages[f];
-            if (MODE == FORK) p.copy_src()[f] = from[j];
+            if (MODE == FORK) {
+              const int of = from[j];
+              p.copy_src()[f] = of;
+              if ((unsigned)of >= (unsigned)p.n_pages) report(p, PAGES_BAD_ENTRY);  // (not copied)
+            }
             if (MODE == IMPORT) p.copy_src()[f] = i << 16 | j;
           }
           if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, 1);
+          else report(p, PAGES_BAD_ENTRY);
         }
         row[j] = pg;
       }
@@ -243,10 +249,12 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PoolView p, long long p
     const int live = ld_scalar(p.scratch + PG_COPIES + 1);
     for (int s = blockIdx.x; s < p.max_seqs; s += gridDim.x) {
       const int l = checked_len(p, s);
+      if (l < 0 && threadIdx.x == 0) report(p, PAGES_BAD_ENTRY);
       for (int j = threadIdx.x; j < (l > 0 ? pages_of(l) : 0); j += 256) {
         int* at = p.table + (size_t)s * p.max_pages + j;
         const int pg = *at;
-        if (pg >= live && pg < p.n_pages) *at = p.moved_to()[pg];
+        if ((unsigned)pg >= (unsigned)p.n_pages) report(p, PAGES_BAD_ENTRY);
+        else if (pg >= live) *at = p.moved_to()[pg];
       }
     }
   }
@@ -289,7 +297,10 @@ __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* 
   __syncthreads();
   int l = s_len;
   if (l < 0 || l > p.max_pages * kPage) {
-    if (threadIdx.x == 0) report(p, PAGES_BAD_ENTRY);
+    if (threadIdx.x == 0) {
+      atomicExch(p.len + s, l);  // (left as it was; another entry of the same sequence finds this or 0)
+      report(p, PAGES_BAD_ENTRY);
+    }
     return;
   }
   for (int j = threadIdx.x; j < pages_of(l); j += 256) {
@@ -297,6 +308,7 @@ __global__ __launch_bounds__(256) void pages_free_kernel(PoolView p, const int* 
     const int pg = *at;
     *at = -1;
     if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, -1);
+    else report(p, PAGES_BAD_ENTRY);
   }
 }
 
