@@ -380,16 +380,17 @@ struct AppendArgs {
   const int *seqs, *pos;
   const bf16_t *k, *v;
   long long row_stride;
+  int first;  // wave of the call that this launch begins with
 };
 template <bool TILES>
 __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
   __shared__ uint4 turn[4][64];
   const PoolView& p = a.p;
-  read_args(a.layer, a.n, a.tokens, a.add, a.blocks, a.seqs, a.pos, a.k, a.v, a.row_stride, p.data, p.refs, p.table, p.len, p.n_pages,
+  read_args(a.layer, a.n, a.tokens, a.add, a.blocks, a.seqs, a.pos, a.k, a.v, a.row_stride, a.first, p.data, p.refs, p.table, p.len, p.n_pages,
             p.max_seqs, p.max_pages, p.n_layers, p.n_kv_heads, p.head_dim);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7, r8 = lane >> 3;
   const int per_block = p.n_kv_heads * (p.head_dim >> 6);  // waves for a block of positions
-  const int u = blockIdx.x * 4 + w, ib = u / per_block, hf = u - ib * per_block, i = ib / a.blocks, blk = ib - i * a.blocks;
+  const int u = a.first + blockIdx.x * 4 + w, ib = u / per_block, hf = u - ib * per_block, i = ib / a.blocks, blk = ib - i * a.blocks;
   if (i >= a.n) return;
   const int h = hf / (p.head_dim >> 6), f0 = (hf - h * (p.head_dim >> 6)) * 64;
   const int p0 = ld_scalar(a.pos + i), s = ld_scalar(a.seqs + i);
@@ -492,14 +493,18 @@ void launch_extend(const PoolView& p, const int* seqs, int n, int tokens, int wa
 static void launch_append(bool tiles, AppendArgs a, hipStream_t st) {
   a.blocks = (a.tokens + 14) / 8;
   const long long waves = (long long)a.n * a.blocks * a.p.n_kv_heads * (a.p.head_dim / 64);
-  const dim3 grid((unsigned)((waves + 3) / 4));
-  if (tiles) hipLaunchKernelGGL(pages_append_kernel<true>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(pages_append_kernel<false>, grid, dim3(256), 0, st, a);
+  // (a launch of 2^32 threads and more would run only what is left of them modulo 2^32; a call has up to 2^28 waves)
+  constexpr int kMost = 1 << 24;
+  for (a.first = 0; a.first < waves; a.first += kMost) {
+    const dim3 grid((unsigned)((std::min<long long>(waves - a.first, kMost) + 3) / 4));
+    if (tiles) hipLaunchKernelGGL(pages_append_kernel<true>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(pages_append_kernel<false>, grid, dim3(256), 0, st, a);
+  }
 }
 
 void launch_append_tiles(const PoolView& p, int layer, const int* seqs, const int* pos, int add, int n,
                          const bf16_t* tiles, hipStream_t st) {
-  const AppendArgs a = {p, layer, n, 1, add, 0, seqs, pos, tiles, nullptr, 0};
+  const AppendArgs a = {p, layer, n, 1, add, 0, seqs, pos, tiles, nullptr, 0, 0};
   launch_append(true, a, st);
 }
 
@@ -591,7 +596,7 @@ int vlac_pages_append(const vlac_pages* pages, int layer, const int32_t* seqs, c
   if (n == 0) return VLAC_OK;
   if (!seqs || !pos || !k || !v) return VLAC_E_NULL;
   if ((uintptr_t)k % 16 || (uintptr_t)v % 16) return VLAC_E_SHAPE;
-  const AppendArgs a = {pool_view(pages), layer, n, tokens, 0, 0, seqs, pos, (const bf16_t*)k, (const bf16_t*)v, row_stride};
+  const AppendArgs a = {pool_view(pages), layer, n, tokens, 0, 0, seqs, pos, (const bf16_t*)k, (const bf16_t*)v, row_stride, 0};
   launch_append(false, a, (hipStream_t)stream);
   return launched();
 }
