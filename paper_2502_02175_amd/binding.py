@@ -39,15 +39,8 @@ class Pages(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_kv_heads", "head_dim", "operand_dtype",
                                          "n_pages", "max_seqs", "max_pages")] + [
         (n, C.c_void_p) for n in ("data", "refs", "table", "len", "scratch")]
-    index = -1   # the pool's device (-1: filled in with bare addresses, the current one)
-
-    def __getattr__(self, name):
-        """(what `pages` sets, for a pool that it did not make)"""
-        if name not in ("torch", "i32", "rows_dtype"):
-            raise AttributeError(name)
-        import torch
-        return {"torch": torch, "i32": torch.int32,
-                "rows_dtype": torch.bfloat16 if self.operand_dtype == OPERAND_BF16 else torch.float16}[name]
+    index = -1          # the pool's device (-1: filled in with bare addresses, the current one)
+    rows_dtype = None   # torch type of the values (None: not asked for yet)
 
 
 _PATH = os.path.join(_HERE, "libvlac.so")
@@ -395,9 +388,8 @@ def pages(n_layers, n_kv_heads, head_dim, operand_dtype, data, refs, table, leng
     p.tensors = (data, refs, table, length, scratch)
     p.index = refs.get_device()
     p.torch = torch
-    p.i32 = torch.int32
     p.raw_stream, p.current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-    p.rows_dtype = torch.bfloat16 if operand_dtype == OPERAND_BF16 else torch.float16
+    p.rows_dtype = _rows_dtype(p)
     p.data = _at(p, data, None, 0, "data")
     p.refs, p.table = _at(p, refs, torch.int32, 0, "refs"), _at(p, table, torch.int32, 0, "table")
     p.len, p.scratch = _at(p, length, torch.int32, 0, "length"), _at(p, scratch, torch.int32, words, "scratch")
@@ -423,14 +415,13 @@ def _at(p, x, dtype, n, name):
     """Address of a contiguous tensor of at least n values on the pool's device (an address or None as it is)."""
     if x is None or isinstance(x, int):
         return x
-    if p is None or p.index < 0:
-        at = _ptr(x, dtype, name)
-        if x.numel() < n:
-            raise ValueError("%s holds %d values, %d are needed" % (name, x.numel(), n))
-        return at
-    if x.get_device() == p.index and (dtype is None or x.dtype is dtype) and x.numel() >= n and x.is_contiguous():
+    if x.get_device() == p.index >= 0 and (dtype is None or x.dtype is dtype) and x.numel() >= n and x.is_contiguous():
         return x.data_ptr()
-    if x.get_device() != p.index:
+    if p.index < 0:
+        at = _ptr(x, dtype, name)
+        if x.numel() >= n:
+            return at
+    elif x.get_device() != p.index:
         raise ValueError("%s lies on %s, the pool on GPU %d" % (name, x.device, p.index))
     if dtype is not None and x.dtype != dtype:
         raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, dtype))
@@ -440,7 +431,22 @@ def _at(p, x, dtype, n, name):
 
 
 def _list(p, x, n, name):
-    return _at(p, x, p.i32 if p is not None else None, n, name)
+    return _at(p, x, _I32 or _int32(), n, name)
+
+
+_I32 = None   # torch.int32, once it is known
+
+
+def _int32():
+    global _I32
+    import torch
+    _I32 = torch.int32
+    return _I32
+
+
+def _rows_dtype(p):
+    import torch
+    return torch.bfloat16 if p.operand_dtype == OPERAND_BF16 else torch.float16
 
 
 def _rows(p, x, count, width, name):
@@ -451,15 +457,16 @@ def _rows(p, x, count, width, name):
         return x.data_ptr(), width
     if x.numel() != count * width:
         raise ValueError("%s holds %d values, expected %d rows of %d" % (name, x.numel(), count, width))
+    dtype = p.rows_dtype or _rows_dtype(p)
     if x.is_contiguous():
-        return _at(p, x, p.rows_dtype, 0, name), width
+        return _at(p, x, dtype, 0, name), width
     try:
         y = x.view(count, width)   # (such a view exists if the rows are equally far apart and dense)
     except RuntimeError:
         y = None
     if y is None or y.stride(1) != 1:
         raise ValueError("%s: rows must be dense and equally far apart" % name)
-    return _at(p, y[0], p.rows_dtype, 0, name), (y.stride(0) if count > 1 else width)
+    return _at(p, y[0], dtype, 0, name), (y.stride(0) if count > 1 else width)
 
 
 def _call(p, name, stream, check, *args):
@@ -553,7 +560,7 @@ def vlac_attend_shared(p, layer, n, tokens, n_q_heads, q, out, workspace, stream
     q_at, q_stride = _rows(p, q, count, width, "q")
     ws, size = _workspace(p, workspace)
     return _call(p, "vlac_attend_shared", stream, check, _ref(p), layer, n, tokens, n_q_heads, q_at, q_stride,
-                 _at(p, out, p.rows_dtype, count * width, "out"), ws, size)
+                 _at(p, out, p.rows_dtype or _rows_dtype(p), count * width, "out"), ws, size)
 
 
 def vlac_candidates_workspace_bytes(ctx, p, n):
@@ -562,9 +569,10 @@ def vlac_candidates_workspace_bytes(ctx, p, n):
 
 def vlac_decode_candidates(ctx, p, seqs, n, L, group, n_new, first_token, out_tokens, out_logits, workspace, stream=None,
                            check=True):
+    import torch
     ws, size = _workspace(p, workspace)
     vocab = _SIZES.get(ctx, (0, 0))[0]
     return _call(p, "vlac_decode_candidates", stream, check, ctx, _ref(p), _list(p, seqs, n, "seqs"), n, L,
                  _list(p, group, n, "group"), n_new, _list(p, first_token, n, "first_token"),
-                 _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, p.torch.float32, n * n_new * vocab, "out_logits"),
+                 _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, torch.float32, n * n_new * vocab, "out_logits"),
                  ws, size)
