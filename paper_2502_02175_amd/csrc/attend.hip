@@ -15,8 +15,9 @@
 // What bounds it, and what it takes (32 query and kv heads of 128, fp16, if not said otherwise):
 // * long lists: memory.  48 candidates over 32801 shared positions (554 MB of K and V) 99 to 102 us, 5.5 TB/s, and 5.5 us to join.
 // * many columns: what a CU moves into registers, 64 bytes per clock.  Every wave reads the K and V of a tile (16 KiB) for
-//   its 32 columns: 16 candidates x 56 tokens over 1057 positions (16 GFLOP) 34 to 35 us, that path busy 73 % of the time, the
-//   matrix cores 27 %, the softmax's instructions 37 %; two waves per SIMD overlap them in part.  (Pages staged in LDS for all
+//   its 32 columns: 16 candidates x 56 tokens over 1057 positions (16 GFLOP) 34 to 36 us, that path busy 73 % of the time, the
+//   matrix cores 27 %, the softmax's instructions 37 %; two waves per SIMD overlap them in part.  (28 blocks x 32 heads in items of 4
+//   are 224 items: 32 of the 256 CUs have none.)  (Pages staged in LDS for all
 //   blocks of an item: 35 us as against 32 then, the meetings of the waves cost what the reads save; two column blocks per wave in 4
 //   waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two per wave in 8 waves, queries in LDS: 36 to
 //   46, no registers are left for K and V to be asked for ahead.)
@@ -73,11 +74,13 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   const size_t cols = (size_t)n * tokens * (n_q_heads / p.n_kv_heads);  // per kv head
   const size_t least = (cols + 31) / 32 * p.n_kv_heads;
   // Parts where the column blocks do not fill the chip by themselves and the tables have room for lists that are long
-  // for 8 waves (that decides whether the second kernel is launched: 2.5 us where it finds nothing to join)
+  // for 8 waves.  That is all that the host knows: it decides whether the second kernel is launched (2.5 us where it finds nothing to
+  // join) and, below, which kernel the first is.  Short lists in wide tables pay for it: 8 candidates over 288 positions 7.3 us a
+  // layer with up to 64 columns, 10.4 with more; 2 groups of up to 8 x 8 tokens over 601 11.9 and 14.7.
   l.parts = least < 2 * kCus && p.max_pages > kLong;
-  // Blocks of up to 16 columns where one round of the chip holds all of them: 8.1 -> 6.8 us for 8 candidates over 288 positions (32
-  // heads of 128), 16.3 -> 14.7 for 60 over 300, 21.3 -> 19.2 for 100.  In more than a round the pages are read too often: 150 over
-  // 300 28.1 -> 34.1, grouped queries, 120 groups of up to 8 over 304, 21.3 -> 24.7.
+  // Blocks of up to 16 columns where one round of the chip holds all of them: 6.8 us, and 8.1 with blocks of 32, for 8 candidates
+  // over 288 positions (32 heads of 128), 14.7 and 16.3 for 60 over 300, 19.2 and 21.3 for 100.  In more than a round the pages
+  // are read too often: 150 over 300 34.1 and 28.1, grouped queries, 120 groups of up to 8 over 304, 24.7 and 21.3.
   l.few = !l.parts && cols <= (size_t)16 * n && (cols + 15) / 16 * p.n_kv_heads <= kCus;
   const size_t max_blocks = (l.few ? (cols + 15) / 16 * p.n_kv_heads : least) + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
   l.part_tiles = l.parts ? (int)std::min<size_t>(kPartTiles, max_blocks * kMaxParts) : 0;
@@ -684,7 +687,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 
     // Two blocks side by side read the same pages, each page by two waves: those keep step (by a barrier that orders no memory, once
     // per shared step that every wave has), so that the second finds the page in this CU's L1.  48 candidates over 32801 positions
-    // 118 -> 112 us, 2 x 40 over 9000 83 -> 79, short lists as before.  With heads of 64 the pages of all waves fit into the L1 anyway
+    // 112 us, and 118 without, 2 x 40 over 9000 79 and 83, short lists equal.  With heads of 64 the pages of all waves fit into the L1 anyway
     // (6 groups of 1 to 3 x 6 tokens over 18532 positions, 4 heads: 26.4 without, 28.0 with), and with four blocks the waves
     // lose by it (grouped queries, 24 x 17009 positions: 32.9 and 37.0).
     const int together = HD == 128 && wc == 2 && (im.block0 + 1) * width < cols ? (s1 - s0) >> wk_log : 0;
