@@ -422,6 +422,127 @@ int vlac_decode_candidates(vlac_ctx* ctx, const vlac_pages* pages, const int32_t
                            int32_t* out_tokens, float* out_logits, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/* ---- Drafted tokens: several tokens of a sequence checked in one pass (beyond the paper) ----
+ *
+ * A caller that has guesses for the tokens to come (from a smaller decoder, from the last step's actions, from a table) lets
+ * one pass look at all of them: the guesses of a sequence form a tree, and the path on which they are what the decoder chooses
+ * is kept.  A pass, in order: vlac_pages_extend (room for the nodes), vlac_attend_tree_plan, per layer
+ * vlac_pages_append_rotated and vlac_attend_tree, on the logits vlac_choose_tokens, then vlac_tree_accept and vlac_pages_keep.
+ *
+ * A tree has `tokens` places, at most VLAC_TREE_MAX_NODES: parents, device int32 [n, tokens]: parents[i, t] < t is the
+ * node that node t follows, -1: it follows the cached sequence, -2: there is no node t (trees of different sizes in a
+ * batch).  A value outside -2 .. t - 1, and a node that follows one which is not there, counts as not there.  Node t has the cache
+ * slot pos[i] + t until a path is kept, and the place pos[i] + (nodes above it) in the text, which is what its rotation goes by. */
+#define VLAC_TREE_MAX_NODES 512
+
+/* Rotary positions: the leading `dims` features of a head (even, at most head_dim) are turned in pairs, pair f by
+ * 2 pi turns[f] * place, and scaled by `amplitude`; the others stay.  VLAC_ROTARY_HALF: features f and f + dims / 2
+ * are a pair (what the context's projections do with dims = head_dim); VLAC_ROTARY_PAIRS: features 2 f and 2 f + 1. */
+enum { VLAC_ROTARY_HALF = 0, VLAC_ROTARY_PAIRS = 1 };
+typedef struct {
+  int32_t dims, layout;
+  float amplitude;      /* 1, or what a scaling for long contexts multiplies queries and keys by */
+  const double* turns;  /* device [dims / 2]: turns per position (vlac_rotary_fill, or the caller's own) */
+} vlac_rotary;
+
+/* turns[f] = w / (2 pi), w = base^(-2 f / dims) scaled for contexts that are `factor` times longer than those of training:
+ * factor = 1: as it is; original = 0: w / factor (positions are interpolated); original > 0: by bands, with r = original * w / (2 pi)
+ * the turns over the original length: w / factor where r <= low, w where r >= high, between them
+ * w (s + (1 - s) / factor), s = (r - low) / (high - low).  dims even, 2 .. 128; base > 1, factor >= 1, original >= 0,
+ * 0 <= low < high, all finite.  In 64 bits.  turns: device [dims / 2]. */
+int vlac_rotary_fill(int dims, double base, double factor, double original, double low, double high, double* turns,
+                     void* stream);
+
+/* vlac_pages_append with the norm of every head and the rotation applied on the way, for queries, keys and values of a joint
+ * projection:  q' = R(place) N(q), k' = R(place) N(k), v' = v,  N(x) = x / sqrt(mean(x^2) + eps) * gain over the head's
+ * features.  K and V go into the pages, q' to q_out.
+ * places: device int32 [n, tokens], what each row is rotated by (vlac_attend_tree_plan's out_places; negative: there is no such
+ * token, its K, V and q' are zeros); NULL: pos[i] + t.  rot: NULL: no rotation.  q_gain, k_gain: device bf16 [head_dim], each
+ * may be NULL: no norm (eps >= 0 is not looked at if both are).
+ * q: device, row (i, t) at element (i * tokens + t) * q_stride, in it [n_q_heads][head_dim] values of the pool's type; q_out the
+ * same with q_out_stride, it may be q (with the same stride).  n_q_heads = 0: keys and values only (q and q_out are not looked at).
+ * n_q_heads at most 1024, else unrelated to n_kv_heads.  k, v, kv_stride, and which positions are written or reported: as for
+ * vlac_pages_append; an entry whose pos is negative is skipped (its rows of q_out stay), any other has its q_out written.
+ * q, k, v, q_out and the gains are 16-byte aligned, strides are multiples of 8.
+ * Computed in fp32 (angles in 64 bits), rounded once; beyond fp16's range finite values saturate at +-65504 there.  A head without norm or
+ * rotation is copied as it is. */
+int vlac_pages_append_rotated(const vlac_pages* pages, int layer, const int32_t* seqs, const int32_t* pos, int n, int tokens,
+                              const vlac_rotary* rot, const int32_t* places, int n_q_heads, const void* q, int64_t q_stride,
+                              const void* k, const void* v, int64_t kv_stride, void* q_out, int64_t q_out_stride,
+                              const void* q_gain, const void* k_gain, float eps, void* stream);
+
+/* vlac_attend_plan and vlac_attend_shared for trees: node t of entry i sees the positions before pos[i], itself and the
+ * nodes above it.  The sequence holds pos[i] + tokens positions (or more).  A node that is not there gets a row of zeros and is
+ * seen by no other; what lies in its slot may be anything.  A parent outside -2 .. t - 1 is reported by vlac_pages_check.
+ * out_places: device int32 [n, tokens] or NULL: every node's place in the text, -1 for those that are not there and for entries
+ * that do not fit.  Everything else, the rules for workspaces among it, is as there; a workspace planned by one of the two plans is
+ * not used by the other's attention.  tokens <= VLAC_TREE_MAX_NODES. */
+size_t vlac_attend_tree_workspace_bytes(const vlac_pages* pages, int n, int tokens, int n_q_heads);
+int vlac_attend_tree_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens,
+                          int n_q_heads, const int32_t* group, const int32_t* parents, int32_t* out_places,
+                          void* workspace, size_t workspace_bytes, void* stream);
+int vlac_attend_tree(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q,
+                     int64_t q_stride, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What may be chosen, and at what price.  In this order, in fp32, each step rounded:
+ *   a token that the row's text holds `count` > 0 times:  l = l > 0 ? l / repetition : l * repetition;  l = l - presence;
+ *   l = l - frequency * count;
+ *   l = l + bias;
+ *   a token that is not allowed: l = -infinity, whatever it was.
+ * The text of a row is its entry's history, and where there are trees (parents and drafted not NULL) the drafted tokens of the row's
+ * node and of those above it; a node that is not there has the history only.  Tokens outside the vocabulary do not count. */
+typedef struct {
+  float repetition, presence, frequency; /* repetition > 0 (1: none), all finite */
+  const float* bias;        /* device [vocab], row r at r * bias_stride (0: one for all rows), or NULL */
+  int64_t bias_stride;
+  const uint32_t* allowed;  /* device bits: token v of row r is bit v % 32 of word r * allowed_stride + v / 32 (0: one for all rows); NULL: every token */
+  int64_t allowed_stride;
+  const int32_t* history;   /* device, entry i's at i * history_stride, history_len[i] of them (both NULL: none) */
+  const int32_t* history_len; /* device [n]; negative counts as 0, more than history_stride as history_stride */
+  int64_t history_stride;
+  int32_t tokens;           /* rows of an entry: row r is node r % tokens of entry r / tokens; 1 without trees */
+  const int32_t *parents, *drafted; /* device [n, tokens], or both NULL */
+} vlac_token_rules;
+#define VLAC_CHOOSE_MAX_ROWS 1048576
+
+/* Applies the rules to the logits of `rows` rows (a multiple of rules->tokens) and picks the greatest of each row.
+ * logits: device fp32, row r at r * stride; out_logits: the same with out_stride, may be logits (with the same stride), or NULL;
+ * out_token: device int32 [rows] or NULL: the greedy token (ties: lower id; a NaN is never chosen; -1: no token is above
+ * -infinity).  rows <= VLAC_CHOOSE_MAX_ROWS, 1 <= vocab <= 2^24.  workspace: device, vlac_choose_workspace_bytes (0: arguments not
+ * allowed), 16-byte aligned; it is written before it is read, and may be NULL where out_token is. */
+size_t vlac_choose_workspace_bytes(int rows, int vocab);
+int vlac_choose_tokens(const float* logits, int rows, int vocab, int64_t stride, const vlac_token_rules* rules,
+                       float* out_logits, int64_t out_stride, int32_t* out_token, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* The path through each tree on which the drafts are what was chosen: it begins at node 0 (whose token is known: the one that
+ * was chosen last and is not in the cache yet) and goes on, from node t, to the first node that follows t and whose drafted
+ * token is chosen[t].  drafted, chosen: device int32 [n, tokens] (chosen: what the decoder picks after each node).
+ * out_path: device int32 [n, tokens]: the nodes of the path, ascending, then -1; out_count: device int32 [n]: how many
+ * (0 if there is no node 0); out_token: device int32 [n]: the token chosen after the last of them (-1 if there is none), the root of
+ * the next tree.  n <= VLAC_PAGES_MAX_LIST.  The outputs overlap neither the inputs nor each other. */
+int vlac_tree_accept(const int32_t* parents, const int32_t* drafted, const int32_t* chosen, int n, int tokens,
+                     int32_t* out_path, int32_t* out_count, int32_t* out_token, void* stream);
+
+/* Keeps the listed new tokens of each sequence and gives the others up: of the `tokens` positions from pos[i] on, which have
+ * to be the sequence's last, those at pos[i] + path[i, 0 .. count[i]) move (K and V, all layers) to pos[i], pos[i] + 1, ...;
+ * the sequence is pos[i] + count[i] positions long afterwards, and pages behind that are released.
+ * path: device int32 [n, tokens], ascending (vlac_tree_accept's out_path), count: device int32 [n], 0 .. tokens.
+ * An entry whose pos is negative is skipped.  Entries that do not fit (a path that does not ascend or leaves the new tokens, a count
+ * out of range, a sequence of another length or listed before, a row to be moved that lies in no page of the pool or moves to one
+ * that other sequences hold) are ignored as a whole and reported by vlac_pages_check.  tokens <= VLAC_TREE_MAX_NODES. */
+int vlac_pages_keep(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens, const int32_t* path,
+                    const int32_t* count, void* stream);
+
+/* vlac_decode_candidates under rules: row (i, t) of the rules' bias and masks is i * n_new + t, the choice of candidate i's
+ * t-th new token; its text is history[i], first_token[i] and the tokens chosen so far.  rules->tokens is 1, and there are no
+ * parents.  out_logits hold the logits under the rules.  A choice of -1 (nothing was allowed) is returned as such, and decoding
+ * goes on as if it were token 0.  workspace: vlac_guided_workspace_bytes. */
+size_t vlac_guided_workspace_bytes(const vlac_ctx* ctx, const vlac_pages* pages, int n);
+int vlac_decode_guided(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L, const int32_t* group,
+                       int n_new, const int32_t* first_token, const vlac_token_rules* rules, int32_t* out_tokens,
+                       float* out_logits, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

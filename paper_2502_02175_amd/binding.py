@@ -43,6 +43,24 @@ class Pages(C.Structure):
     rows_dtype = None   # torch type of the values (None: not asked for yet)
 
 
+ROTARY_HALF, ROTARY_PAIRS = 0, 1
+TREE_MAX_NODES = 512
+
+
+class Rotary(C.Structure):
+    """vlac_rotary; made by `rotary`, which keeps its table alive."""
+    _fields_ = [("dims", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("turns", C.c_void_p)]
+
+
+class TokenRules(C.Structure):
+    """vlac_token_rules; made by `token_rules`, which keeps the tensors alive."""
+    _fields_ = [("repetition", C.c_float), ("presence", C.c_float), ("frequency", C.c_float),
+                ("bias", C.c_void_p), ("bias_stride", C.c_int64), ("allowed", C.c_void_p), ("allowed_stride", C.c_int64),
+                ("history", C.c_void_p), ("history_len", C.c_void_p), ("history_stride", C.c_int64),
+                ("tokens", C.c_int32), ("parents", C.c_void_p), ("drafted", C.c_void_p)]
+    index, entries, rows, vocab, words = -1, None, None, None, None   # the tensors' device and sizes (None: any)
+
+
 _PATH = os.path.join(_HERE, "libvlac.so")
 _LOADED = {}
 _SIZES = {}   # of the contexts that vlac_create made here: handle -> (vocabulary, bytes of the cache)
@@ -121,6 +139,23 @@ def lib():
         L.vlac_candidates_workspace_bytes.argtypes = [vp, pp, i32]
         L.vlac_candidates_workspace_bytes.restype = sz
         L.vlac_decode_candidates.argtypes = [vp, pp, vp, i32, i32, vp, i32, vp, vp, vp, vp, sz, vp]
+        rp, tp, f64 = C.POINTER(Rotary), C.POINTER(TokenRules), C.c_double
+        L.vlac_rotary_fill.argtypes = [i32, f64, f64, f64, f64, f64, vp, vp]
+        L.vlac_pages_append_rotated.argtypes = [pp, i32, vp, vp, i32, i32, rp, vp, i32, vp, i64, vp, vp, i64, vp, i64, vp, vp, f32, vp]
+        L.vlac_attend_tree_workspace_bytes.argtypes = [pp, i32, i32, i32]
+        L.vlac_attend_tree_plan.argtypes = [pp, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.vlac_attend_tree.argtypes = [pp, i32, i32, i32, i32, vp, i64, vp, vp, sz, vp]
+        L.vlac_choose_workspace_bytes.argtypes = [i32, i32]
+        L.vlac_choose_tokens.argtypes = [vp, i32, i32, i64, tp, vp, i64, vp, vp, sz, vp]
+        L.vlac_tree_accept.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.vlac_pages_keep.argtypes = [pp, vp, vp, i32, i32, vp, vp, vp]
+        L.vlac_guided_workspace_bytes.argtypes = [vp, pp, i32]
+        L.vlac_decode_guided.argtypes = [vp, pp, vp, i32, i32, vp, i32, vp, tp, vp, vp, vp, sz, vp]
+        for name in ("vlac_attend_tree_workspace_bytes", "vlac_choose_workspace_bytes", "vlac_guided_workspace_bytes"):
+            getattr(L, name).restype = sz
+        for name in ("vlac_rotary_fill", "vlac_pages_append_rotated", "vlac_attend_tree_plan", "vlac_attend_tree", "vlac_choose_tokens",
+                     "vlac_tree_accept", "vlac_pages_keep", "vlac_decode_guided"):
+            getattr(L, name).restype = i32
         for name in ("vlac_pages_reset", "vlac_pages_check", "vlac_pages_import", "vlac_pages_fork", "vlac_pages_extend",
                      "vlac_pages_append", "vlac_pages_free", "vlac_pages_compact", "vlac_attend_plan",
                      "vlac_attend_shared", "vlac_decode_candidates"):
@@ -576,3 +611,237 @@ def vlac_decode_candidates(ctx, p, seqs, n, L, group, n_new, first_token, out_to
                  _list(p, group, n, "group"), n_new, _list(p, first_token, n, "first_token"),
                  _list(p, out_tokens, n * n_new, "out_tokens"), _at(p, out_logits, torch.float32, n * n_new * vocab, "out_logits"),
                  ws, size)
+
+
+# ---- drafted tokens: a tree of them checked in one pass ----
+
+class _Gpu:
+    """What a call without a pool asks of a device (a pool carries the same)."""
+    rows_dtype = None
+
+    def __init__(self, index):
+        import torch
+        self.index, self.torch = index, torch
+        self.raw_stream, self.current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+_GPUS = {}
+
+
+def _gpu_of(*tensors):
+    """The device of the first tensor among the arguments (None: addresses only, the current one)."""
+    for x in tensors:
+        if hasattr(x, "get_device"):
+            index = x.get_device()
+            if index < 0:
+                raise ValueError("the tensors must live in GPU memory")
+            g = _GPUS.get(index)
+            if g is None:
+                g = _GPUS[index] = _Gpu(index)
+            return g
+    return None
+
+
+def _on(g, x, dtype, n, name):
+    if g is None:
+        return x
+    return _at(g, x, dtype, n, name)
+
+
+def vlac_rotary_fill(dims, base, factor, original, low, high, turns, stream=None, check=True):
+    """turns: float64 GPU tensor [dims / 2]."""
+    import torch
+    g = _gpu_of(turns)
+    return _call(g, "vlac_rotary_fill", stream, check, dims, base, factor, original, low, high,
+                 _on(g, turns, torch.float64, dims // 2, "turns"))
+
+
+def rotary(dims, layout=ROTARY_HALF, base=10000.0, factor=1.0, original=0, low=1.0, high=32.0, amplitude=1.0, turns=None, device="cuda"):
+    """The vlac_rotary for the leading `dims` features of a head: its table is filled by vlac_rotary_fill, or is the caller's
+    `turns` (float64 [dims / 2], turns per position)."""
+    import torch
+    if turns is None:
+        turns = torch.empty(max(int(dims) // 2, 1), dtype=torch.float64, device=device)
+        vlac_rotary_fill(dims, base, factor, original, low, high, turns)
+    r = Rotary(dims, layout, amplitude, _at(_gpu_of(turns), turns, torch.float64, dims // 2, "turns"))
+    r.tensors = (turns,)
+    r.ref = C.byref(r)
+    return r
+
+
+def _heads(p, x, count, heads, name):
+    """Address and row stride of rows [.., heads, head_dim] of the pool's type: the last two dimensions dense, rows equally far apart."""
+    if x is None or isinstance(x, int):
+        return x, heads * p.head_dim
+    return _rows(p, x, count, heads * p.head_dim, name)
+
+
+def vlac_pages_append_rotated(p, layer, seqs, pos, n, tokens, rot, places, n_q_heads, q, k, v, q_out, q_gain=None, k_gain=None, eps=1e-6,
+                              stream=None, check=True):
+    """q, q_out: [n, tokens, n_q_heads, head_dim], k, v: [n, tokens, n_kv_heads, head_dim], of the pool's type; slices of a joint
+    projection have one row stride.  rot: `rotary`'s, or None; gains: bf16 [head_dim], or None."""
+    count = n * tokens
+    k_at, k_stride = _heads(p, k, count, p.n_kv_heads, "k")
+    v_at, v_stride = _heads(p, v, count, p.n_kv_heads, "v")
+    if k_stride != v_stride:
+        raise ValueError("k and v: rows %d and %d values apart" % (k_stride, v_stride))
+    if n_q_heads > 0:
+        q_at, q_stride = _heads(p, q, count, n_q_heads, "q")
+        o_at, o_stride = _heads(p, q_out, count, n_q_heads, "q_out")
+    else:
+        q_at = o_at = None
+        q_stride = o_stride = 0
+    if q_gain is not None or k_gain is not None:
+        import torch
+        q_gain, k_gain = (_at(p, x, torch.bfloat16, p.head_dim, name) for x, name in ((q_gain, "q_gain"), (k_gain, "k_gain")))
+    return _call(p, "vlac_pages_append_rotated", stream, check, _ref(p), layer, _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n,
+                 tokens, _ref(rot), _list(p, places, count, "places"), n_q_heads, q_at, q_stride, k_at, v_at, k_stride, o_at, o_stride,
+                 q_gain, k_gain, eps)
+
+
+def vlac_attend_tree_workspace_bytes(p, n, tokens, n_q_heads):
+    return int(lib().vlac_attend_tree_workspace_bytes(_ref(p), n, tokens, n_q_heads))
+
+
+def vlac_attend_tree_plan(p, seqs, pos, n, tokens, n_q_heads, group, parents, out_places, workspace, stream=None, check=True):
+    """parents, out_places: int32 [n, tokens]."""
+    ws, size = _workspace(p, workspace)
+    return _call(p, "vlac_attend_tree_plan", stream, check, _ref(p), _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n, tokens,
+                 n_q_heads, _list(p, group, n, "group"), _list(p, parents, n * tokens, "parents"),
+                 _list(p, out_places, n * tokens, "out_places"), ws, size)
+
+
+def vlac_attend_tree(p, layer, n, tokens, n_q_heads, q, out, workspace, stream=None, check=True):
+    """q: [n, tokens, n_q_heads, head_dim] of the pool's type, rows equally far apart; out the same, contiguous."""
+    count, width = n * tokens, n_q_heads * p.head_dim
+    q_at, q_stride = _rows(p, q, count, width, "q")
+    ws, size = _workspace(p, workspace)
+    return _call(p, "vlac_attend_tree", stream, check, _ref(p), layer, n, tokens, n_q_heads, q_at, q_stride,
+                 _at(p, out, p.rows_dtype or _rows_dtype(p), count * width, "out"), ws, size)
+
+
+def token_rules(repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, history=None, history_len=None, parents=None,
+                drafted=None):
+    """The vlac_token_rules over GPU tensors: bias fp32 [vocab] or [rows, vocab], allowed int32 (32 tokens a word) [words] or
+    [rows, words], history int32 [n, most], history_len int32 [n], parents and drafted int32 [n, tokens]."""
+    import torch
+    r = TokenRules(repetition, presence, frequency)
+    r.tensors = (bias, allowed, history, history_len, parents, drafted)
+    g = _gpu_of(*r.tensors)
+    r.index = g.index if g is not None else -1
+    i32 = torch.int32
+
+    def of_rows(x, dtype, name):   # one row for all, or one each
+        if x.dim() not in (1, 2):
+            raise ValueError("%s: one row, or one for each row of the logits" % name)
+        if x.dim() == 2:
+            if r.rows is not None and r.rows != x.shape[0]:
+                raise ValueError("%s: %d rows, other rules have %d" % (name, x.shape[0], r.rows))
+            r.rows = x.shape[0]
+        return _at(g, x, dtype, 0, name), (x.shape[1] if x.dim() == 2 else 0), x.shape[-1]
+
+    def of_entries(x, name, dim):
+        if x.dim() != dim:
+            raise ValueError("%s: %d dimensions, expected %d" % (name, x.dim(), dim))
+        if r.entries is not None and r.entries != x.shape[0]:
+            raise ValueError("%s: %d entries, other rules have %d" % (name, x.shape[0], r.entries))
+        r.entries = x.shape[0]
+        return _at(g, x, i32, 0, name)
+
+    if bias is not None:
+        r.bias, r.bias_stride, r.vocab = of_rows(bias, torch.float32, "bias")
+    if allowed is not None:
+        if allowed.dtype == getattr(torch, "uint32", None):
+            allowed = allowed.view(i32)
+        r.allowed, r.allowed_stride, r.words = of_rows(allowed, i32, "allowed")
+    if (history is None) != (history_len is None) or (parents is None) != (drafted is None):
+        raise ValueError("history and history_len, and parents and drafted, come together")
+    if history is not None:
+        r.history, r.history_len, r.history_stride = of_entries(history, "history", 2), of_entries(history_len, "history_len", 1), history.shape[1]
+    r.tokens = 1
+    if parents is not None:
+        if parents.shape != drafted.shape:
+            raise ValueError("parents and drafted differ in shape")
+        r.parents, r.drafted, r.tokens = of_entries(parents, "parents", 2), of_entries(drafted, "drafted", 2), parents.shape[1]
+    r.ref = C.byref(r)
+    return r
+
+
+def _fits(rules, rows, vocab, entries):
+    """Whether the rules' tensors are those of so many rows of logits."""
+    if rules.vocab is not None and rules.vocab != vocab:
+        raise ValueError("bias holds %d tokens, the vocabulary has %d" % (rules.vocab, vocab))
+    if rules.words is not None and rules.words != -(-vocab // 32):
+        raise ValueError("allowed holds %d words a row, %d are needed" % (rules.words, -(-vocab // 32)))
+    if rules.rows is not None and rules.rows != rows:
+        raise ValueError("the rules are for %d rows, not %d" % (rules.rows, rows))
+    if rules.entries is not None and rules.entries != entries:
+        raise ValueError("the rules are for %d entries, not %d" % (rules.entries, entries))
+
+
+def vlac_choose_workspace_bytes(rows, vocab):
+    return int(lib().vlac_choose_workspace_bytes(rows, vocab))
+
+
+def _matrix(g, x, name):
+    """Address and row stride of an fp32 matrix with dense rows."""
+    if x is None:
+        return None, 0
+    import torch
+    if x.dtype is not torch.float32:
+        raise TypeError("%s: dtype %s, expected %s" % (name, x.dtype, torch.float32))
+    if x.get_device() != g.index:
+        raise ValueError("%s lies on %s, the logits on GPU %d" % (name, x.device, g.index))
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("%s: a matrix with dense rows" % name)
+    return x.data_ptr(), (x.stride(0) if x.shape[0] > 1 else x.shape[1])
+
+
+def vlac_choose_tokens(logits, rules, out_logits, out_token, workspace, stream=None, check=True):
+    """logits, out_logits: fp32 [rows, vocab], rows dense; out_token: int32 [rows]; out_logits may be logits, either may be None."""
+    g = _gpu_of(logits)
+    rows, vocab = logits.shape
+    at, stride = _matrix(g, logits, "logits")
+    o_at, o_stride = _matrix(g, out_logits, "out_logits")
+    if out_logits is not None and out_logits.shape != logits.shape:
+        raise ValueError("out_logits and logits differ in shape")
+    if rules is not None and rules.index >= 0:
+        if rules.index != g.index:
+            raise ValueError("the rules lie on GPU %d, the logits on GPU %d" % (rules.index, g.index))
+        _fits(rules, rows, vocab, rows // max(rules.tokens, 1))
+    ws, size = _workspace(g, workspace)
+    return _call(g, "vlac_choose_tokens", stream, check, at, rows, vocab, stride, _ref(rules), o_at, o_stride,
+                 _list(g, out_token, rows, "out_token"), ws, size)
+
+
+def vlac_tree_accept(parents, drafted, chosen, n, tokens, out_path, out_count, out_token, stream=None, check=True):
+    """parents, drafted, chosen, out_path: int32 [n, tokens]; out_count, out_token: int32 [n]."""
+    g, i32 = _gpu_of(parents, drafted, chosen, out_path, out_count, out_token), _I32 or _int32()
+    args = [_on(g, x, i32, n * tokens, name) for x, name in ((parents, "parents"), (drafted, "drafted"), (chosen, "chosen"))]
+    return _call(g, "vlac_tree_accept", stream, check, *args, n, tokens, _on(g, out_path, i32, n * tokens, "out_path"),
+                 _on(g, out_count, i32, n, "out_count"), _on(g, out_token, i32, n, "out_token"))
+
+
+def vlac_pages_keep(p, seqs, pos, n, tokens, path, count, stream=None, check=True):
+    """path: int32 [n, tokens]; count: int32 [n]."""
+    return _call(p, "vlac_pages_keep", stream, check, _ref(p), _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n, tokens,
+                 _list(p, path, n * tokens, "path"), _list(p, count, n, "count"))
+
+
+def vlac_guided_workspace_bytes(ctx, p, n):
+    return int(lib().vlac_guided_workspace_bytes(ctx, _ref(p), n))
+
+
+def vlac_decode_guided(ctx, p, seqs, n, L, group, n_new, first_token, rules, out_tokens, out_logits, workspace, stream=None, check=True):
+    """vlac_decode_candidates under rules: row i * n_new + t of the rules is candidate i's t-th choice."""
+    import torch
+    ws, size = _workspace(p, workspace)
+    vocab = _SIZES.get(ctx, (0, 0))[0]
+    if rules is not None and rules.index >= 0:
+        if rules.index != p.index >= 0:
+            raise ValueError("the rules lie on GPU %d, the pool on GPU %d" % (rules.index, p.index))
+        if vocab:
+            _fits(rules, n * n_new, vocab, n)
+    return _call(p, "vlac_decode_guided", stream, check, ctx, _ref(p), _list(p, seqs, n, "seqs"), n, L, _list(p, group, n, "group"), n_new,
+                 _list(p, first_token, n, "first_token"), _ref(rules), _list(p, out_tokens, n * n_new, "out_tokens"),
+                 _at(p, out_logits, torch.float32, n * n_new * vocab, "out_logits"), ws, size)

@@ -8,6 +8,7 @@
 #include <new>
 
 #include "common.h"
+#include "choose.h"
 #include "pages.h"
 
 namespace {
@@ -664,10 +665,11 @@ void run_layer_decode(vlac_ctx* c, int layer, int B, int pos, bf16_t* kv, Decode
   r.pending = s_d > 1 ? s_d : 0;
 }
 
-// Final norm + output head + greedy token for B rows: (stream b, position pos) of the
+// Final norm + output head + greedy token (under `rules`, if given: the logits are changed in place) for B rows: (stream b, position pos) of the
 // residual stream, or, with `fused` given, the rows of a decode pass (norm fused).
 void run_head(vlac_ctx* c, int B, int pos, float* logits, size_t logits_stride, int32_t* out_token,
-              int out_stride, const NextEmbed& next, hipStream_t st, const NormIn* fused = nullptr) {
+              int out_stride, const NextEmbed& next, hipStream_t st, const NormIn* fused = nullptr,
+              const ChooseArgs* rules = nullptr) {
   const vlac_model_cfg& m = c->cfg;
   GemmEpi e;
   memset(&e, 0, sizeof(e));
@@ -686,12 +688,20 @@ void run_head(vlac_ctx* c, int B, int pos, float* logits, size_t logits_stride, 
                         m.d_model, c->xa, c->kpad_d / 16, st);
     launch_gemm(c, EPI_LOGITS, c->w_head, c->s_head, m.vocab / 32, c->kpad_d, c->xa, nullptr, B, B, e, st);
   }
+  if (rules) {
+    ChooseArgs a = *rules;
+    a.logits = a.out = logits; a.stride = a.out_stride = (long long)logits_stride;
+    a.token = out_token; a.token_stride = out_stride;
+    launch_choose(a, st);
+    if (next.h) launch_embed_rows(next.embed, out_token, B, m.d_model, m.vocab, next.h, next.h_seq, next.h_pos, st, out_stride);
+    return;
+  }
   launch_argmax(c->head_best, B, m.vocab, out_token, out_stride, next, st);
 }
 
 // n_new decode passes over B rows at positions L, L + 1, ...: streams of the cache, or sequences of a pool
 void decode_passes(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_token, bf16_t* kv, int32_t* out_tokens,
-                   float* out_logits, PagePath* pg, hipStream_t st, const int* group = nullptr) {
+                   float* out_logits, PagePath* pg, hipStream_t st, const int* group = nullptr, ChooseArgs* rules = nullptr) {
   const vlac_model_cfg& m = ctx->cfg;
   const int ms = m.max_seq;
   const bool fused = gemm_can_fuse_norm(B, L, ctx->kpad_d) && ctx->rpart_floats >= (size_t)8 * B * m.d_model;
@@ -701,6 +711,10 @@ void decode_passes(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_
     const size_t lstride = out_logits ? (size_t)n_new * m.vocab : (size_t)m.vocab;
     // (the residual rows of every later pass are written by the argmax of the pass before it)
     const bool more = t + 1 < n_new;
+    if (rules) {  // (the tokens chosen so far belong to the text)
+      rules->more_n = t;
+      rules->rule_row0 = t;
+    }
     if (pg) {
       pg->add = t;
       launch_attend_plan(pg->p, pg->seqs, pg->pos, t, B, 1, m.n_q_heads, group, pg->ws, st);
@@ -713,7 +727,7 @@ void decode_passes(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_
       for (int l = 0; l < m.n_layers; ++l)
         run_layer_decode(ctx, l, B, L + t, kv, r, st, pg);
       const NormIn n = decode_norm(ctx, B, r, ctx->g_final, false);
-      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st, &n);
+      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st, &n, rules);
     } else {
       // More than 4 streams: the general layer pass over the rows (b, L + t).  With more than
       // 32 of them the prefill's GEMM and row kernels serve the pass, and those read the row
@@ -732,7 +746,7 @@ void decode_passes(vlac_ctx* ctx, int B, int L, int n_new, const int32_t* first_
         launch_resid_norm_rows(ctx->f16, ctx->h, ms, ctx->rpart, pending, B, ctx->h, ms, drows, nullptr,
                                nullptr, B, B, nullptr, m.rms_eps, m.d_model, ctx->xa, ctx->kpad_d / 16,
                                st, &ctx->pending_adapt);
-      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st);
+      run_head(ctx, B, L + t, logits, lstride, out_tokens + t, n_new, next, st, nullptr, rules);
     }
   }
 }
@@ -834,30 +848,61 @@ size_t vlac_candidates_workspace_bytes(const vlac_ctx* ctx, const vlac_pages* pa
   return att ? candidates_pos_bytes(n) + candidates_tile_bytes(ctx, n) + att : 0;
 }
 
-int vlac_decode_candidates(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L,
-                           const int32_t* group, int n_new, const int32_t* first_token, int32_t* out_tokens,
-                           float* out_logits, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!ctx) return VLAC_E_NULL;
-  const int rc = check_pages(pages, true);
-  if (rc != VLAC_OK) return rc;
+static int decode_pages(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L, const int32_t* group, int n_new,
+                        const int32_t* first_token, const vlac_token_rules* rules, int32_t* out_tokens, float* out_logits,
+                        void* workspace, size_t workspace_bytes, void* stream) {
   const vlac_model_cfg& m = ctx->cfg;
   if (n < 0 || n > m.max_batch || n > VLAC_PAGES_MAX_LIST || L < 1 || n_new < 0) return VLAC_E_RANGE;
   if (!pool_fits(ctx, pages) || (long)L + n_new > m.max_seq || (long)L + n_new > (long)pages->max_pages * kPage) return VLAC_E_SHAPE;
   if (n == 0 || n_new == 0) return VLAC_OK;
   if (!seqs || !first_token || !out_tokens || !workspace) return VLAC_E_NULL;
   if ((uintptr_t)workspace % 16) return VLAC_E_SHAPE;
-  const size_t need = vlac_candidates_workspace_bytes(ctx, pages, n);
-  if (need == 0 || workspace_bytes < need) return VLAC_E_RANGE;
+  const size_t need = vlac_candidates_workspace_bytes(ctx, pages, n), more = rules ? choose_workspace(n, m.vocab) : 0;
+  if (need == 0 || workspace_bytes < need + more) return VLAC_E_RANGE;
   if (!weights_ready(ctx)) return VLAC_E_STATE;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
   int* pos = (int*)ws;
   PagePath pg = {pool_view(pages), seqs, pos, 0, n, (bf16_t*)(ws + candidates_pos_bytes(n)),
                  ws + candidates_pos_bytes(n) + candidates_tile_bytes(ctx, n)};
+  ChooseArgs choose;
+  if (rules) {
+    choose = choose_args(nullptr, n, m.vocab, 0, *rules, nullptr, 0, nullptr, ws + need);
+    choose.rule_rows = n_new;
+    choose.more = out_tokens; choose.more_stride = n_new;
+    choose.one = first_token;
+  }
   launch_extend(pg.p, seqs, n, n_new, L, pos, st);
-  decode_passes(ctx, n, L, n_new, first_token, nullptr, out_tokens, out_logits, &pg, st, group);
+  decode_passes(ctx, n, L, n_new, first_token, nullptr, out_tokens, out_logits, &pg, st, group, rules ? &choose : nullptr);
   VLAC_HIP(hipGetLastError());
   return VLAC_OK;
+}
+
+int vlac_decode_candidates(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L,
+                           const int32_t* group, int n_new, const int32_t* first_token, int32_t* out_tokens,
+                           float* out_logits, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!ctx) return VLAC_E_NULL;
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  return decode_pages(ctx, pages, seqs, n, L, group, n_new, first_token, nullptr, out_tokens, out_logits, workspace, workspace_bytes,
+                      stream);
+}
+
+size_t vlac_guided_workspace_bytes(const vlac_ctx* ctx, const vlac_pages* pages, int n) {
+  const size_t bytes = vlac_candidates_workspace_bytes(ctx, pages, n);
+  return bytes ? bytes + choose_workspace(n, ctx->cfg.vocab) : 0;
+}
+
+int vlac_decode_guided(vlac_ctx* ctx, const vlac_pages* pages, const int32_t* seqs, int n, int L, const int32_t* group, int n_new,
+                       const int32_t* first_token, const vlac_token_rules* rules, int32_t* out_tokens, float* out_logits,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  if (!ctx) return VLAC_E_NULL;
+  int rc = check_pages(pages, true);
+  if (rc == VLAC_OK) rc = check_rules(rules, ctx->cfg.vocab);
+  if (rc != VLAC_OK) return rc;
+  if (rules->tokens != 1 || rules->parents) return VLAC_E_SHAPE;
+  return decode_pages(ctx, pages, seqs, n, L, group, n_new, first_token, rules, out_tokens, out_logits, workspace, workspace_bytes,
+                      stream);
 }
 
 }  // extern "C"

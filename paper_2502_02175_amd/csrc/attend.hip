@@ -63,13 +63,17 @@ __device__ inline Item load_item(const Item* at) {
 }
 
 struct Layout {
-  size_t ent, own, item, ml, o, total;
+  size_t ent, own, item, ml, o, mask, total;
   size_t max_items;
   int part_tiles;
   bool parts;  // there may be parts to join
   bool few;    // blocks of up to 16 columns
 };
-inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
+// Words of a tree node's mask: bit b of word x says whether the node sees position 32 (pos / 32 + x) + b; its slots may
+// begin at the last position of a page.
+__host__ __device__ inline int mask_words(int tokens) { return (tokens + 62) / 32; }
+
+inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads, bool tree) {
   Layout l;
   const size_t cols = (size_t)n * tokens * (n_q_heads / p.n_kv_heads);  // per kv head
   const size_t least = (cols + 31) / 32 * p.n_kv_heads;
@@ -93,16 +97,17 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads) {
   l.item = l.own + up(sizeof(Own) * n * p.max_pages);
   l.ml = l.item + up(sizeof(Item) * l.max_items);
   l.o = l.ml + (size_t)l.part_tiles * 64 * sizeof(float2);
-  l.total = l.o + (size_t)l.part_tiles * 32 * p.head_dim * sizeof(float);
+  l.mask = l.o + (size_t)l.part_tiles * 32 * p.head_dim * sizeof(float);
+  l.total = l.mask + (tree ? up((size_t)n * tokens * mask_words(tokens) * sizeof(uint32_t)) : 0);
   return l;
 }
 
 // What a plan was made for, behind the number of items in the workspace: a workspace that holds another plan, or none, is
 // not read any further.
 struct Made { int v[15]; };
-inline Made made_for(const PoolView& p, int n, int tokens, int n_q_heads) {
+inline Made made_for(const PoolView& p, int n, int tokens, int n_q_heads, bool tree) {
   const uint64_t d = (uint64_t)(uintptr_t)p.data, t = (uint64_t)(uintptr_t)p.table;
-  return {{0x564c4150, n, tokens, n_q_heads, p.n_layers, p.n_kv_heads, p.head_dim, p.n_pages, p.max_seqs, p.max_pages, (int)d,
+  return {{0x564c4150 + tree, n, tokens, n_q_heads, p.n_layers, p.n_kv_heads, p.head_dim, p.n_pages, p.max_seqs, p.max_pages, (int)d,
            (int)(d >> 32), (int)t, (int)(t >> 32), kWaves}};
 }
 __device__ inline int differs(const int* head, const Made& m) {
@@ -499,7 +504,19 @@ struct AttendArgs {
   int kc_out;
   int layer, n, tokens, n_q_heads;
   float scale_log2e;
+  const uint32_t* mask;  // trees: [n][tokens][mask_words]
 };
+
+// Which positions of tile kt a tree's node sees, for a query row whose entry's new positions begin at pos
+__device__ inline uint32_t sees(const AttendArgs& a, int row, int pos, int kt) {
+  const int x = kt - pos / kPage;
+  return x < 0 ? ~0u : a.mask[(size_t)row * mask_words(a.tokens) + x];
+}
+// ... and whether there is such a node: it sees itself
+__device__ inline bool is_there(const AttendArgs& a, int row, int pos) {
+  const int self = pos % kPage + row % a.tokens;
+  return a.mask[(size_t)row * mask_words(a.tokens) + self / kPage] >> (self & 31) & 1;
+}
 
 template <bool F16>
 __device__ inline uint32_t pack2(float lo, float hi) {
@@ -559,8 +576,8 @@ __device__ inline void store_out(const AttendArgs& a, int row, int f, const floa
 template <int HD>
 __device__ inline int feature_of(int h, int quad, int g) { return h * HD + 32 * (quad >> 2) + 8 * (quad & 3) + 4 * g; }
 
-template <int HD, bool F16>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
+template <int HD, bool F16, bool TREE>
+__device__ __forceinline__ void attend_columns(const AttendArgs& a) {
   constexpr int NC = HD / 16, NI = HD / 32, REGS = NI * 16;
   __shared__ float park[kWaves][2 + REGS][64];
   const PoolView& p = a.p;
@@ -596,7 +613,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     const int h = hk * grp + ci - ti * grp;
     const Ent mine = a.ent[e0 + ei];
     const int last = mine.pos + ti;  // its last visible position
-    const bool valid = c < cols_end && mine.seq >= 0;
+    const bool valid = c < cols_end && mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos));
     uint4 qf[NC];
     {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)NC * 512 + (size_t)(((row & 31) + 32 * g) << 3)
@@ -729,9 +746,15 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
           load_k(now);
           __builtin_amdgcn_sched_barrier(0);
           if (own) {
-            const int see = ei == what >> 16 ? last - 32 * kt - 4 * g : -1;
+            if constexpr (TREE) {
+              const uint32_t see = ei == what >> 16 ? sees(a, row, mine.pos, kt) >> (4 * g) : 0u;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+              for (int x = 0; x < 16; ++x) s[x] = see >> (8 * (x >> 2) + (x & 3)) & 1 ? s[x] : -INFINITY;
+            } else {
+              const int see = ei == what >> 16 ? last - 32 * kt - 4 * g : -1;
+#pragma unroll
+              for (int x = 0; x < 16; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+            }
           }
           uint4 pb[2];
           weigh(s, pb);
@@ -771,7 +794,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
         const int at64 = (i - n_shared) & 63;
         if (at64 == 0) load_steps(i);
         const int what = __builtin_amdgcn_readlane(st_what, at64), kt = what & 0xffff, held = __builtin_amdgcn_readlane(st_page, at64) >> 24;
-        const int see = ei == what >> 16 ? last - 32 * kt : -1;  // this column's last key of the tile
+        // the keys of the tile that this column sees: those up to `see`, or the bits of `sees_of`
+        const int see = ei == what >> 16 ? last - 32 * kt : -1;
+        uint32_t sees_of = 0u;
+        if constexpr (TREE) sees_of = ei == what >> 16 ? sees(a, row, mine.pos, kt) : 0u;
+        auto seen = [&](int key) { return TREE ? (sees_of >> key & 1) != 0 : key <= see; };
         const bf16_t* at = tile_of(at64);
         load_k(at);
         f32x16 s;
@@ -781,7 +808,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
         for (int x = 0; x < NC; ++x) s = mfma32<F16>(kf[x], qf[x], s);
 #pragma unroll
         for (int x = 0; x < 16; ++x)
-          s[x] = 8 * (x >> 2) + 4 * g + (x & 3) <= see ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
+          s[x] = seen(8 * (x >> 2) + 4 * g + (x & 3)) ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const uint4 pb = {pack2<F16>(s[8 * t], s[8 * t + 1]), pack2<F16>(s[8 * t + 2], s[8 * t + 3]),
@@ -802,7 +829,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
               for (int r = 0; r < 16; ++r) z[r] = 0.f;
               z = mfma32<F16>(only, pb, z);
 #pragma unroll
-              for (int r = 0; r < 16; ++r) o[ib][r] += 16 * t + k <= see ? z[r] : 0.f;
+              for (int r = 0; r < 16; ++r) o[ib][r] += seen(16 * t + k) ? z[r] : 0.f;
             }
           }
         }
@@ -855,13 +882,18 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   }
 }
 
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) { attend_columns<HD, F16, false>(a); }
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_tree_kernel(AttendArgs a) { attend_columns<HD, F16, true>(a); }
+
 // The same for short lists of blocks of up to 16 columns, no parts: products of 16 x 16 x 32, half the registers per column
 // block, and so two tiles at a time per wave.  A row of K is the key that the second product wants there: the row m = 4 * q + e of
 // product rb is key 16 * (q >> 1) + 8 * rb + 4 * (q & 1) + e, so that the 8 scores of a lane are, in order, the 8 weights that it owes
 // as the second operand, for the 16 bytes of V that lie together in the page.  Bound by latency, then by what a CU fetches: one
 // token of 8 candidates over 288 positions, 32 heads of 128, 6.8 us; 2 groups of up to 8 x 8 tokens over 601 (36 MB) 11.6.
-template <int HD, bool F16>
-__global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
+template <int HD, bool F16, bool TREE>
+__device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
   constexpr int NB = HD / 32, NF = HD / 16, U = 2;
   __shared__ float park[kWaves][2 + 4 * NF][64];
   const PoolView& p = a.p;
@@ -892,7 +924,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
     const int h = hk * grp + ci - ti * grp;
     const Ent mine = a.ent[e0 + ei];
     const int last = mine.pos + ti;  // its last visible position
-    const bool valid = c < cols_end && mine.seq >= 0;
+    const bool valid = c < cols_end && mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos));
     uint4 qf[NB];
     {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)(HD / 16) * 512 + (size_t)((row & 31) << 3) + half
@@ -983,9 +1015,15 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
             float s[8];
             scores(kf[u], s);
             if (own) {
-              const int see = ei == what >> 16 ? last - 32 * kt - first_key : -1;
+              if constexpr (TREE) {
+                const uint32_t see = ei == what >> 16 ? sees(a, row, mine.pos, kt) >> first_key : 0u;
 #pragma unroll
-              for (int x = 0; x < 8; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+                for (int x = 0; x < 8; ++x) s[x] = see >> (8 * (x >> 2) + (x & 3)) & 1 ? s[x] : -INFINITY;
+              } else {
+                const int see = ei == what >> 16 ? last - 32 * kt - first_key : -1;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+              }
             }
             // (the reference point as above)
             float tmax = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
@@ -1045,7 +1083,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
         const int at64 = (i - n_shared) & 63;
         if (at64 == 0) load_steps(i);
         const int what = __builtin_amdgcn_readlane(st_what, at64), kt = what & 0xffff, held = __builtin_amdgcn_readlane(st_page, at64) >> 24;
-        const int see = ei == what >> 16 ? last - 32 * kt : -1;  // this column's last key of the tile
+        const int see = ei == what >> 16 ? last - 32 * kt : -1;  // (as above)
+        uint32_t sees_of = 0u;
+        if constexpr (TREE) sees_of = ei == what >> 16 ? sees(a, row, mine.pos, kt) : 0u;
+        auto seen = [&](int key) { return TREE ? (sees_of >> key & 1) != 0 : key <= see; };
         const bf16_t* at = tile_of(at64);
         uint4 kf[2 * NB];
         load_k(kf, at);
@@ -1053,7 +1094,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
         scores(kf, s);
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-          s[x] = first_key + 8 * (x >> 2) + (x & 3) <= see ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
+          s[x] = seen(first_key + 8 * (x >> 2) + (x & 3)) ? __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, m == -INFINITY ? 0.f : -m)) : 0.f;
         const uint4 pb = weights(s);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
@@ -1068,7 +1109,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
               y[d] = here && d == 2 * (k >> 3 & 1) + (k >> 1 & 1) ? x[d] & far_values<F16>(x[d], !(k & 1), k & 1) : 0u;
             const f32x4v z = mfma16<F16>(only, pb, f32x4v{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[f][e] += k <= see ? z[e] : 0.f;
+            for (int e = 0; e < 4; ++e) o[f][e] += seen(k) ? z[e] : 0.f;
           }
         }
       }
@@ -1102,10 +1143,15 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) {
   }
 }
 
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_few_kernel(AttendArgs a) { attend_few_columns<HD, F16, false>(a); }
+template <int HD, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void attend_tree_few_kernel(AttendArgs a) { attend_few_columns<HD, F16, true>(a); }
+
 // Joins the parts.  The items of a (head, column blocks) deal its sums among themselves: a wave takes four sums of a block's
 // lanes, over all parts.
-template <int HD, bool F16>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+template <int HD, bool F16, bool TREE>
+__device__ __forceinline__ void join_parts(const AttendArgs& a) {
   constexpr int QUADS = HD / 8;
   const PoolView& p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
@@ -1154,7 +1200,55 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
       const int ei = c / per_entry, ci = c - ei * per_entry, ti = ci / grp;
       float y[4] = {x.x, x.y, x.z, x.w};
       averages<F16>(y, 1.f / L);
-      store_out<HD, F16>(a, (e0 + ei) * a.tokens + ti, feature_of<HD>(hk * grp + ci - ti * grp, quad, g), y, a.ent[e0 + ei].seq >= 0);
+      const int row = (e0 + ei) * a.tokens + ti;
+      const Ent mine = a.ent[e0 + ei];
+      store_out<HD, F16>(a, row, feature_of<HD>(hk * grp + ci - ti * grp, quad, g), y, mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos)));
+    }
+  }
+}
+
+template <int HD, bool F16>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) { join_parts<HD, F16, false>(a); }
+template <int HD, bool F16>
+__global__ __launch_bounds__(256) void attend_tree_join_kernel(AttendArgs a) { join_parts<HD, F16, true>(a); }
+
+// The masks of a tree's nodes, and their places in the text.  A workgroup takes an entry: the parents lie in LDS and every node
+// follows them up, twice: to see whether the way ends at the cached sequence, then, word by word (parents come before
+// their nodes, so the bits are met in descending order).  Bound by latency: the list, then depth x an LDS round trip.
+__global__ __launch_bounds__(256) void attend_tree_mask_kernel(PoolView p, const int* __restrict__ seqs, const int* __restrict__ pos,
+                                                             const int* __restrict__ parents, int tokens, uint32_t* __restrict__ mask,
+                                                             int* __restrict__ out_places) {
+  __shared__ int above[VLAC_TREE_MAX_NODES];
+  const int i = blockIdx.x, tid = threadIdx.x, words = mask_words(tokens);
+  const int p0 = pos[i], l = checked_len(p, seqs[i]);
+  const bool fits = p0 >= 0 && l >= 0 && (long long)p0 + tokens <= l;
+  for (int t = tid; t < tokens; t += 256) {
+    const int x = parents[(size_t)i * tokens + t];
+    if (fits && (x < -2 || x >= t)) report(p, PAGES_BAD_ENTRY);
+    above[t] = x < -2 || x >= t ? -2 : x;
+  }
+  __syncthreads();
+  const int first = fits ? p0 % kPage : 0;  // bit of node 0
+  for (int t = tid; t < tokens; t += 256) {
+    const size_t row = (size_t)i * tokens + t;
+    int depth = 0, x = t, up = above[t];
+    while (up >= 0) {
+      ++depth;
+      x = up;
+      up = above[x];
+    }
+    const bool there = fits && up == -1;
+    if (out_places) out_places[row] = there ? p0 + depth : -1;
+    uint32_t* const out = mask + row * words;
+    x = there ? t : -1;
+    for (int k = words - 1; k >= 0; --k) {
+      uint32_t bits = 0u;
+      while (x >= 0 && (first + x) / 32 == k) {
+        bits |= 1u << ((first + x) & 31);
+        x = above[x];
+      }
+      if (k == 0 && there) bits |= (1u << first) - 1u;  // cached positions of the same page
+      out[k] = bits;
     }
   }
 }
@@ -1164,28 +1258,29 @@ bool sizes_ok(const vlac_pages* p, int n, int tokens, int n_q_heads) {
          n_q_heads <= 1024 && n_q_heads >= p->n_kv_heads && n_q_heads % p->n_kv_heads == 0;
 }
 
-int check_attend(const vlac_pages* pages, int n, int tokens, int n_q_heads, const void* ws, size_t ws_bytes) {
+int check_attend(const vlac_pages* pages, int n, int tokens, int n_q_heads, const void* ws, size_t ws_bytes, bool tree = false) {
   const int rc = check_pages(pages, true);
   if (rc != VLAC_OK) return rc;
+  if (tree && tokens > VLAC_TREE_MAX_NODES) return VLAC_E_RANGE;
   if (!sizes_ok(pages, n, tokens, n_q_heads)) return n_q_heads >= 1 && n_q_heads % pages->n_kv_heads ? VLAC_E_SHAPE : VLAC_E_RANGE;
   if (n == 0) return VLAC_OK;
   if (!ws) return VLAC_E_NULL;
   if ((uintptr_t)ws % 16) return VLAC_E_SHAPE;
-  const size_t need = attend_workspace(pool_view(pages), n, tokens, n_q_heads);
+  const size_t need = layout_of(pool_view(pages), n, tokens, n_q_heads, tree).total;
   return need == 0 || ws_bytes < need ? VLAC_E_RANGE : VLAC_OK;
 }
 
 }  // namespace
 
 size_t attend_workspace(const PoolView& p, int n, int tokens, int n_q_heads) {
-  return layout_of(p, n > 0 ? n : 1, tokens, n_q_heads).total;
+  return layout_of(p, n > 0 ? n : 1, tokens, n_q_heads, false).total;
 }
 
-void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
-                        const int* group, void* ws, hipStream_t st) {
-  const Layout l = layout_of(p, n, tokens, n_q_heads);
+static void launch_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
+                        const int* group, void* ws, bool tree, hipStream_t st) {
+  const Layout l = layout_of(p, n, tokens, n_q_heads, tree);
   char* b = (char*)ws;
-  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles,
+  const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads, tree), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles,
                       (int)l.max_items, l.few ? 16 : 32, (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
   // (4 waves or 16: one token of 2 candidates 7.3 and 8.2 us, 16 candidates x 56 tokens over 1057 positions 8.0 and 8.6; 48
   // candidates with tables of 1027 pages 40 and 20 when both were tried.  More entries than 128 are a second round for 4 waves.)
@@ -1195,27 +1290,58 @@ void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int 
     hipLaunchKernelGGL((attend_plan_kernel<1024, VLAC_PAGES_MAX_LIST>), dim3(1), dim3(1024), 0, st, a);
 }
 
-void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, int n_q_heads, const AttendIo& io, void* ws,
-                   hipStream_t st) {
-  const Layout l = layout_of(p, n, tokens, n_q_heads);
+void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
+                        const int* group, void* ws, hipStream_t st) {
+  launch_plan(p, seqs, pos, add, n, tokens, n_q_heads, group, ws, false, st);
+}
+
+static void launch_layer(const PoolView& p, bool f16, int layer, int n, int tokens, int n_q_heads, const AttendIo& io, void* ws,
+                         bool tree, hipStream_t st) {
+  const Layout l = layout_of(p, n, tokens, n_q_heads, tree);
   char* b = (char*)ws;
-  const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own),
+  const AttendArgs a = {p, made_for(p, n, tokens, n_q_heads, tree), (const int*)b, (const Ent*)(b + l.ent), (const Own*)(b + l.own),
                         (const Item*)(b + l.item),
                         (float2*)(b + l.ml), (float4*)(b + l.o), io.q, io.q_stride, io.out, io.kc_out, layer, n, tokens,
-                        n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim)};
+                        n_q_heads, 1.4426950408889634f / sqrtf((float)p.head_dim), (const uint32_t*)(b + l.mask)};
   const dim3 grid((unsigned)std::min<size_t>(l.max_items, kCus)), join((unsigned)std::min<size_t>(l.max_items, 4 * kCus));
-#define VLAC_ATTEND(HD_, F16_)                                                                        \
-  {                                                                                                   \
-    if (l.few) hipLaunchKernelGGL((attend_few_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a); \
-    else hipLaunchKernelGGL((attend_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);           \
-    if (l.parts) hipLaunchKernelGGL((attend_join_kernel<HD_, F16_>), join, dim3(256), 0, st, a);      \
+#define VLAC_ATTEND(HD_, F16_, TREE_)                                                                         \
+  {                                                                                                           \
+    if (l.few) hipLaunchKernelGGL((attend_##TREE_##few_kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a); \
+    else hipLaunchKernelGGL((attend_##TREE_##kernel<HD_, F16_>), grid, dim3(64 * kWaves), 0, st, a);           \
+    if (l.parts) hipLaunchKernelGGL((attend_##TREE_##join_kernel<HD_, F16_>), join, dim3(256), 0, st, a);      \
   }
-  if (p.head_dim == 128) {
-    if (f16) VLAC_ATTEND(128, true) else VLAC_ATTEND(128, false)
-  } else {
-    if (f16) VLAC_ATTEND(64, true) else VLAC_ATTEND(64, false)
+#define VLAC_ATTEND_TYPES(TREE_)                                                \
+  {                                                                             \
+    if (p.head_dim == 128) {                                                    \
+      if (f16) VLAC_ATTEND(128, true, TREE_) else VLAC_ATTEND(128, false, TREE_) \
+    } else {                                                                    \
+      if (f16) VLAC_ATTEND(64, true, TREE_) else VLAC_ATTEND(64, false, TREE_)   \
+    }                                                                           \
   }
+  if (tree) VLAC_ATTEND_TYPES(tree_)
+  else VLAC_ATTEND_TYPES()
+#undef VLAC_ATTEND_TYPES
 #undef VLAC_ATTEND
+}
+
+void launch_attend(const PoolView& p, bool f16, int layer, int n, int tokens, int n_q_heads, const AttendIo& io, void* ws,
+                   hipStream_t st) {
+  launch_layer(p, f16, layer, n, tokens, n_q_heads, io, ws, false, st);
+}
+
+// One layer over a plan of either kind
+static int attend_layer(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q, int64_t q_stride, void* out,
+                        void* workspace, size_t workspace_bytes, bool tree, void* stream) {
+  const int rc = check_attend(pages, n, tokens, n_q_heads, workspace, workspace_bytes, tree);
+  if (rc != VLAC_OK) return rc;
+  if (layer < 0 || layer >= pages->n_layers) return VLAC_E_RANGE;
+  if (n == 0) return VLAC_OK;
+  if (!q || !out) return VLAC_E_NULL;
+  if (q_stride < (int64_t)n_q_heads * pages->head_dim || q_stride % 8 || q_stride > 1 << 30 || (uintptr_t)q % 16 || (uintptr_t)out % 8)
+    return VLAC_E_SHAPE;
+  const AttendIo io = {(const bf16_t*)q, q_stride, (bf16_t*)out, 0};
+  launch_layer(pool_view(pages), pages_f16(pages), layer, n, tokens, n_q_heads, io, workspace, tree, (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
 }
 
 extern "C" {
@@ -1236,16 +1362,31 @@ int vlac_attend_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t
 
 int vlac_attend_shared(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q, int64_t q_stride,
                        void* out, void* workspace, size_t workspace_bytes, void* stream) {
-  const int rc = check_attend(pages, n, tokens, n_q_heads, workspace, workspace_bytes);
-  if (rc != VLAC_OK) return rc;
-  if (layer < 0 || layer >= pages->n_layers) return VLAC_E_RANGE;
-  if (n == 0) return VLAC_OK;
-  if (!q || !out) return VLAC_E_NULL;
-  if (q_stride < (int64_t)n_q_heads * pages->head_dim || q_stride % 8 || q_stride > 1 << 30 || (uintptr_t)q % 16 || (uintptr_t)out % 8)
-    return VLAC_E_SHAPE;
-  const AttendIo io = {(const bf16_t*)q, q_stride, (bf16_t*)out, 0};
-  launch_attend(pool_view(pages), pages_f16(pages), layer, n, tokens, n_q_heads, io, workspace, (hipStream_t)stream);
+  return attend_layer(pages, layer, n, tokens, n_q_heads, q, q_stride, out, workspace, workspace_bytes, false, stream);
+}
+
+size_t vlac_attend_tree_workspace_bytes(const vlac_pages* pages, int n, int tokens, int n_q_heads) {
+  if (check_pages(pages, false) != VLAC_OK || !sizes_ok(pages, n, tokens, n_q_heads) || tokens > VLAC_TREE_MAX_NODES) return 0;
+  return layout_of(pool_view(pages), n > 0 ? n : 1, tokens, n_q_heads, true).total;
+}
+
+int vlac_attend_tree_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens, int n_q_heads,
+                          const int32_t* group, const int32_t* parents, int32_t* out_places, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  const int rc = check_attend(pages, n, tokens, n_q_heads, workspace, workspace_bytes, true);
+  if (rc != VLAC_OK || n == 0) return rc;
+  if (!seqs || !pos || !parents) return VLAC_E_NULL;
+  hipStream_t st = (hipStream_t)stream;
+  const PoolView p = pool_view(pages);
+  launch_plan(p, seqs, pos, 0, n, tokens, n_q_heads, group, workspace, true, st);
+  uint32_t* mask = (uint32_t*)((char*)workspace + layout_of(p, n, tokens, n_q_heads, true).mask);
+  hipLaunchKernelGGL(attend_tree_mask_kernel, dim3(n), dim3(256), 0, st, p, seqs, pos, parents, tokens, mask, out_places);
   return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
+}
+
+int vlac_attend_tree(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q, int64_t q_stride, void* out,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  return attend_layer(pages, layer, n, tokens, n_q_heads, q, q_stride, out, workspace, workspace_bytes, true, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,223 @@
+// What may be chosen, and at what price: the rules of vlac_token_rules over rows of logits, and the greatest of each row.
+//   l -> l > 0 ? l / repetition : l * repetition, - presence   where the row's text holds the token,
+//   l -> l - frequency * count, l -> l + bias, l -> -infinity where it is not allowed; every step rounded to fp32.
+// A workgroup takes a piece of a row: how often its text holds each token of the piece is counted in LDS (whole numbers, so
+// that the order of the atomics decides nothing), then the piece goes by once.  The greatest logits of the pieces meet in a
+// second launch.
+#include <algorithm>
+#include <cmath>
+
+#include "choose.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPiece = 8192;  // logits of a work item
+
+// The greatest of a row so far, and its token; what is not above -infinity (a NaN among it) is never taken
+struct Best { float v; int at; };
+__device__ inline void take(Best& b, float v, int at) {
+  if (v > b.v || (v == b.v && at < b.at)) { b.v = v; b.at = at; }
+}
+constexpr int kNobody = 0x7fffffff;
+
+// Over the workgroup, in every thread of the first wave
+__device__ inline Best best_of_all(Best b, float* sv, int* si) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float v = __shfl_xor(b.v, d);
+    const int i = __shfl_xor(b.at, d);
+    take(b, v, i);
+  }
+  if ((tid & 63) == 0) { sv[tid >> 6] = b.v; si[tid >> 6] = b.at; }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kThreads / 64; ++k) take(b, sv[k], si[k]);
+  return b;
+}
+
+// -infinity is the start of every search: equal values do not replace it, so a row of nothing but -infinity has no token
+__device__ inline int token_of(const Best& b) { return b.v > -INFINITY ? b.at : -1; }
+
+// A logit under the rules, every step rounded by itself (a multiply-add would round product and difference at once)
+__device__ inline float priced(float y, int n, float repetition, float presence, float frequency) {
+#pragma clang fp contract(off)
+  if (n > 0) {
+    y = y > 0.f ? __fdiv_rn(y, repetition) : y * repetition;
+    y = y - presence;
+    y = y - frequency * (float)n;
+  }
+  return y;
+}
+
+template <bool COUNTS>
+__global__ __launch_bounds__(kThreads) void choose_kernel(ChooseArgs a) {
+  __shared__ __align__(16) int counts[COUNTS ? kPiece : 4];
+  __shared__ int above[COUNTS ? VLAC_TREE_MAX_NODES : 1];
+  __shared__ float sv[kThreads / 64];
+  __shared__ int si[kThreads / 64];
+  read_args(a.logits, a.rows, a.vocab, a.stride, a.out, a.out_stride, a.token, a.token_stride, a.best, a.repetition, a.presence, a.frequency,
+            a.bias, a.bias_stride, a.allowed, a.allowed_stride, a.history, a.history_len, a.history_stride, a.tokens, a.parents,
+            a.drafted, a.more, a.more_stride, a.more_n, a.one, a.pieces, a.row0, a.rule_row0, a.rule_rows);
+  const int tid = threadIdx.x, local = blockIdx.x / a.pieces, piece = blockIdx.x - local * a.pieces, row = a.row0 + local;
+  const int c0 = piece * kPiece, c1 = min(c0 + kPiece, a.vocab), entry = row / a.tokens, node = row - entry * a.tokens;
+  if (COUNTS) {
+    for (int k = tid; k < kPiece / 4; k += kThreads) ((int4*)counts)[k] = make_int4(0, 0, 0, 0);
+    if (a.parents)
+      for (int t = tid; t < a.tokens; t += kThreads) {
+        const int x = a.parents[(size_t)entry * a.tokens + t];
+        above[t] = x < -2 || x >= t ? -2 : x;
+      }
+    __syncthreads();
+    auto count = [&](int token) {
+      if (token >= c0 && token < c1) atomicAdd(&counts[token - c0], 1);
+    };
+    if (a.history) {
+      const int n = (int)min((long long)max(a.history_len[entry], 0), a.history_stride);
+      const int* text = a.history + entry * a.history_stride;
+      for (int k = tid; k < n; k += kThreads) count(text[k]);
+    }
+    for (int k = tid; k < a.more_n; k += kThreads) count(a.more[(size_t)entry * a.more_stride + k]);
+    if (a.one && tid == 0) count(a.one[entry]);
+    if (a.parents && tid == 0) {
+      int x = node;
+      while (x >= 0) x = above[x];
+      if (x == -1)
+        for (x = node; x >= 0; x = above[x]) count(a.drafted[(size_t)entry * a.tokens + x]);
+    }
+    __syncthreads();
+  }
+  const size_t rule_row = (size_t)row * a.rule_rows + a.rule_row0;
+  const float* const x = a.logits + row * a.stride;
+  float* const out = a.out ? a.out + row * a.out_stride : nullptr;
+  const float* const bias = a.bias ? a.bias + rule_row * a.bias_stride : nullptr;
+  const uint32_t* const allowed = a.allowed ? a.allowed + rule_row * a.allowed_stride : nullptr;
+  Best b = {-INFINITY, kNobody};
+  constexpr int U = 8;
+  for (int v0 = c0 + tid; v0 < c1; v0 += U * kThreads) {
+    float l[U], add[U];
+    uint32_t word[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = min(v0 + u * kThreads, c1 - 1);
+      l[u] = x[v];
+      add[u] = bias ? bias[v] : 0.f;
+      word[u] = allowed ? allowed[v >> 5] : ~0u;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + u * kThreads;
+      if (v >= c1) break;
+      float y = l[u];
+      if (COUNTS) y = priced(y, counts[v - c0], a.repetition, a.presence, a.frequency);
+      if (bias) y = y + add[u];
+      if (!(word[u] >> (v & 31) & 1)) y = -INFINITY;
+      if (out) out[v] = y;
+      take(b, y, v);
+    }
+  }
+  if (!a.token) return;
+  b = best_of_all(b, sv, si);
+  if (tid == 0) {
+    if (a.pieces > 1) a.best[(size_t)row * a.pieces + piece] = make_float2(b.v, __int_as_float(b.at));
+    else a.token[(size_t)row * a.token_stride] = token_of(b);
+  }
+}
+
+// The pieces' best, a wave per row
+__global__ __launch_bounds__(kThreads) void choose_join_kernel(ChooseArgs a) {
+  const int lane = threadIdx.x & 63, row = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  Best b = {-INFINITY, kNobody};
+  for (int k = lane; k < a.pieces; k += 64) {
+    const float2 x = a.best[(size_t)row * a.pieces + k];
+    take(b, x.x, __float_as_int(x.y));
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float v = __shfl_xor(b.v, d);
+    const int i = __shfl_xor(b.at, d);
+    take(b, v, i);
+  }
+  if (lane == 0) a.token[(size_t)row * a.token_stride] = token_of(b);
+}
+
+int pieces_of(int vocab) { return (vocab + kPiece - 1) / kPiece; }
+
+}  // namespace
+
+int check_rules(const vlac_token_rules* r, int vocab) {
+  if (!r) return VLAC_E_NULL;
+  if (!(std::isfinite(r->repetition) && r->repetition > 0.f && std::isfinite(r->presence) && std::isfinite(r->frequency)))
+    return VLAC_E_RANGE;
+  if (r->tokens < 1 || r->tokens > VLAC_TREE_MAX_NODES) return VLAC_E_RANGE;
+  if ((r->history == nullptr) != (r->history_len == nullptr) || (r->parents == nullptr) != (r->drafted == nullptr)) return VLAC_E_NULL;
+  if (!r->parents && r->tokens > 1) return VLAC_E_NULL;
+  if (r->bias && r->bias_stride != 0 && r->bias_stride < vocab) return VLAC_E_SHAPE;
+  if (r->allowed && r->allowed_stride != 0 && r->allowed_stride < (vocab + 31) / 32) return VLAC_E_SHAPE;
+  if (r->history && (r->history_stride < 0 || r->history_stride > 1LL << 31)) return VLAC_E_SHAPE;
+  if ((r->bias && r->bias_stride > 1LL << 31) || (r->allowed && r->allowed_stride > 1LL << 31)) return VLAC_E_SHAPE;
+  if ((uintptr_t)r->bias % 4 || (uintptr_t)r->allowed % 4 || (uintptr_t)r->history % 4 || (uintptr_t)r->history_len % 4 ||
+      (uintptr_t)r->parents % 4 || (uintptr_t)r->drafted % 4)
+    return VLAC_E_SHAPE;
+  return VLAC_OK;
+}
+
+size_t choose_workspace(int rows, int vocab) { return ((size_t)std::max(rows, 1) * pieces_of(vocab) * sizeof(float2) + 255) / 256 * 256; }
+
+ChooseArgs choose_args(const float* logits, int rows, int vocab, int64_t stride, const vlac_token_rules& r, float* out, int64_t out_stride,
+                       int32_t* token, void* ws) {
+  ChooseArgs a = {};
+  a.logits = logits; a.rows = rows; a.vocab = vocab; a.stride = stride;
+  a.out = out; a.out_stride = out_stride;
+  a.token = token; a.token_stride = 1;
+  a.best = (float2*)ws;
+  a.repetition = r.repetition; a.presence = r.presence; a.frequency = r.frequency;
+  a.bias = r.bias; a.bias_stride = r.bias_stride;
+  a.allowed = r.allowed; a.allowed_stride = r.allowed_stride;
+  a.history = r.history; a.history_len = r.history_len; a.history_stride = r.history_stride;
+  a.tokens = r.tokens; a.parents = r.parents; a.drafted = r.drafted;
+  a.rule_rows = 1;
+  return a;
+}
+
+void launch_choose(ChooseArgs a, hipStream_t st) {
+  a.pieces = pieces_of(a.vocab);
+  const bool prices = a.repetition != 1.f || a.presence != 0.f || a.frequency != 0.f;
+  const bool counts = prices && (a.history || a.parents || a.more_n > 0 || a.one);
+  const int most = std::max(1, (1 << 23) / a.pieces);  // rows of a launch (one of 2^32 threads would not run whole)
+  for (a.row0 = 0; a.row0 < a.rows; a.row0 += most) {
+    const dim3 grid((unsigned)(std::min(a.rows - a.row0, most) * a.pieces));
+    if (counts) hipLaunchKernelGGL(choose_kernel<true>, grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(choose_kernel<false>, grid, dim3(kThreads), 0, st, a);
+  }
+  if (a.token && a.pieces > 1)
+    hipLaunchKernelGGL(choose_join_kernel, dim3((unsigned)((a.rows + kThreads / 64 - 1) / (kThreads / 64))), dim3(kThreads), 0, st, a);
+}
+
+extern "C" {
+
+size_t vlac_choose_workspace_bytes(int rows, int vocab) {
+  return rows < 0 || rows > VLAC_CHOOSE_MAX_ROWS || vocab < 1 || vocab > 1 << 24 ? 0 : choose_workspace(rows, vocab);
+}
+
+int vlac_choose_tokens(const float* logits, int rows, int vocab, int64_t stride, const vlac_token_rules* rules, float* out_logits,
+                       int64_t out_stride, int32_t* out_token, void* workspace, size_t workspace_bytes, void* stream) {
+  if (rows < 0 || rows > VLAC_CHOOSE_MAX_ROWS || vocab < 1 || vocab > 1 << 24) return VLAC_E_RANGE;
+  const int rc = check_rules(rules, vocab);
+  if (rc != VLAC_OK) return rc;
+  if (rows % rules->tokens) return VLAC_E_SHAPE;
+  if (stride < vocab || stride > 1LL << 31) return VLAC_E_SHAPE;
+  if (out_logits && (out_stride < vocab || out_stride > 1LL << 31 || (out_logits == logits && out_stride != stride))) return VLAC_E_SHAPE;
+  if (rows == 0) return VLAC_OK;
+  if (!logits || (out_token && !workspace)) return VLAC_E_NULL;
+  if ((uintptr_t)logits % 4 || (uintptr_t)out_logits % 4 || (uintptr_t)out_token % 4 || (out_token && (uintptr_t)workspace % 16))
+    return VLAC_E_SHAPE;
+  if (out_token && workspace_bytes < choose_workspace(rows, vocab)) return VLAC_E_RANGE;
+  if (!out_logits && !out_token) return VLAC_OK;
+  launch_choose(choose_args(logits, rows, vocab, stride, *rules, out_logits, out_stride, out_token, workspace), (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
+}
+
+}  // extern "C"

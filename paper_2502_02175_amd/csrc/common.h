@@ -273,7 +273,7 @@ struct NextEmbed { const bf16_t* embed; int d; float* h; int h_seq, h_pos; };
 void launch_argmax(const float2* best, int B, int vocab, int32_t* out, int out_stride, const NextEmbed& next,
                    hipStream_t st);
 void launch_embed_rows(const bf16_t* embed, const int32_t* tokens, int B, int d, int vocab, float* h,
-                       int max_seq, int pos, hipStream_t st);
+                       int max_seq, int pos, hipStream_t st, int tokens_stride = 1);
 // e4m3 storage: scales of the N source rows, then codes in fragment order (two k-tiles per
 // 16-byte lane slot) and the scales in packed row order
 void launch_row_scales(const bf16_t* src, int N, int K, float* scales, hipStream_t st);

@@ -717,15 +717,15 @@ void launch_argmax(const float2* best, int B, int vocab, int32_t* out, int out_s
 __global__ __launch_bounds__(256) void embed_rows_kernel(const bf16_t* __restrict__ embed,
                                                          const int32_t* __restrict__ tokens, int d,
                                                          int vocab, float* __restrict__ h,
-                                                         int max_seq, int pos) {
+                                                         int max_seq, int pos, int tokens_stride) {
   const int b = blockIdx.x;
-  embed_row(embed, tokens[b], vocab, d, h + ((size_t)b * max_seq + pos) * d, threadIdx.x, 256);
+  embed_row(embed, tokens[(size_t)b * tokens_stride], vocab, d, h + ((size_t)b * max_seq + pos) * d, threadIdx.x, 256);
 }
 
 void launch_embed_rows(const bf16_t* embed, const int32_t* tokens, int B, int d, int vocab, float* h,
-                       int max_seq, int pos, hipStream_t st) {
+                       int max_seq, int pos, hipStream_t st, int tokens_stride) {
   hipLaunchKernelGGL(embed_rows_kernel, dim3(B), dim3(256), 0, st, embed, tokens, d, vocab, h,
-                     max_seq, pos);
+                     max_seq, pos, tokens_stride);
 }
 
 // ---------------------------------------------------------------------------

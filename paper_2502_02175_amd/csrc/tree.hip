@@ -1,0 +1,182 @@
+// Trees of drafted tokens: the path on which the drafts are what was chosen, and that path kept in the pages.  Whole numbers, and
+// values that are copied bit for bit.
+#include <algorithm>
+#include <type_traits>
+
+#include "pages.h"
+
+namespace {
+
+// A workgroup takes an entry.  Every node that was drafted as its parent's choice offers itself to the parent, which keeps the
+// first (a minimum: no order decides); then one thread follows the offers from node 0 on, an LDS round trip per node of the path.
+constexpr int kAccept = 256;
+__global__ __launch_bounds__(kAccept) void tree_accept_kernel(const int* __restrict__ parents, const int* __restrict__ drafted,
+                                                            const int* __restrict__ chosen, int tokens, int* __restrict__ out_path,
+                                                            int* __restrict__ out_count, int* __restrict__ out_token) {
+  __shared__ int pick[VLAC_TREE_MAX_NODES], next[VLAC_TREE_MAX_NODES], path[VLAC_TREE_MAX_NODES];
+  __shared__ int s_count;
+  const int tid = threadIdx.x;
+  const size_t at = (size_t)blockIdx.x * tokens;
+  for (int t = tid; t < tokens; t += kAccept) {
+    pick[t] = chosen[at + t];
+    next[t] = tokens;
+  }
+  __syncthreads();
+  for (int t = tid; t < tokens; t += kAccept) {
+    const int up = parents[at + t];
+    if (t > 0 && up >= 0 && up < t && drafted[at + t] == pick[up]) atomicMin(&next[up], t);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int n = 0;
+    if (parents[at] == -1)
+      for (int t = 0; t < tokens; t = next[t]) path[n++] = t;  // (a node's offers come after it: the path ascends)
+    s_count = n;
+    out_count[blockIdx.x] = n;
+    out_token[blockIdx.x] = n > 0 ? pick[path[n - 1]] : -1;
+  }
+  __syncthreads();
+  for (int t = tid; t < tokens; t += kAccept) out_path[at + t] = t < s_count ? path[t] : -1;
+}
+
+struct KeepArgs {
+  PoolView p;
+  const int *seqs, *pos, *path, *count;
+  int n, tokens;
+};
+
+// Whether entry i can be done, worked out by every workgroup that has to do with it: -> how many rows are kept, or -1.
+// from, to: where row k comes from and goes to, page * 32 + position in it (equal: it stays).
+constexpr int kKeep = 256;
+__device__ int keep_entry(const KeepArgs& a, int i, int* from, int* to, int* bad) {
+  const PoolView& p = a.p;
+  const int tid = threadIdx.x, s = a.seqs[i], p0 = a.pos[i], m = a.count[i];
+  if (p0 < 0) return -1;
+  const int l = checked_len(p, s);
+  if (tid == 0) *bad = l < 0 || m < 0 || m > a.tokens || (long long)p0 + a.tokens != l;
+  __syncthreads();
+  if (*bad) return -1;
+  bool wrong = false;
+  for (int k = tid; k < i; k += kKeep) wrong |= a.seqs[k] == s && a.pos[k] >= 0;
+  for (int k = tid; k < m; k += kKeep) {
+    const int t = a.path[(size_t)i * a.tokens + k], before = k > 0 ? a.path[(size_t)i * a.tokens + k - 1] : -1;
+    int f = 0, g = 0;
+    if (t <= before || t < k || t >= a.tokens) {
+      wrong = true;
+    } else if (t != k) {
+      const int* row = p.table + (size_t)s * p.max_pages;
+      const int fp = row[(p0 + t) / kPage], gp = row[(p0 + k) / kPage];
+      if ((unsigned)fp >= (unsigned)p.n_pages || (unsigned)gp >= (unsigned)p.n_pages || p.refs[gp] != 1) {
+        wrong = true;
+      } else {
+        f = fp * kPage + (p0 + t) % kPage;
+        g = gp * kPage + (p0 + k) % kPage;
+      }
+    }
+    from[k] = f;
+    to[k] = g;
+  }
+  if (wrong) *bad = 1;
+  __syncthreads();
+  return *bad ? -1 : m;
+}
+
+// The rows of the path, one behind the other.  A workgroup takes an entry, a layer and some kv heads; a thread takes 16 bytes of K of
+// every row (8 features), and a feature of V.  A row only moves down and rows are taken in ascending order, a thread's own
+// words: what is read was not written before.  Eight rows are asked for at a time.
+// Tables, counts and lengths stay as they are until the next launch; that this entry can be done is left for it in the pool's
+// scratch (is_dst of the sequence, zero between calls: the entry's number + 1).
+constexpr int kHeads = 4;  // of a work item
+__global__ __launch_bounds__(kKeep) void pages_keep_kernel(KeepArgs a, int head_groups, int items) {
+  __shared__ int from[VLAC_TREE_MAX_NODES], to[VLAC_TREE_MAX_NODES];
+  __shared__ int bad;
+  const PoolView& p = a.p;
+  const int hd = p.head_dim;
+  const size_t page = p.page(), tile = p.tile();
+  for (int it = blockIdx.x; it < items; it += gridDim.x) {
+    const int hg = it % head_groups, rest = it / head_groups, layer = rest % p.n_layers, i = rest / p.n_layers;
+    const int m = keep_entry(a, i, from, to, &bad);
+    if (m >= 0 && threadIdx.x == 0 && hg == 0 && layer == 0) p.is_dst()[a.seqs[i]] = i + 1;
+    const int h0 = hg * kHeads, heads = min(kHeads, p.n_kv_heads - h0);
+    bf16_t* const k0 = p.data + ((size_t)layer * 2 * p.n_kv_heads + h0) * tile;
+    bf16_t* const v0 = k0 + p.n_kv_heads * tile;
+    auto move = [&](auto* base, auto at) {  // the rows' words that lie at(position) behind base, in their page
+      for (int r0 = 0; r0 < m; r0 += 8) {
+        std::decay_t<decltype(*base)> y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int f = from[min(r0 + e, m - 1)];
+          y[e] = base[(f >> 5) * (page * sizeof(bf16_t) / sizeof(*base)) + at(f & 31)];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int k = min(r0 + e, m - 1), t = to[k];
+          if (r0 + e < m && from[k] != t) base[(t >> 5) * (page * sizeof(bf16_t) / sizeof(*base)) + at(t & 31)] = y[e];
+        }
+      }
+    };
+    for (int u = threadIdx.x; u < heads * hd / 8; u += kKeep) {  // 16 bytes of K
+      const int h = u / (hd / 8), c = u - h * (hd / 8);
+      move((u32x4*)(k0 + h * tile + (c >> 1) * 512 + (c & 1) * 256), [](int r) { return r; });
+    }
+    for (int u = threadIdx.x; u < heads * hd; u += kKeep) {  // a feature of V
+      const int h = u / hd, f = u - h * hd;
+      move(v0 + h * tile + (f >> 5) * 1024 + (f & 31) * 8, [](int r) { return (r >> 4) * 512 + (r >> 2 & 1) * 256 + (r >> 3 & 1) * 4 + (r & 3); });
+    }
+    __syncthreads();  // (from and to are written again)
+  }
+}
+
+// Lengths, and what lies behind them is released.  A workgroup per entry, behind the launch that moves the rows.
+__global__ __launch_bounds__(64) void pages_keep_end_kernel(KeepArgs a) {
+  const PoolView& p = a.p;
+  const int i = blockIdx.x, s = a.seqs[i], p0 = a.pos[i];
+  if (p0 < 0) return;
+  if ((unsigned)s >= (unsigned)p.max_seqs || p.is_dst()[s] != i + 1) {
+    if (threadIdx.x == 0) report(p, PAGES_BAD_ENTRY);
+    return;
+  }
+  const int m = a.count[i], kept = pages_of(p0 + m), held = pages_of(p0 + a.tokens);
+  for (int j = kept + threadIdx.x; j < held; j += 64) {
+    int* at = p.table + (size_t)s * p.max_pages + j;
+    const int pg = *at;
+    *at = -1;
+    if ((unsigned)pg < (unsigned)p.n_pages) atomicAdd(p.refs + pg, -1);
+    else report(p, PAGES_BAD_ENTRY);
+  }
+  if (threadIdx.x == 0) {
+    p.len[s] = p0 + m;
+    p.is_dst()[s] = 0;  // (another entry of the sequence finds this or i + 1, neither of which is its own)
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int vlac_tree_accept(const int32_t* parents, const int32_t* drafted, const int32_t* chosen, int n, int tokens, int32_t* out_path,
+                     int32_t* out_count, int32_t* out_token, void* stream) {
+  if (n < 0 || n > VLAC_PAGES_MAX_LIST || tokens < 1 || tokens > VLAC_TREE_MAX_NODES) return VLAC_E_RANGE;
+  if (n == 0) return VLAC_OK;
+  if (!parents || !drafted || !chosen || !out_path || !out_count || !out_token) return VLAC_E_NULL;
+  hipLaunchKernelGGL(tree_accept_kernel, dim3(n), dim3(kAccept), 0, (hipStream_t)stream, parents, drafted, chosen, tokens, out_path,
+                     out_count, out_token);
+  return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
+}
+
+int vlac_pages_keep(const vlac_pages* pages, const int32_t* seqs, const int32_t* pos, int n, int tokens, const int32_t* path,
+                    const int32_t* count, void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc != VLAC_OK) return rc;
+  if (n < 0 || n > VLAC_PAGES_MAX_LIST || tokens < 1 || tokens > VLAC_TREE_MAX_NODES) return VLAC_E_RANGE;
+  if (n == 0) return VLAC_OK;
+  if (!seqs || !pos || !path || !count) return VLAC_E_NULL;
+  const KeepArgs a = {pool_view(pages), seqs, pos, path, count, n, tokens};
+  hipStream_t st = (hipStream_t)stream;
+  const int groups = (pages->n_kv_heads + kHeads - 1) / kHeads, items = n * pages->n_layers * groups;  // (less than 2^30)
+  hipLaunchKernelGGL(pages_keep_kernel, dim3((unsigned)std::min(items, 1 << 16)), dim3(kKeep), 0, st, a, groups, items);
+  hipLaunchKernelGGL(pages_keep_end_kernel, dim3(n), dim3(64), 0, st, a);
+  return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
+}
+
+}  // extern "C"
