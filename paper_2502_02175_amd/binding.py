@@ -50,6 +50,7 @@ TREE_MAX_NODES = 512
 class Rotary(C.Structure):
     """vlac_rotary; made by `rotary`, which keeps its table alive."""
     _fields_ = [("dims", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("turns", C.c_void_p)]
+    index = -1          # the table's device (-1: an address)
 
 
 class TokenRules(C.Structure):
@@ -664,30 +665,37 @@ def rotary(dims, layout=ROTARY_HALF, base=10000.0, factor=1.0, original=0, low=1
         turns = torch.empty(max(int(dims) // 2, 1), dtype=torch.float64, device=device)
         vlac_rotary_fill(dims, base, factor, original, low, high, turns)
     r = Rotary(dims, layout, amplitude, _at(_gpu_of(turns), turns, torch.float64, dims // 2, "turns"))
-    r.tensors = (turns,)
+    r.tensors, r.index = (turns,), turns.get_device()
     r.ref = C.byref(r)
     return r
 
 
-def _heads(p, x, count, heads, name):
-    """Address and row stride of rows [.., heads, head_dim] of the pool's type: the last two dimensions dense, rows equally far apart."""
-    if x is None or isinstance(x, int):
-        return x, heads * p.head_dim
-    return _rows(p, x, count, heads * p.head_dim, name)
+def _heads(p, x, n, tokens, heads, name):
+    """Address and row stride of rows [n, tokens, heads, head_dim] of the pool's type: the last two dimensions dense, rows equally far
+    apart.  (A slice of a joint projection, as a rule: looked at without making a view of it.)"""
+    if x is not None and not isinstance(x, int) and x.dim() == 4 and x.dtype is p.rows_dtype and x.get_device() == p.index >= 0:
+        hd = p.head_dim
+        if x.shape == (n, tokens, heads, hd):
+            s0, s1, s2, s3 = x.stride()
+            if s3 == 1 and (s2 == hd or heads == 1) and (n == 1 or (s0 == tokens * s1 if tokens > 1 else True)):
+                return x.data_ptr(), (s1 if tokens > 1 else s0 if n > 1 else heads * hd)
+    return _rows(p, x, n * tokens, heads * p.head_dim, name)
 
 
 def vlac_pages_append_rotated(p, layer, seqs, pos, n, tokens, rot, places, n_q_heads, q, k, v, q_out, q_gain=None, k_gain=None, eps=1e-6,
                               stream=None, check=True):
     """q, q_out: [n, tokens, n_q_heads, head_dim], k, v: [n, tokens, n_kv_heads, head_dim], of the pool's type; slices of a joint
     projection have one row stride.  rot: `rotary`'s, or None; gains: bf16 [head_dim], or None."""
-    count = n * tokens
-    k_at, k_stride = _heads(p, k, count, p.n_kv_heads, "k")
-    v_at, v_stride = _heads(p, v, count, p.n_kv_heads, "v")
+    if rot is not None and rot.index != p.index and rot.index >= 0 <= p.index:
+        raise ValueError("the rotation's table lies on GPU %d, the pool on GPU %d" % (rot.index, p.index))
+    heads = p.n_kv_heads
+    k_at, k_stride = _heads(p, k, n, tokens, heads, "k")
+    v_at, v_stride = _heads(p, v, n, tokens, heads, "v")
     if k_stride != v_stride:
         raise ValueError("k and v: rows %d and %d values apart" % (k_stride, v_stride))
     if n_q_heads > 0:
-        q_at, q_stride = _heads(p, q, count, n_q_heads, "q")
-        o_at, o_stride = _heads(p, q_out, count, n_q_heads, "q_out")
+        q_at, q_stride = _heads(p, q, n, tokens, n_q_heads, "q")
+        o_at, o_stride = (q_at, q_stride) if q_out is q else _heads(p, q_out, n, tokens, n_q_heads, "q_out")
     else:
         q_at = o_at = None
         q_stride = o_stride = 0
@@ -695,8 +703,8 @@ def vlac_pages_append_rotated(p, layer, seqs, pos, n, tokens, rot, places, n_q_h
         import torch
         q_gain, k_gain = (_at(p, x, torch.bfloat16, p.head_dim, name) for x, name in ((q_gain, "q_gain"), (k_gain, "k_gain")))
     return _call(p, "vlac_pages_append_rotated", stream, check, _ref(p), layer, _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n,
-                 tokens, _ref(rot), _list(p, places, count, "places"), n_q_heads, q_at, q_stride, k_at, v_at, k_stride, o_at, o_stride,
-                 q_gain, k_gain, eps)
+                 tokens, _ref(rot), None if places is None else _list(p, places, n * tokens, "places"),
+                 n_q_heads, q_at, q_stride, k_at, v_at, k_stride, o_at, o_stride, q_gain, k_gain, eps)
 
 
 def vlac_attend_tree_workspace_bytes(p, n, tokens, n_q_heads):

@@ -1,9 +1,20 @@
 // Queries, keys and values of new tokens on their way into the pages: the norm of every head and the rotation of its position
 // in the same pass,
 //   q' = R(place) N(q), k' = R(place) N(k), v' = v,   N(x) = x rsqrt(mean x^2 + eps) gain,
-//   R turns pair f by 2 pi turns[f] place (in 64 bits up to the fraction of a turn: 32 lose it at far places).
+//   R turns pair f by 2 pi turns[f] place.
+// Norm and rotation in fp32, rounded once.  The turn is worked out in 64 bits and its fraction rounded to 32 (which lose it
+// at far places otherwise); the chip's sine and cosine of a fraction of a turn are off by 1.3e-7 at most, a 3000th of
+// a half step of fp16 of the larger value.
+//
+// Bound by latency up to some MB (arguments - position and sequence - rows, page and table of turns - stores: one token of
+// two sequences 3.1 us, 8 x 31 tokens of 32 heads of 128, 12 MB, 7.4), then by memory: 1024 tokens of 32 heads (50 MB read and written) 12.0
+// us, 4096 49, 4.1 TB/s.  Whole rows of a head would be longer pieces than a wave's, but a page stores K by 8 features of 32 positions and V
+// by 8 positions of a feature, so a wave takes 8 positions of queries and keys, and 16 of values: a line of K, or a word of
+// every feature, is written at once.  (V by 8 positions through LDS: 9.2 us instead of 7.4; its last rows by single values
+// instead of four at a time: 16 x 64 tokens of 32 heads 23 us instead of 15.)
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "pages.h"
 
@@ -11,7 +22,7 @@ namespace {
 
 struct RotaryArgs {
   PoolView p;
-  int layer, n, tokens, blocks;  // blocks: of 8 positions that an entry's tokens may touch
+  int layer, n, tokens;
   const int *seqs, *pos, *places;
   int n_q_heads;
   const bf16_t *q, *k, *v;
@@ -20,11 +31,15 @@ struct RotaryArgs {
   long long q_out_stride;
   const bf16_t *q_gain, *k_gain;
   float eps;
-  int dims, pairs;  // rotated features (0: none); pairs: neighbours are a pair
+  int dims;  // rotated features (0: none)
   float amplitude;
   const double* turns;
   int first;  // wave of the call that this launch begins with
+  // a wave takes up to G heads: of queries and keys (the first qk_waves waves of an entry, in qk_groups groups per block of 8
+  // positions), or of values (v_waves, v_groups per block of 16)
+  int qk_groups, v_groups, qk_waves, v_waves;
 };
+enum Turning { COPY, PAIRS, HALVES, ANY_HALVES };  // (HALVES: dims / 2 is a multiple of 8, so that a lane's 8 partners are another lane's)
 
 template <bool F16>
 __device__ inline void widen(uint32_t x, float& lo, float& hi) {
@@ -50,155 +65,303 @@ __device__ inline uint32_t narrow2(float lo, float hi) {
   }
 }
 
-// Sum over the GROUP lanes (8 or 16, aligned) that share a row
+// Sum over the GROUP lanes (8 or 16, aligned) that share a row, by moves inside the vector ALU: neighbours, pairs of them, the other
+// quads of a half row (mirrored), the other half (mirrored)
+template <int HOW>
+__device__ inline float moved(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), HOW, 0xf, 0xf, true));
+}
 template <int GROUP>
 __device__ inline float row_sum(float x) {
-#pragma unroll
-  for (int d = 1; d < GROUP; d <<= 1) x += __shfl_xor(x, d);
+  x += moved<0xb1>(x);    // (quad: 1 0 3 2)
+  x += moved<0x4e>(x);    // (quad: 2 3 0 1)
+  x += moved<0x141>(x);   // (half row mirrored)
+  if constexpr (GROUP == 16) x += moved<0x140>(x);  // (row mirrored)
   return x;
 }
 
-// A wave takes one head (of the queries, the keys or the values) at 8 positions that lie side by side in a page: one page to
-// look up, and a K store of 8 rows is a line.  A lane holds 8 features of a row, so head_dim / 8 lanes hold a row; the partners of a
-// pair, and V's 4 neighbouring positions, meet in LDS.
-template <int HD, bool F16>
-__global__ __launch_bounds__(256) void rotary_append_kernel(RotaryArgs a) {
-  constexpr int LANES = HD / 8, ROWS = 64 / LANES, STEPS = 8 / ROWS;  // rows at a time
-  __shared__ float meet[4][8 * HD];
-  const PoolView& p = a.p;
-  read_args(a.layer, a.n, a.tokens, a.blocks, a.seqs, a.pos, a.places, a.n_q_heads, a.q, a.k, a.v, a.q_stride, a.kv_stride, a.q_out,
-            a.q_out_stride, a.q_gain, a.k_gain, a.eps, a.dims, a.pairs, a.amplitude, a.turns, a.first, p.data, p.refs, p.table, p.len,
-            p.n_pages, p.max_seqs, p.max_pages, p.n_layers, p.n_kv_heads);
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & (LANES - 1), r0 = lane / LANES;
-  const int units = a.n_q_heads + 2 * p.n_kv_heads;
-  const int u = a.first + blockIdx.x * 4 + w;  // (a call has less than 2^29 waves)
-  const int ib = u / units, unit = u - ib * units, i = ib / a.blocks, blk = ib - i * a.blocks;
-  if (i >= a.n) return;
-  const int p0 = ld_scalar(a.pos + i), s = ld_scalar(a.seqs + i);
-  if (p0 < 0) return;
-  const long long at8 = ((long long)p0 / 8 + blk) * 8;  // the block's first position
-  if (at8 >= (long long)p0 + a.tokens) return;
-  const int t0 = (int)(at8 - p0);                        // the token of its first row (negative: before the first)
-  const int what = unit < a.n_q_heads ? 0 : unit < a.n_q_heads + p.n_kv_heads ? 1 : 2;  // queries, keys, values
-  const int h = what == 0 ? unit : unit - a.n_q_heads - (what - 1) * p.n_kv_heads;
+// A store of 16 bytes, non-temporal in large calls: with 2 heads of 128 or more to a wave, 1024 tokens of 32 heads 15.1 -> 12.0 us, 4
+// x 1057 of 12 on 2 12.5 -> 11.0, 32 x 2 tokens' equal.  (V's stores marked so as well: 17 us.)
+template <bool STREAM>
+__device__ inline void put(bf16_t* to, const uint4& x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), (u32x4*)to);
+  else *(uint4*)to = x;
+}
 
-  // the rows, asked for before it is known whether they have a place
-  const bf16_t* src = what == 0 ? a.q : what == 1 ? a.k : a.v;
-  const long long stride = what == 0 ? a.q_stride : a.kv_stride;
-  uint4 x16[STEPS];
-  int place[STEPS];
+// Where the tokens of an entry lie that a wave takes: rows from .. to - 1 of the block of positions that begins at `at`, the first of them
+// token t0 + from; and the page, if they may be stored there (rows before `last` lie inside the sequence).
+struct Block {
+  int i, seq, t0, from, to, last;
+  long long at;
+  bf16_t* page;  // of the layer
+};
+// The block blk of `size` positions of entry i: false if no token lies in it
+__device__ inline bool block_of(const RotaryArgs& a, int i, int blk, int size, Block& b) {
+  const int p0 = ld_scalar(a.pos + i);
+  b.i = i;
+  b.seq = ld_scalar(a.seqs + i);
+  b.at = ((long long)p0 / size + blk) * size;
+  if (p0 < 0 || b.at >= (long long)p0 + a.tokens) return false;
+  b.t0 = (int)(b.at - p0);
+  b.from = max(-b.t0, 0);
+  b.to = min(a.tokens - b.t0, size);
+  return true;
+}
+__device__ inline void find_page(const RotaryArgs& a, Block& b, int size, int lane) {
+  const PoolView& p = a.p;
+  const bool known = (unsigned)b.seq < (unsigned)p.max_seqs;
+  const int l = known ? ld_scalar(p.len + b.seq) : -1;
+  const long long j = b.at / kPage;
+  int pg = known && j < p.max_pages ? ld_scalar(p.table + (size_t)b.seq * p.max_pages + j) : -1;
+  const bool fits = l >= 0 && l <= p.max_pages * kPage;
+  if ((unsigned)pg >= (unsigned)p.n_pages || ld_scalar(p.refs + pg) != 1) pg = -1;
+  if (lane == 0 && (pg < 0 || !fits || b.at + b.to > l)) report(p, PAGES_BAD_ENTRY);
+  b.page = pg >= 0 && fits ? p.data + (size_t)pg * p.page() + (size_t)a.layer * 2 * p.n_kv_heads * p.tile() : nullptr;
+  b.last = fits ? (int)min(l - b.at, (long long)size) : 0;
+}
+
+// Values: 16 positions, whose words of a page (8 of them, of one feature) a wave has together.  A lane loads 8 features of a
+// row and changes places with the lanes 16, 32 and 48 further, which have them of the next three rows: two swaps of registers between
+// halves and two between quarters of the wave transpose 4 x 4 words, without LDS.
+template <int HD, int G>
+__device__ inline void value_rows(const RotaryArgs& a, Block& b, int group, int lane) {
+  constexpr int LANES = HD / 8, SIDE = 16 / LANES, STEPS = 4 / SIDE;  // groups of 4 rows side by side, and behind one another
+  const PoolView& p = a.p;
+  const int c = lane & (LANES - 1), side = (lane & 15) / LANES, e4 = lane >> 4, hkv = p.n_kv_heads;
+  const int h0 = group * G;
+  size_t row[STEPS];
+  bool mine[STEPS];
 #pragma unroll
   for (int y = 0; y < STEPS; ++y) {
-    const int t = t0 + r0 + y * ROWS;
-    const bool mine = t >= 0 && t < a.tokens;
-    const size_t row = (size_t)i * a.tokens + (mine ? t : 0);
-    x16[y] = mine ? *(const uint4*)(src + row * stride + (size_t)h * HD + 8 * c) : make_uint4(0, 0, 0, 0);
-    place[y] = !mine ? -1 : a.places ? a.places[row] : (int)min((long long)p0 + t, 0x7fffffffLL);
+    const int r = 4 * (y * SIDE + side) + e4;
+    mine[y] = r >= b.from && r < b.to;
+    row[y] = (size_t)b.i * a.tokens + (mine[y] ? b.t0 + r : 0);
   }
-
-  // where K and V go
-  bf16_t* tile = nullptr;
-  int l = 0;
-  if (what > 0) {
-    const bool known = (unsigned)s < (unsigned)p.max_seqs;
-    l = known ? ld_scalar(p.len + s) : -1;
-    const long long j = at8 / kPage;
-    int pg = known && j < p.max_pages ? ld_scalar(p.table + (size_t)s * p.max_pages + j) : -1;
-    const bool fits = l >= 0 && l <= p.max_pages * kPage;
-    const bool whole = fits && min(at8 + 8, (long long)p0 + a.tokens) <= l;  // (all of the block's tokens lie inside)
-    if ((unsigned)pg >= (unsigned)p.n_pages || ld_scalar(p.refs + pg) != 1) pg = -1;
-    if (lane == 0 && (pg < 0 || !whole)) report(p, PAGES_BAD_ENTRY);
-    if (pg < 0 || !fits) return;
-    tile = p.data + (size_t)pg * p.page() + ((size_t)a.layer * 2 * p.n_kv_heads + (what - 1) * p.n_kv_heads + h) * p.tile();
-  }
-  float* const mine_lds = meet[w];
-
-  if (what == 2) {
-    // [position][feature] in LDS, then a feature per lane
+  auto load = [&](uint4(&x)[STEPS], int h) {
 #pragma unroll
     for (int y = 0; y < STEPS; ++y)
-      ((uint4*)mine_lds)[(r0 + y * ROWS) * LANES + c] = place[y] >= 0 ? x16[y] : make_uint4(0, 0, 0, 0);
-    asm volatile("" ::: "memory");  // (read as another type below: the order is the wave's own, if the compiler keeps it)
-    const bf16_t* rows = (const bf16_t*)mine_lds;
-    const int from = max(-t0, 0), to = (int)min(min((long long)a.tokens - t0, l - at8), 8LL);  // rows that are stored
+      x[y] = mine[y] ? *(const uint4*)(a.v + row[y] * a.kv_stride + (size_t)h * HD + 8 * c) : make_uint4(0, 0, 0, 0);
+  };
+  uint4 all[G][STEPS];
 #pragma unroll
-    for (int half = 0; half < HD / 64; ++half) {
-      const int f = 64 * half + lane;
+  for (int k = 0; k < G; ++k) load(all[k], min(h0 + k, hkv - 1));
+  bool gone[STEPS];  // (rows that are not there are zeros)
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        uint32_t y[4];
+  for (int y = 0; y < STEPS; ++y) gone[y] = a.places && mine[y] && a.places[row[y]] < 0;
+  find_page(a, b, 16, lane);
+  if (!b.page) return;
+  const int end = min(b.to, b.last), r16 = ((int)b.at & 31) >> 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = rows[(4 * g + e) * HD + f];
-        bf16_t* d = tile + (size_t)(f >> 5) * 1024 + (((int)at8 & 31) >> 4) * 512 + g * 256 + (f & 31) * 8 + (((int)at8 >> 3) & 1) * 4;
-        if (from <= 4 * g && to >= 4 * g + 4) {
-          *(uint2*)d = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (4 * g + e >= from && 4 * g + e < to) d[e] = (bf16_t)y[e];
-        }
-      }
-    }
-    return;
-  }
-
-  const bf16_t* gain = what == 0 ? a.q_gain : a.k_gain;
-  if (gain || a.dims > 0) {
-    float g8[8];
-    if (gain) {
-      const uint4 x = *(const uint4*)(gain + 8 * c);
-      widen<false>(x.x, g8[0], g8[1]);
-      widen<false>(x.y, g8[2], g8[3]);
-      widen<false>(x.z, g8[4], g8[5]);
-      widen<false>(x.w, g8[6], g8[7]);
-    }
-    const int half = a.dims >> 1;
+  for (int head = 0; head < G; ++head) {
+    const int h = h0 + head;
+    if (h >= hkv) break;
+    const uint4(&x)[STEPS] = all[head];
+    uint2 out[STEPS][2];  // the two features of this lane: the group's 4 rows
 #pragma unroll
     for (int y = 0; y < STEPS; ++y) {
-      const int r = r0 + y * ROWS;
-      float x[8];
-      widen<F16>(x16[y].x, x[0], x[1]);
-      widen<F16>(x16[y].y, x[2], x[3]);
-      widen<F16>(x16[y].z, x[4], x[5]);
-      widen<F16>(x16[y].w, x[6], x[7]);
-      if (gain) {
-        float sum = 0.f;
+      uint32_t w0 = gone[y] ? 0u : x[y].x, w1 = gone[y] ? 0u : x[y].y, w2 = gone[y] ? 0u : x[y].z, w3 = gone[y] ? 0u : x[y].w;
+      // word k of row r (the lane's quarter) -> word r of quarter k
+      auto s = __builtin_amdgcn_permlane32_swap(w0, w2, false, false);
+      w0 = s[0]; w2 = s[1];
+      s = __builtin_amdgcn_permlane32_swap(w1, w3, false, false);
+      w1 = s[0]; w3 = s[1];
+      s = __builtin_amdgcn_permlane16_swap(w0, w1, false, false);
+      w0 = s[0]; w1 = s[1];
+      s = __builtin_amdgcn_permlane16_swap(w2, w3, false, false);
+      w2 = s[0]; w3 = s[1];
+      out[y][0] = make_uint2((w0 & 0xffffu) | w1 << 16, (w2 & 0xffffu) | w3 << 16);
+      out[y][1] = make_uint2(w0 >> 16 | (w1 & 0xffff0000u), w2 >> 16 | (w3 & 0xffff0000u));
+    }
+    bf16_t* const tile = b.page + ((size_t)hkv + h) * p.tile() + r16 * 512;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-        const float scale = rsqrtf(row_sum<LANES>(sum) * (1.f / HD) + a.eps);
+    for (int k = 0; k < 2; ++k) {
+      const int f = 8 * c + 2 * e4 + k;
+      bf16_t* const at = tile + (size_t)(f >> 5) * 1024 + (f & 31) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * scale * g8[e];
-      }
-      if (a.dims > 0) {
-        float* row = mine_lds + r * HD;
-        *(float4*)(row + 8 * c) = make_float4(x[0], x[1], x[2], x[3]);
-        *(float4*)(row + 8 * c + 4) = make_float4(x[4], x[5], x[6], x[7]);
-        asm volatile("" ::: "memory");
+      for (int y = 0; y < STEPS / 2; ++y) {
+        // rows r .. r + 3 and r + 8 .. r + 11 make up a word
+        const int four = y * SIDE + side, r = 4 * four;
+        bf16_t* const d = at + four * 256;
+        const uint2 lo = out[y][k], hi = out[y + STEPS / 2][k];
+        if (r >= b.from && r + 12 <= end) {
+          *(uint4*)d = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int f = 8 * c + e;
-          if (f >= a.dims) continue;
-          const bool second = a.pairs ? f & 1 : f >= half;
-          const int pair = a.pairs ? f >> 1 : second ? f - half : f;
-          const float other = row[a.pairs ? f ^ 1 : second ? f - half : f + half];
-          const double turn = (double)place[y] * a.turns[pair];
-          const float part = (float)(turn - floor(turn));
-          const float co = __builtin_amdgcn_cosf(part) * a.amplitude, si = __builtin_amdgcn_sinf(part) * a.amplitude;
-          x[e] = second ? fmaf(x[e], co, other * si) : fmaf(x[e], co, -(other * si));
+          for (int i = 0; i < 2; ++i) {
+            const uint2 four_rows = i ? hi : lo;
+            const int r4 = r + 8 * i;
+            if (r4 >= b.from && r4 + 4 <= end) {
+              *(uint2*)(d + 4 * i) = four_rows;
+            } else if (r4 + 4 > b.from && r4 < end) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (r4 + e >= b.from && r4 + e < end) d[4 * i + e] = (bf16_t)((e < 2 ? four_rows.x : four_rows.y) >> (16 * (e & 1)));
+            }
+          }
         }
       }
-      x16[y] = make_uint4(narrow2<F16>(x[0], x[1]), narrow2<F16>(x[2], x[3]), narrow2<F16>(x[4], x[5]), narrow2<F16>(x[6], x[7]));
     }
   }
+}
+
+// Queries and keys: 8 positions that lie side by side in a page (one page to look up, and a K store of 8 rows is a line) and one or
+// more heads there: the angles are worked out once for all of them.  A lane holds 8 features of a row, so head_dim / 8 lanes
+// hold a row.
+template <int HD, bool F16, int TURN, int G>
+__device__ inline void query_key_rows(const RotaryArgs& a, Block& b, int group, int lane, float* meet) {
+  constexpr int LANES = HD / 8, ROWS = 64 / LANES, STEPS = 8 / ROWS;  // rows at a time
+  constexpr int ANGLES = TURN == COPY ? 1 : TURN == PAIRS ? 4 : 8;
+  const PoolView& p = a.p;
+  const int c = lane & (LANES - 1), r0 = lane / LANES;
+  const int units = a.n_q_heads + p.n_kv_heads, unit0 = group * G;
+  size_t row[STEPS];
+  bool mine[STEPS];
 #pragma unroll
   for (int y = 0; y < STEPS; ++y) {
-    const int r = r0 + y * ROWS, t = t0 + r;
-    if (t < 0 || t >= a.tokens) continue;
-    const uint4 x = place[y] >= 0 ? x16[y] : make_uint4(0, 0, 0, 0);
-    if (what == 0) *(uint4*)(a.q_out + ((size_t)i * a.tokens + t) * a.q_out_stride + (size_t)h * HD + 8 * c) = x;
-    else if (at8 + r < l) *(uint4*)(tile + (size_t)(c >> 1) * 512 + (c & 1) * 256 + (((int)at8 & 31) + r) * 8) = x;
+    const int r = r0 + y * ROWS;
+    mine[y] = r >= b.from && r < b.to;
+    row[y] = (size_t)b.i * a.tokens + (mine[y] ? b.t0 + r : 0);
+  }
+  auto load = [&](uint4(&x)[STEPS], int unit) {
+    const bool is_q = unit < a.n_q_heads;
+    const bf16_t* src = (is_q ? a.q : a.k) + (size_t)(is_q ? unit : unit - a.n_q_heads) * HD + 8 * c;
+    const long long stride = is_q ? a.q_stride : a.kv_stride;
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y) x[y] = mine[y] ? *(const uint4*)(src + row[y] * stride) : make_uint4(0, 0, 0, 0);
+  };
+  // everything that has an address already is asked for first
+  uint4 all[G][STEPS];
+#pragma unroll
+  for (int k = 0; k < G; ++k) load(all[k], min(unit0 + k, units - 1));
+  const int half = a.dims >> 1;
+  double turns[ANGLES];
+  if constexpr (TURN != COPY) {
+#pragma unroll
+    for (int e = 0; e < ANGLES; ++e) {
+      const int f = TURN == PAIRS ? 8 * c + 2 * e : 8 * c + e, pair = TURN == PAIRS ? f >> 1 : f >= half ? f - half : f;
+      turns[e] = a.turns[f < a.dims ? pair : 0];
+    }
+  }
+  int place[STEPS];
+#pragma unroll
+  for (int y = 0; y < STEPS; ++y)
+    place[y] = !mine[y] ? -1 : a.places ? a.places[row[y]] : (int)min(b.at + r0 + y * ROWS, 0x7fffffffLL);
+  b.page = nullptr;
+  b.last = 0;
+  if (min(unit0 + G, units) > a.n_q_heads) find_page(a, b, 8, lane);
+
+  // the angles of this lane's rows and features
+  float co[STEPS][ANGLES], si[STEPS][ANGLES];
+  if constexpr (TURN != COPY) {
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y)
+#pragma unroll
+      for (int e = 0; e < ANGLES; ++e) {
+        const float part = (float)__builtin_amdgcn_fract((double)place[y] * turns[e]);
+        co[y][e] = __builtin_amdgcn_cosf(part) * a.amplitude;
+        si[y][e] = __builtin_amdgcn_sinf(part) * a.amplitude;
+        // the second of a pair turns the other way
+        if (TURN != PAIRS && 8 * c + e < half) si[y][e] = -si[y][e];
+      }
+  }
+
+#pragma unroll
+  for (int head = 0; head < G; ++head) {
+    const int unit = unit0 + head;
+    if (unit >= units) break;
+    uint4(&x16)[STEPS] = all[head];
+    const bool is_q = unit < a.n_q_heads;
+    const int h = is_q ? unit : unit - a.n_q_heads;
+    const bf16_t* gain = is_q ? a.q_gain : a.k_gain;
+    if (TURN != COPY || gain) {
+      float g8[8];
+      if (gain) {
+        const uint4 x = *(const uint4*)(gain + 8 * c);
+        widen<false>(x.x, g8[0], g8[1]);
+        widen<false>(x.y, g8[2], g8[3]);
+        widen<false>(x.z, g8[4], g8[5]);
+        widen<false>(x.w, g8[6], g8[7]);
+      }
+#pragma unroll
+      for (int y = 0; y < STEPS; ++y) {
+        float x[8];
+        widen<F16>(x16[y].x, x[0], x[1]);
+        widen<F16>(x16[y].y, x[2], x[3]);
+        widen<F16>(x16[y].z, x[4], x[5]);
+        widen<F16>(x16[y].w, x[6], x[7]);
+        if (gain) {
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+          const float scale = rsqrtf(row_sum<LANES>(sum) * (1.f / HD) + a.eps);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * scale * g8[e];
+        }
+        if constexpr (TURN == PAIRS) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (8 * c + 2 * e < a.dims) {
+              const float x0 = x[2 * e], x1 = x[2 * e + 1];
+              x[2 * e] = fmaf(x0, co[y][e], -(x1 * si[y][e]));
+              x[2 * e + 1] = fmaf(x1, co[y][e], x0 * si[y][e]);
+            }
+        } else if constexpr (TURN == HALVES) {
+          const int partner = lane + (8 * c < half ? half >> 3 : -(half >> 3));  // (of lanes beyond the rotated ones: nobody looks)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float other = __shfl(x[e], partner);
+            if (8 * c < a.dims) x[e] = fmaf(x[e], co[y][e], other * si[y][e]);
+          }
+        } else if constexpr (TURN == ANY_HALVES) {
+          float* const row32 = meet + (r0 + y * ROWS) * HD;
+          *(float4*)(row32 + 8 * c) = make_float4(x[0], x[1], x[2], x[3]);
+          *(float4*)(row32 + 8 * c + 4) = make_float4(x[4], x[5], x[6], x[7]);
+          asm volatile("" ::: "memory");  // (the order is the wave's own, if the compiler keeps it)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int f = 8 * c + e;
+            if (f < a.dims) x[e] = fmaf(x[e], co[y][e], row32[f < half ? f + half : f - half] * si[y][e]);
+          }
+          asm volatile("" ::: "memory");
+        }
+        x16[y] = make_uint4(narrow2<F16>(x[0], x[1]), narrow2<F16>(x[2], x[3]), narrow2<F16>(x[4], x[5]), narrow2<F16>(x[6], x[7]));
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y) {
+      if (!mine[y]) continue;
+      const int r = r0 + y * ROWS;
+      const uint4 x = place[y] >= 0 ? x16[y] : make_uint4(0, 0, 0, 0);
+      if (is_q) put<(G > 1)>(a.q_out + row[y] * a.q_out_stride + (size_t)h * HD + 8 * c, x);
+      else if (b.page && r < b.last) put<(G > 1)>(b.page + h * p.tile() + (size_t)(c >> 1) * 512 + (c & 1) * 256 + (((int)b.at & 31) + r) * 8, x);
+    }
   }
 }
+
+template <int HD, bool F16, int TURN, int G>
+__global__ __launch_bounds__(256, 4) void rotary_append_kernel(RotaryArgs a) {
+  __shared__ float4 meet[4][TURN == ANY_HALVES ? 8 * HD / 4 : 1];  // (the partners of a pair, where they are in no one lane)
+  const PoolView& p = a.p;
+  read_args(a.layer, a.n, a.tokens, a.seqs, a.pos, a.places, a.n_q_heads, a.q, a.k, a.v, a.q_stride, a.kv_stride, a.q_out,
+            a.q_out_stride, a.q_gain, a.k_gain, a.eps, a.dims, a.amplitude, a.turns, a.first, a.qk_groups, a.v_groups, a.qk_waves,
+            a.v_waves, p.data, p.refs, p.table, p.len, p.n_pages, p.max_seqs, p.max_pages, p.n_layers, p.n_kv_heads);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = a.first + blockIdx.x * 4 + w, per_entry = a.qk_waves + a.v_waves;  // (a call has less than 2^29 waves)
+  const int i = u / per_entry, k = u - i * per_entry;
+  if (i >= a.n) return;
+  Block b;
+  if (k < a.qk_waves) {
+    const int blk = k / a.qk_groups;
+    if (block_of(a, i, blk, 8, b)) query_key_rows<HD, F16, TURN, G>(a, b, k - blk * a.qk_groups, lane, (float*)meet[w]);
+  } else {
+    const int blk = (k - a.qk_waves) / a.v_groups;
+    if (block_of(a, i, blk, 16, b)) value_rows<HD, G>(a, b, k - a.qk_waves - blk * a.v_groups, lane);
+  }
+}
+
+// Waves that a call should have before they take more than one head each (8 per CU), us per layer with this many, half and twice
+// as many: 8 x 31 tokens of 32 heads 7.4, 10.0, 7.4; 4 x 1057 of 12 on 2 11.0, 13.0, 12.5; 64 x 1 of 32 6.8, 8.2, 7.4.
+constexpr int kWavesWanted = 2048;
 
 __global__ __launch_bounds__(64) void rotary_fill_kernel(int dims, double base, double factor, double original, double low,
                                                          double high, double* __restrict__ turns) {
@@ -252,23 +415,44 @@ int vlac_pages_append_rotated(const vlac_pages* pages, int layer, const int32_t*
   if ((uintptr_t)k % 16 || (uintptr_t)v % 16 || (uintptr_t)q_gain % 16 || (uintptr_t)k_gain % 16 ||
       (n_q_heads > 0 && ((uintptr_t)q % 16 || (uintptr_t)q_out % 16)))
     return VLAC_E_SHAPE;
-  RotaryArgs a = {pool_view(pages), layer, n, tokens, (tokens + 14) / 8, seqs, pos, places, n_q_heads, (const bf16_t*)q, (const bf16_t*)k,
+  RotaryArgs a = {pool_view(pages), layer, n, tokens, seqs, pos, places, n_q_heads, (const bf16_t*)q, (const bf16_t*)k,
                   (const bf16_t*)v, q_stride, kv_stride, (bf16_t*)q_out, q_out_stride, (const bf16_t*)q_gain, (const bf16_t*)k_gain, eps,
-                  rot ? rot->dims : 0, rot ? rot->layout == VLAC_ROTARY_PAIRS : 0, rot ? rot->amplitude : 1.f,
-                  rot ? rot->turns : nullptr, 0};
-  const long long waves = (long long)n * a.blocks * (n_q_heads + 2 * pages->n_kv_heads);
+                  rot ? rot->dims : 0, rot ? rot->amplitude : 1.f, rot ? rot->turns : nullptr, 0, 0, 0, 0, 0};
+  const int qk = n_q_heads + pages->n_kv_heads, blocks8 = (tokens + 14) / 8, blocks16 = (tokens + 30) / 16;
+  const long long work = (long long)n * blocks8 * qk;
+  const int per_wave = work >= 4 * kWavesWanted ? 4 : work >= 2 * kWavesWanted ? 2 : 1;
+  a.qk_groups = (qk + per_wave - 1) / per_wave;
+  a.v_groups = (pages->n_kv_heads + per_wave - 1) / per_wave;
+  a.qk_waves = blocks8 * a.qk_groups;
+  a.v_waves = blocks16 * a.v_groups;
+  const long long waves = (long long)n * (a.qk_waves + a.v_waves);
+  const int turn = !rot ? COPY : rot->layout == VLAC_ROTARY_PAIRS ? PAIRS : rot->dims % 16 == 0 ? HALVES : ANY_HALVES;
+  hipStream_t st = (hipStream_t)stream;
   // (a launch of 2^32 threads and more would run only what is left of them modulo 2^32)
   constexpr int kMost = 1 << 24;
-  hipStream_t st = (hipStream_t)stream;
   for (a.first = 0; a.first < waves; a.first += kMost) {
     const dim3 grid((unsigned)((std::min<long long>(waves - a.first, kMost) + 3) / 4));
-    if (pages->head_dim == 128) {
-      if (pages_f16(pages)) hipLaunchKernelGGL((rotary_append_kernel<128, true>), grid, dim3(256), 0, st, a);
-      else hipLaunchKernelGGL((rotary_append_kernel<128, false>), grid, dim3(256), 0, st, a);
-    } else {
-      if (pages_f16(pages)) hipLaunchKernelGGL((rotary_append_kernel<64, true>), grid, dim3(256), 0, st, a);
-      else hipLaunchKernelGGL((rotary_append_kernel<64, false>), grid, dim3(256), 0, st, a);
-    }
+    auto launch = [&](auto hd, auto f16, auto how, auto heads) {
+      hipLaunchKernelGGL((rotary_append_kernel<decltype(hd)::value, decltype(f16)::value, decltype(how)::value, decltype(heads)::value>), grid,
+                         dim3(256), 0, st, a);
+    };
+    auto by_heads = [&](auto hd, auto f16, auto how) {
+      if (per_wave == 4) launch(hd, f16, how, std::integral_constant<int, 4>{});
+      else if (per_wave == 2) launch(hd, f16, how, std::integral_constant<int, 2>{});
+      else launch(hd, f16, how, std::integral_constant<int, 1>{});
+    };
+    auto by_turn = [&](auto hd, auto f16) {
+      if (turn == COPY) by_heads(hd, f16, std::integral_constant<int, COPY>{});
+      else if (turn == PAIRS) by_heads(hd, f16, std::integral_constant<int, PAIRS>{});
+      else if (turn == HALVES) by_heads(hd, f16, std::integral_constant<int, HALVES>{});
+      else by_heads(hd, f16, std::integral_constant<int, ANY_HALVES>{});
+    };
+    auto typed = [&](auto hd) {
+      if (pages_f16(pages)) by_turn(hd, std::true_type{});
+      else by_turn(hd, std::false_type{});
+    };
+    if (pages->head_dim == 128) typed(std::integral_constant<int, 128>{});
+    else typed(std::integral_constant<int, 64>{});
   }
   return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
 }
