@@ -45,63 +45,77 @@ struct KeepArgs {
   int n, tokens;
 };
 
-// Whether entry i can be done, worked out by every workgroup that has to do with it: -> how many rows are kept, or -1.
-// from, to: where row k comes from and goes to, page * 32 + position in it (equal: it stays).
+// Whether entry i can be done, worked out by every workgroup that has to do with it: -> how many rows are kept, or -1; *stay: the first of
+// them that stay where they are (a path ascends, so all others move).  from, to: where row k comes from and goes to, page * 32 +
+// position in it.  A chain of reads (lists and path, length and table, counts of the pages), about 0.7 us each.
 constexpr int kKeep = 256;
-__device__ int keep_entry(const KeepArgs& a, int i, int* from, int* to, int* bad) {
+struct Rows { int from[VLAC_TREE_MAX_NODES], to[VLAC_TREE_MAX_NODES], bad, stay; };
+__device__ int keep_entry(const KeepArgs& a, int i, Rows& rows, int* stay) {
+  constexpr int PER = VLAC_TREE_MAX_NODES / kKeep;
   const PoolView& p = a.p;
   const int tid = threadIdx.x, s = a.seqs[i], p0 = a.pos[i], m = a.count[i];
+  int node[PER], before[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int k = u * kKeep + tid;
+    node[u] = k < a.tokens ? a.path[(size_t)i * a.tokens + k] : -1;
+    before[u] = k > 0 && k < a.tokens ? a.path[(size_t)i * a.tokens + k - 1] : -1;
+  }
   if (p0 < 0) return -1;
   const int l = checked_len(p, s);
-  if (tid == 0) *bad = l < 0 || m < 0 || m > a.tokens || (long long)p0 + a.tokens != l;
-  __syncthreads();
-  if (*bad) return -1;
+  if (tid == 0) {
+    rows.bad = l < 0 || m < 0 || m > a.tokens || (long long)p0 + a.tokens != l;
+    rows.stay = 0;
+  }
   bool wrong = false;
   for (int k = tid; k < i; k += kKeep) wrong |= a.seqs[k] == s && a.pos[k] >= 0;
-  for (int k = tid; k < m; k += kKeep) {
-    const int t = a.path[(size_t)i * a.tokens + k], before = k > 0 ? a.path[(size_t)i * a.tokens + k - 1] : -1;
-    int f = 0, g = 0;
-    if (t <= before || t < k || t >= a.tokens) {
+  __syncthreads();
+  if (rows.bad) return -1;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int k = u * kKeep + tid, t = node[u];
+    if (k >= m) break;
+    if (t <= before[u] || t < k || t >= a.tokens) {
       wrong = true;
-    } else if (t != k) {
+    } else if (t == k) {
+      atomicAdd(&rows.stay, 1);
+    } else {
       const int* row = p.table + (size_t)s * p.max_pages;
       const int fp = row[(p0 + t) / kPage], gp = row[(p0 + k) / kPage];
-      if ((unsigned)fp >= (unsigned)p.n_pages || (unsigned)gp >= (unsigned)p.n_pages || p.refs[gp] != 1) {
-        wrong = true;
-      } else {
-        f = fp * kPage + (p0 + t) % kPage;
-        g = gp * kPage + (p0 + k) % kPage;
-      }
+      rows.from[k] = fp * kPage + (p0 + t) % kPage;
+      rows.to[k] = gp * kPage + (p0 + k) % kPage;
+      wrong |= (unsigned)fp >= (unsigned)p.n_pages || (unsigned)gp >= (unsigned)p.n_pages || p.refs[min((unsigned)gp, p.n_pages - 1u)] != 1;
     }
-    from[k] = f;
-    to[k] = g;
   }
-  if (wrong) *bad = 1;
+  if (wrong) rows.bad = 1;
   __syncthreads();
-  return *bad ? -1 : m;
+  *stay = rows.stay;
+  return rows.bad ? -1 : m;
 }
 
 // The rows of the path, one behind the other.  A workgroup takes an entry, a layer and some kv heads; a thread takes 16 bytes of K of
 // every row (8 features), and a feature of V.  A row only moves down and rows are taken in ascending order, a thread's own
-// words: what is read was not written before.  Eight rows are asked for at a time.
+// words: what is read was not written before.  Eight rows are asked for at a time.  Bound by the lines that the layout touches: a position's K
+// lies in 16 lines of a head of 128, of which it has an eighth, its V in as many more.
 // Tables, counts and lengths stay as they are until the next launch; that this entry can be done is left for it in the pool's
 // scratch (is_dst of the sequence, zero between calls: the entry's number + 1).
 constexpr int kHeads = 4;  // of a work item
 __global__ __launch_bounds__(kKeep) void pages_keep_kernel(KeepArgs a, int head_groups, int items) {
-  __shared__ int from[VLAC_TREE_MAX_NODES], to[VLAC_TREE_MAX_NODES];
-  __shared__ int bad;
+  __shared__ Rows rows;
   const PoolView& p = a.p;
   const int hd = p.head_dim;
+  const int *from = rows.from, *to = rows.to;
   const size_t page = p.page(), tile = p.tile();
   for (int it = blockIdx.x; it < items; it += gridDim.x) {
     const int hg = it % head_groups, rest = it / head_groups, layer = rest % p.n_layers, i = rest / p.n_layers;
-    const int m = keep_entry(a, i, from, to, &bad);
+    int stay = 0;
+    const int m = keep_entry(a, i, rows, &stay);
     if (m >= 0 && threadIdx.x == 0 && hg == 0 && layer == 0) p.is_dst()[a.seqs[i]] = i + 1;
     const int h0 = hg * kHeads, heads = min(kHeads, p.n_kv_heads - h0);
     bf16_t* const k0 = p.data + ((size_t)layer * 2 * p.n_kv_heads + h0) * tile;
     bf16_t* const v0 = k0 + p.n_kv_heads * tile;
     auto move = [&](auto* base, auto at) {  // the rows' words that lie at(position) behind base, in their page
-      for (int r0 = 0; r0 < m; r0 += 8) {
+      for (int r0 = stay; r0 < m; r0 += 8) {
         std::decay_t<decltype(*base)> y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -111,7 +125,7 @@ __global__ __launch_bounds__(kKeep) void pages_keep_kernel(KeepArgs a, int head_
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int k = min(r0 + e, m - 1), t = to[k];
-          if (r0 + e < m && from[k] != t) base[(t >> 5) * (page * sizeof(bf16_t) / sizeof(*base)) + at(t & 31)] = y[e];
+          if (r0 + e < m) base[(t >> 5) * (page * sizeof(bf16_t) / sizeof(*base)) + at(t & 31)] = y[e];
         }
       }
     };
