@@ -117,6 +117,51 @@ __device__ inline int differs(const int* head, const Made& m) {
   return x;
 }
 
+// The masks of a tree's nodes, and their places in the text.  A workgroup takes an entry: the parents lie in LDS and every node
+// follows them up, twice: to see whether the way ends at the cached sequence, then, word by word (parents come before
+// their nodes, so the bits are met in descending order).  Bound by latency: the lists, then depth x an LDS round trip.
+struct TreeArgs {
+  const int* parents;  // nullptr: no trees
+  uint32_t* mask;
+  int* places;
+};
+__device__ inline void mask_entry(const PoolView& p, const int* seqs, const int* pos, int tokens, const TreeArgs& tree, int i, int* above) {
+  const int tid = threadIdx.x, words = mask_words(tokens);
+  const int p0 = pos[i], s = seqs[i];
+  for (int t = tid; t < tokens; t += blockDim.x) above[t] = tree.parents[(size_t)i * tokens + t];
+  const int l = checked_len(p, s);
+  const bool fits = p0 >= 0 && l >= 0 && (long long)p0 + tokens <= l;
+  for (int t = tid; t < tokens; t += blockDim.x)
+    if (above[t] < -2 || above[t] >= t) {
+      above[t] = -2;
+      if (fits) report(p, PAGES_BAD_ENTRY);
+    }
+  __syncthreads();
+  const int first = fits ? p0 % kPage : 0;  // bit of node 0
+  for (int t = tid; t < tokens; t += blockDim.x) {
+    const size_t row = (size_t)i * tokens + t;
+    int depth = 0, x = t, up = above[t];
+    while (up >= 0) {
+      ++depth;
+      x = up;
+      up = above[x];
+    }
+    const bool there = fits && up == -1;
+    if (tree.places) tree.places[row] = there ? p0 + depth : -1;
+    uint32_t* const out = tree.mask + row * words;
+    x = there ? t : -1;
+    for (int k = words - 1; k >= 0; --k) {
+      uint32_t bits = 0u;
+      while (x >= 0 && (first + x) / 32 == k) {
+        bits |= 1u << ((first + x) & 31);
+        x = above[x];
+      }
+      if (k == 0 && there) bits |= (1u << first) - 1u;  // cached positions of the same page
+      out[k] = bits;
+    }
+  }
+}
+
 struct PlanArgs {
   PoolView p;
   Made made;
@@ -126,6 +171,7 @@ struct PlanArgs {
   Ent* ent;
   Own* own;
   Item* item;
+  TreeArgs tree;
 };
 
 // Sums of two numbers over the threads before this one, and over all
@@ -172,6 +218,11 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_area, s_own, s_cols;
   __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
+  if (N <= 128 && blockIdx.x > 0) {  // (a tree's masks: beside the plan)
+    __shared__ int above[VLAC_TREE_MAX_NODES];
+    mask_entry(p, a.seqs, a.pos, a.tokens, a.tree, blockIdx.x - 1, above);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   read_args(a.seqs, a.pos, a.group, a.add, a.n, a.tokens, a.n_q_heads, a.part_tiles, a.max_items, a.head, a.ent, a.own,
             a.item, p.table, p.len, p.max_seqs, p.max_pages, p.n_kv_heads);
@@ -507,7 +558,8 @@ struct AttendArgs {
   const uint32_t* mask;  // trees: [n][tokens][mask_words]
 };
 
-// Which positions of tile kt a tree's node sees, for a query row whose entry's new positions begin at pos
+// Which positions of tile kt a tree's node sees, for a query row whose entry's new positions begin at pos (kt at most the entry's last
+// tile)
 __device__ inline uint32_t sees(const AttendArgs& a, int row, int pos, int kt) {
   const int x = kt - pos / kPage;
   return x < 0 ? ~0u : a.mask[(size_t)row * mask_words(a.tokens) + x];
@@ -1212,45 +1264,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) { join_p
 template <int HD, bool F16>
 __global__ __launch_bounds__(256) void attend_tree_join_kernel(AttendArgs a) { join_parts<HD, F16, true>(a); }
 
-// The masks of a tree's nodes, and their places in the text.  A workgroup takes an entry: the parents lie in LDS and every node
-// follows them up, twice: to see whether the way ends at the cached sequence, then, word by word (parents come before
-// their nodes, so the bits are met in descending order).  Bound by latency: the list, then depth x an LDS round trip.
-__global__ __launch_bounds__(256) void attend_tree_mask_kernel(PoolView p, const int* __restrict__ seqs, const int* __restrict__ pos,
-                                                             const int* __restrict__ parents, int tokens, uint32_t* __restrict__ mask,
-                                                             int* __restrict__ out_places) {
+__global__ __launch_bounds__(256) void attend_tree_mask_kernel(PoolView p, const int* __restrict__ seqs, const int* __restrict__ pos, int tokens,
+                                                             TreeArgs tree) {
   __shared__ int above[VLAC_TREE_MAX_NODES];
-  const int i = blockIdx.x, tid = threadIdx.x, words = mask_words(tokens);
-  const int p0 = pos[i], l = checked_len(p, seqs[i]);
-  const bool fits = p0 >= 0 && l >= 0 && (long long)p0 + tokens <= l;
-  for (int t = tid; t < tokens; t += 256) {
-    const int x = parents[(size_t)i * tokens + t];
-    if (fits && (x < -2 || x >= t)) report(p, PAGES_BAD_ENTRY);
-    above[t] = x < -2 || x >= t ? -2 : x;
-  }
-  __syncthreads();
-  const int first = fits ? p0 % kPage : 0;  // bit of node 0
-  for (int t = tid; t < tokens; t += 256) {
-    const size_t row = (size_t)i * tokens + t;
-    int depth = 0, x = t, up = above[t];
-    while (up >= 0) {
-      ++depth;
-      x = up;
-      up = above[x];
-    }
-    const bool there = fits && up == -1;
-    if (out_places) out_places[row] = there ? p0 + depth : -1;
-    uint32_t* const out = mask + row * words;
-    x = there ? t : -1;
-    for (int k = words - 1; k >= 0; --k) {
-      uint32_t bits = 0u;
-      while (x >= 0 && (first + x) / 32 == k) {
-        bits |= 1u << ((first + x) & 31);
-        x = above[x];
-      }
-      if (k == 0 && there) bits |= (1u << first) - 1u;  // cached positions of the same page
-      out[k] = bits;
-    }
-  }
+  mask_entry(p, seqs, pos, tokens, tree, blockIdx.x, above);
 }
 
 bool sizes_ok(const vlac_pages* p, int n, int tokens, int n_q_heads) {
@@ -1277,22 +1294,29 @@ size_t attend_workspace(const PoolView& p, int n, int tokens, int n_q_heads) {
 }
 
 static void launch_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
-                        const int* group, void* ws, bool tree, hipStream_t st) {
+                        const int* group, void* ws, const int* parents, int* places, hipStream_t st) {
+  const bool tree = parents != nullptr;
   const Layout l = layout_of(p, n, tokens, n_q_heads, tree);
   char* b = (char*)ws;
+  const TreeArgs masks = {parents, (uint32_t*)(b + l.mask), places};
   const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads, tree), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles,
-                      (int)l.max_items, l.few ? 16 : 32, (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item)};
+                      (int)l.max_items, l.few ? 16 : 32, (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item),
+                      masks};
   // (4 waves or 16: one token of 2 candidates 7.3 and 8.2 us, 16 candidates x 56 tokens over 1057 positions 8.0 and 8.6; 48
   // candidates with tables of 1027 pages 40 and 20 when both were tried.  More entries than 128 are a second round for 4 waves.)
-  if (n <= 128 && (long long)n * p.max_pages <= 4096)
-    hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(1), dim3(256), 0, st, a);
-  else
+  // A tree's masks are made by further workgroups of the small kernel, by a launch of their own beside the large one (whose LDS would
+  // leave a CU to each of them).
+  if (n <= 128 && (long long)n * p.max_pages <= 4096) {
+    hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(tree ? 1 + n : 1), dim3(256), 0, st, a);
+  } else {
     hipLaunchKernelGGL((attend_plan_kernel<1024, VLAC_PAGES_MAX_LIST>), dim3(1), dim3(1024), 0, st, a);
+    if (tree) hipLaunchKernelGGL(attend_tree_mask_kernel, dim3(n), dim3(256), 0, st, p, seqs, pos, tokens, masks);
+  }
 }
 
 void launch_attend_plan(const PoolView& p, const int* seqs, const int* pos, int add, int n, int tokens, int n_q_heads,
                         const int* group, void* ws, hipStream_t st) {
-  launch_plan(p, seqs, pos, add, n, tokens, n_q_heads, group, ws, false, st);
+  launch_plan(p, seqs, pos, add, n, tokens, n_q_heads, group, ws, nullptr, nullptr, st);
 }
 
 static void launch_layer(const PoolView& p, bool f16, int layer, int n, int tokens, int n_q_heads, const AttendIo& io, void* ws,
@@ -1376,11 +1400,7 @@ int vlac_attend_tree_plan(const vlac_pages* pages, const int32_t* seqs, const in
   const int rc = check_attend(pages, n, tokens, n_q_heads, workspace, workspace_bytes, true);
   if (rc != VLAC_OK || n == 0) return rc;
   if (!seqs || !pos || !parents) return VLAC_E_NULL;
-  hipStream_t st = (hipStream_t)stream;
-  const PoolView p = pool_view(pages);
-  launch_plan(p, seqs, pos, 0, n, tokens, n_q_heads, group, workspace, true, st);
-  uint32_t* mask = (uint32_t*)((char*)workspace + layout_of(p, n, tokens, n_q_heads, true).mask);
-  hipLaunchKernelGGL(attend_tree_mask_kernel, dim3(n), dim3(256), 0, st, p, seqs, pos, parents, tokens, mask, out_places);
+  launch_plan(pool_view(pages), seqs, pos, 0, n, tokens, n_q_heads, group, workspace, parents, out_places, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
 }
 

@@ -173,6 +173,43 @@ def test_against_the_definition(hq, hkv, hd, operand, layout, dims, norm, tokens
     assert torch.equal(s.data, after)
 
 
+@pytest.mark.parametrize("hq,hkv,hd,n,tokens", [(31, 6, 64, 5, 200), (30, 7, 128, 3, 601), (9, 2, 128, 80, 33), (5, 2, 64, 3, 3400),
+                                                   (1, 13, 128, 300, 9)])
+@pytest.mark.parametrize("operand", [0, 1])
+@pytest.mark.parametrize("layout,dims,norm", [(V.ROTARY_HALF, 64, "qk"), (V.ROTARY_PAIRS, 64, ""), (V.ROTARY_HALF, 50, "k"), (None, 0, "q")])
+def test_calls_whose_waves_take_several_heads(hq, hkv, hd, n, tokens, operand, layout, dims, norm):
+    """4096 and 8192 heads of 8 positions and more; numbers of heads that the waves do not divide."""
+    import torch
+    assert n * ((tokens + 14) // 8) * (hq + hkv) >= 4096
+    starts = [(37 * i + 5) % 90 for i in range(n)]
+    s = Setup(hkv, hd, operand, starts, tokens, layers=1, seed=tokens)
+    rot = None if layout is None else V.rotary(dims, layout, 1e4)
+    qkv = s.randn((n, tokens, hq + 2 * hkv, hd))
+    q, k, v = qkv.split((hq, hkv, hkv), 2)
+    gains = [(1 + 0.3 * torch.randn(hd, generator=s.g, device=DEV)).bfloat16() if w in norm else None for w in "qk"]
+    out = torch.empty((n, tokens, hq, hd), dtype=s.dt, device=DEV)
+    before = s.data.clone()
+    call(s, 0, rot, None, hq, q, k, v, out, gains)
+    assert V.vlac_pages_check(s.pool, check=False) == OK
+    places = torch.tensor(starts, device=DEV)[:, None] + torch.arange(tokens, device=DEV)
+    table = s.pool.tensors[2].long()
+    page, r = table[torch.arange(n, device=DEV)[:, None], places // PAGE], places % PAGE
+    ka, va = (torch.tensor(f(hd), device=DEV)[r] for f in (k_tile_at, v_tile_at))          # [n, tokens, hd]
+    kk, vv = (torch.gather(s.data[:, 0, w][page], 3, at[:, :, None, :].expand(-1, -1, hkv, -1)).view(s.dt) for w, at in ((0, ka), (1, va)))
+    assert torch.equal(vv, v)
+    spec = None if rot is None else (dims, layout == V.ROTARY_PAIRS, 1.0, rot.tensors[0])
+    for x, gain, got in ((q, gains[0], out), (k, gains[1], kk)):
+        want, err = definition(x, places, spec, gain, 1e-5)
+        near(got, want, err, s.dt)
+    again = s.data.clone()                                      # nothing else was written
+    for w, at in ((0, ka), (1, va)):
+        again[:, 0, w][page[..., None, None], torch.arange(hkv, device=DEV)[:, None], at[:, :, None, :]] = \
+            before[:, 0, w][page[..., None, None], torch.arange(hkv, device=DEV)[:, None], at[:, :, None, :]]
+    assert torch.equal(again, before)
+    call(s, 0, rot, None, hq, q, k, v, q, gains)                # in place
+    assert torch.equal(q.contiguous().view(torch.int16), out.view(torch.int16))
+
+
 @pytest.mark.parametrize("operand,hd", [(1, 128), (0, 64)])
 @pytest.mark.parametrize("layout", [V.ROTARY_HALF, V.ROTARY_PAIRS])
 def test_places_of_its_own(operand, hd, layout):
