@@ -70,8 +70,10 @@ struct Layout {
   bool few;    // blocks of up to 16 columns
 };
 // Words of a tree node's mask: bit b of word x says whether the node sees position 32 (pos / 32 + x) + b; its slots may
-// begin at the last position of a page.
+// begin at the last position of a page.  One more word says whether there is such a node (of the row alone, so that it can be
+// asked for before the entry's position is known).
 __host__ __device__ inline int mask_words(int tokens) { return (tokens + 62) / 32; }
+__host__ __device__ inline int mask_row(int tokens) { return mask_words(tokens) + 1; }
 
 inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads, bool tree) {
   Layout l;
@@ -98,7 +100,7 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads, boo
   l.ml = l.item + up(sizeof(Item) * l.max_items);
   l.o = l.ml + (size_t)l.part_tiles * 64 * sizeof(float2);
   l.mask = l.o + (size_t)l.part_tiles * 32 * p.head_dim * sizeof(float);
-  l.total = l.mask + (tree ? up((size_t)n * tokens * mask_words(tokens) * sizeof(uint32_t)) : 0);
+  l.total = l.mask + (tree ? up((size_t)n * tokens * mask_row(tokens) * sizeof(uint32_t)) : 0);
   return l;
 }
 
@@ -148,7 +150,8 @@ __device__ inline void mask_entry(const PoolView& p, const int* seqs, const int*
     }
     const bool there = fits && up == -1;
     if (tree.places) tree.places[row] = there ? p0 + depth : -1;
-    uint32_t* const out = tree.mask + row * words;
+    uint32_t* const out = tree.mask + row * mask_row(tokens);
+    out[words] = there;
     x = there ? t : -1;
     for (int k = words - 1; k >= 0; --k) {
       uint32_t bits = 0u;
@@ -555,19 +558,23 @@ struct AttendArgs {
   int kc_out;
   int layer, n, tokens, n_q_heads;
   float scale_log2e;
-  const uint32_t* mask;  // trees: [n][tokens][mask_words]
+  const uint32_t* mask;  // trees: [n][tokens][mask_row]
 };
 
 // Which positions of tile kt a tree's node sees, for a query row whose entry's new positions begin at pos (kt at most the entry's last
 // tile)
 __device__ inline uint32_t sees(const AttendArgs& a, int row, int pos, int kt) {
   const int x = kt - pos / kPage;
-  return x < 0 ? ~0u : a.mask[(size_t)row * mask_words(a.tokens) + x];
+  return x < 0 ? ~0u : a.mask[(size_t)row * mask_row(a.tokens) + x];
 }
-// ... and whether there is such a node: it sees itself
-__device__ inline bool is_there(const AttendArgs& a, int row, int pos) {
-  const int self = pos % kPage + row % a.tokens;
-  return a.mask[(size_t)row * mask_words(a.tokens) + self / kPage] >> (self & 31) & 1;
+// (The word is asked for ahead, with the page's values, and where it is not needed as well: what is asked for later is waited for with
+// everything before it.)
+__device__ inline uint32_t mask_word(const AttendArgs& a, int row, int pos, int kt) {
+  return a.mask[(size_t)row * mask_row(a.tokens) + min(max(kt - pos / kPage, 0), mask_words(a.tokens) - 1)];
+}
+// ... and whether there is such a node
+__device__ inline uint32_t is_there(const AttendArgs& a, int row) {
+  return a.mask[(size_t)row * mask_row(a.tokens) + mask_words(a.tokens)];
 }
 
 template <bool F16>
@@ -580,6 +587,20 @@ __device__ inline uint32_t pack2(float lo, float hi) {
     return f2bf2(lo, hi);
   }
 }
+
+// Maximum and sum over a lane and the one 32 (16) further on, in both, by swaps between the halves (quarters) of two registers:
+// an instruction where a shuffle is a trip through LDS, of which a tile's chain has two.  (An exchange of the same two values: the same bits.)
+struct Both { float a, b; };
+__device__ inline Both over32(float x) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return {__uint_as_float(s[0]), __uint_as_float(s[1])};
+}
+__device__ inline Both over16(float x) {
+  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return {__uint_as_float(s[0]), __uint_as_float(s[1])};
+}
+__device__ inline float max_of(const Both& x) { return fmaxf(x.a, x.b); }
+__device__ inline float sum_of(const Both& x) { return x.a + x.b; }
 
 // How far above a column's maximum (log2) the reference point of its exponentials stands.  In fp32 a sum of weights times values of
 // bf16 would pass 2^128 where V is near the end of the type: with weights of up to 2^(8 - 32) and at most 2^20 positions it
@@ -665,7 +686,7 @@ __device__ __forceinline__ void attend_columns(const AttendArgs& a) {
     const int h = hk * grp + ci - ti * grp;
     const Ent mine = a.ent[e0 + ei];
     const int last = mine.pos + ti;  // its last visible position
-    const bool valid = c < cols_end && mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos));
+    const uint32_t there = TREE ? is_there(a, row) : 1u;
     uint4 qf[NC];
     {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)NC * 512 + (size_t)(((row & 31) + 32 * g) << 3)
@@ -725,7 +746,7 @@ __device__ __forceinline__ void attend_columns(const AttendArgs& a) {
       float tmax = -INFINITY;
 #pragma unroll
       for (int x = 0; x < 16; ++x) tmax = fmaxf(tmax, s[x]);
-      tmax = fmaf(fmaxf(tmax, __shfl_xor(tmax, 32)), a.scale_log2e, kAbove<F16>);  // (m is in units of log2)
+      tmax = fmaf(max_of(over32(tmax)), a.scale_log2e, kAbove<F16>);  // (m is in units of log2)
       float alpha = 1.f;
       if (tmax > m + 8.f) {
         alpha = __builtin_amdgcn_exp2f(m - tmax);  // (the first time 2^-inf = 0)
@@ -839,7 +860,7 @@ __device__ __forceinline__ void attend_columns(const AttendArgs& a) {
         for (int x = 0; x < 16; ++x) worst = fmaf(o[ib][x], 0.f, worst);
       if (!__any(worst != 0.f)) break;
     }
-    l += __shfl_xor(l, 32);
+    l = sum_of(over32(l));
     if (__builtin_expect(__any(odd), 0)) {
       // key by key, added where it is seen
       for (int i = n_shared; i < n_steps; ++i) {
@@ -923,7 +944,7 @@ __device__ __forceinline__ void attend_columns(const AttendArgs& a) {
         } else if (c < cols_end) {
           averages<F16>(x, 1.f / L);
 #pragma unroll
-          for (int r = 0; r < R; r += 4) store_out<HD, F16>(a, row, feature_of<HD>(h, (r0 + r) / 4, g), x + r, valid);
+          for (int r = 0; r < R; r += 4) store_out<HD, F16>(a, row, feature_of<HD>(h, (r0 + r) / 4, g), x + r, mine.seq >= 0 && there != 0);
         }
       }
       __syncthreads();  // (the next item parks here)
@@ -946,7 +967,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_tree_kernel(AttendArgs a) 
 // token of 8 candidates over 288 positions, 32 heads of 128, 6.8 us; 2 groups of up to 8 x 8 tokens over 601 (36 MB) 11.6.
 template <int HD, bool F16, bool TREE>
 __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
-  constexpr int NB = HD / 32, NF = HD / 16, U = 2;
+  constexpr int NB = HD / 32, NF = HD / 16;
   __shared__ float park[kWaves][2 + 4 * NF][64];
   const PoolView& p = a.p;
   read_args(a.head, a.item, a.ent, a.q, a.q_stride, a.out, a.kc_out, a.layer, a.tokens, a.n_q_heads, a.scale_log2e, p.data, p.table,
@@ -976,7 +997,7 @@ __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
     const int h = hk * grp + ci - ti * grp;
     const Ent mine = a.ent[e0 + ei];
     const int last = mine.pos + ti;  // its last visible position
-    const bool valid = c < cols_end && mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos));
+    const uint32_t there = TREE ? is_there(a, row) : 1u;
     uint4 qf[NB];
     {
       const bf16_t* q = a.q_stride < 0 ? a.q + ((size_t)(row >> 5) * a.n_q_heads + h) * (size_t)(HD / 16) * 512 + (size_t)((row & 31) << 3) + half
@@ -1041,82 +1062,96 @@ __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
     auto weights = [&](const float(&s)[8]) {
       return make_uint4(pack2<F16>(s[0], s[1]), pack2<F16>(s[2], s[3]), pack2<F16>(s[4], s[5]), pack2<F16>(s[6], s[7]));
     };
+    // Two tiles in registers: while one is worked on the other is on its way.
+    struct Tile { uint4 k[2 * NB], v[NF]; uint32_t word; };
+    auto load_tile = [&](Tile& t, int i) __attribute__((always_inline)) {
+      const bf16_t* from = tile_of(i);
+      load_k(t.k, from);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) t.v[f] = *(const uint4*)v_at(from, f);
+      if constexpr (TREE) t.word = mask_word(a, row, mine.pos, __builtin_amdgcn_readlane(st_what, i) & 0xffff);
+      __builtin_amdgcn_sched_barrier(0);
+    };
     bool odd = false;
+    auto work = [&](Tile& t, int first, int i, int care) __attribute__((always_inline)) {
+        const bool own = first + i >= n_shared;
+        const int what = __builtin_amdgcn_readlane(st_what, i), kt = what & 0xffff;
+        const int held = __builtin_amdgcn_readlane(st_page, i) >> 24;  // positions of an own page that hold a token
+        float s[8];
+        scores(t.k, s);
+        if (own) {
+          if constexpr (TREE) {
+            const uint32_t see = ei == what >> 16 ? (kt < mine.pos / kPage ? ~0u : t.word) >> first_key : 0u;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s[x] = see >> (8 * (x >> 2) + (x & 3)) & 1 ? s[x] : -INFINITY;
+          } else {
+            const int see = ei == what >> 16 ? last - 32 * kt - first_key : -1;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
+          }
+        }
+        // (the reference point as above)
+        float tmax = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+        tmax = max_of(over16(tmax));
+        tmax = fmaf(max_of(over32(tmax)), a.scale_log2e, kAbove<F16>);
+        float alpha = 1.f;
+        if (tmax > m + 8.f) {
+          alpha = __builtin_amdgcn_exp2f(m - tmax);
+          m = tmax;
+        }
+        const float m_use = m == -INFINITY ? 0.f : m;
+        float psum = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -m_use));
+          psum += s[x];
+        }
+        l = fmaf(l, alpha, psum);
+        const uint4 pb = weights(s);
+        if (__any(alpha != 1.f)) {
+#pragma unroll
+          for (int f = 0; f < NF; ++f) o[f] *= alpha;
+        }
+        if (own && (care || held < kPage)) {
+          // V of positions that hold no token may be anything
+#pragma unroll
+          for (int f = 0; f < NF; ++f) {
+            uint32_t* x = (uint32_t*)&t.v[f];
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const int kp = first_key + 8 * (d >> 1) + 2 * (d & 1);
+              const uint32_t far = far_values<F16>(x[d], care, care);
+              const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
+              odd |= (far & seen) != 0;
+              x[d] &= seen & ~far;
+            }
+          }
+        }
+#pragma unroll
+        for (int f = 0; f < NF; ++f) o[f] = mfma16<F16>(t.v[f], pb, o[f]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
     for (int care = 0; care < 2; ++care) {  // (as above: twice only where a column comes out infinite or NaN)
       if (care) clear();
       for (int first = 0; first < n_steps; first += 64) {
         load_steps(first);
         const int n64 = min(n_steps - first, 64);
-        for (int i = 0; i < n64; i += U) {
-          uint4 kf[U][2 * NB], vf[U][NF];
-#pragma unroll
-          for (int u = 0; u < U; ++u) load_k(kf[u], i + u < n64 ? tile_of(min(i + u, n64 - 1)) : kv);
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const bf16_t* t = i + u < n64 ? tile_of(min(i + u, n64 - 1)) : kv;
-#pragma unroll
-            for (int f = 0; f < NF; ++f) vf[u][f] = *(const uint4*)v_at(t, f);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            if (i + u >= n64) break;
-            const bool own = first + i + u >= n_shared;
-            const int what = __builtin_amdgcn_readlane(st_what, min(i + u, 63)), kt = what & 0xffff;
-            const int held = __builtin_amdgcn_readlane(st_page, min(i + u, 63)) >> 24;  // positions of an own page that hold a token
-            float s[8];
-            scores(kf[u], s);
-            if (own) {
-              if constexpr (TREE) {
-                const uint32_t see = ei == what >> 16 ? sees(a, row, mine.pos, kt) >> first_key : 0u;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) s[x] = see >> (8 * (x >> 2) + (x & 3)) & 1 ? s[x] : -INFINITY;
-              } else {
-                const int see = ei == what >> 16 ? last - 32 * kt - first_key : -1;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) s[x] = 8 * (x >> 2) + (x & 3) <= see ? s[x] : -INFINITY;
-              }
-            }
-            // (the reference point as above)
-            float tmax = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-            tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
-            tmax = fmaf(fmaxf(tmax, __shfl_xor(tmax, 32)), a.scale_log2e, kAbove<F16>);
-            float alpha = 1.f;
-            if (tmax > m + 8.f) {
-              alpha = __builtin_amdgcn_exp2f(m - tmax);
-              m = tmax;
-            }
-            const float m_use = m == -INFINITY ? 0.f : m;
-            float psum = 0.f;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -m_use));
-              psum += s[x];
-            }
-            l = fmaf(l, alpha, psum);
-            const uint4 pb = weights(s);
-            if (__any(alpha != 1.f)) {
-#pragma unroll
-              for (int f = 0; f < NF; ++f) o[f] *= alpha;
-            }
-            if (own && (care || held < kPage)) {
-              // V of positions that hold no token may be anything
-#pragma unroll
-              for (int f = 0; f < NF; ++f) {
-                uint32_t* x = (uint32_t*)&vf[u][f];
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                  const int kp = first_key + 8 * (d >> 1) + 2 * (d & 1);
-                  const uint32_t far = far_values<F16>(x[d], care, care);
-                  const uint32_t seen = kp + 1 < held ? ~0u : kp < held ? 0xffffu : 0u;
-                  odd |= (far & seen) != 0;
-                  x[d] &= seen & ~far;
-                }
-              }
-            }
-#pragma unroll
-            for (int f = 0; f < NF; ++f) o[f] = mfma16<F16>(vf[u][f], pb, o[f]);
-          }
+        Tile t0, t1;
+        load_tile(t0, 0);
+        int i = 0;
+        for (; i + 2 < n64; i += 2) {
+          load_tile(t1, i + 1);
+          work(t0, first, i, care);
+          load_tile(t0, i + 2);
+          work(t1, first, i + 1, care);
+        }
+        // (the last one or two: no load that is not used, and no branch around one that others wait behind)
+        if (i + 1 < n64) {
+          load_tile(t1, i + 1);
+          work(t0, first, i, care);
+          work(t1, first, i + 1, care);
+        } else {
+          work(t0, first, i, care);
         }
       }
       if (care) break;
@@ -1127,8 +1162,7 @@ __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
         for (int e = 0; e < 4; ++e) worst = fmaf(o[f][e], 0.f, worst);
       if (!__any(worst != 0.f)) break;
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    l = sum_of(over32(sum_of(over16(l))));
     if (__builtin_expect(__any(odd), 0)) {
       // key by key, added where it is seen
       for (int i = n_shared; i < n_steps; ++i) {
@@ -1189,7 +1223,7 @@ __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
         for (int e = 0; e < 4; ++e) x[e] = fmaf(f, park[y][2 + 4 * w + e][lane], x[e]);
       }
       averages<F16>(x, 1.f / L);
-      store_out<HD, F16>(a, row, h * HD + 16 * w + 4 * q4, x, valid);
+      store_out<HD, F16>(a, row, h * HD + 16 * w + 4 * q4, x, mine.seq >= 0 && there != 0);
     }
     __syncthreads();  // (the next item parks here)
   }
@@ -1254,7 +1288,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a) {
       averages<F16>(y, 1.f / L);
       const int row = (e0 + ei) * a.tokens + ti;
       const Ent mine = a.ent[e0 + ei];
-      store_out<HD, F16>(a, row, feature_of<HD>(hk * grp + ci - ti * grp, quad, g), y, mine.seq >= 0 && (!TREE || is_there(a, row, mine.pos)));
+      store_out<HD, F16>(a, row, feature_of<HD>(hk * grp + ci - ti * grp, quad, g), y, mine.seq >= 0 && (!TREE || is_there(a, row) != 0));
     }
   }
 }
