@@ -517,7 +517,8 @@ int vlac_choose_tokens(const float* logits, int rows, int vocab, int64_t stride,
 
 /* The path through each tree on which the drafts are what was chosen: it begins at node 0 (whose token is known: the one that
  * was chosen last and is not in the cache yet) and goes on, from node t, to the first node that follows t and whose drafted
- * token is chosen[t].  drafted, chosen: device int32 [n, tokens] (chosen: what the decoder picks after each node).
+ * token is chosen[t].  drafted, chosen: device int32 [n, tokens] (chosen: what the decoder picks after each node; a negative choice,
+ * vlac_choose_tokens' where nothing is allowed, is followed by none).
  * out_path: device int32 [n, tokens]: the nodes of the path, ascending, then -1; out_count: device int32 [n]: how many
  * (0 if there is no node 0); out_token: device int32 [n]: the token chosen after the last of them (-1 if there is none), the root of
  * the next tree.  n <= VLAC_PAGES_MAX_LIST.  The outputs overlap neither the inputs nor each other. */

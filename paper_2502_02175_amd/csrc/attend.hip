@@ -22,9 +22,11 @@
 //   waves of 512 registers: 42, one wave per SIMD does not hide its own softmax; two per wave in 8 waves, queries in LDS: 36 to
 //   46, no registers are left for K and V to be asked for ahead.)
 // * short lists: the chain launch arguments - item - tables - pages, 2.6 us to the first product, then 1.4 us for every tile of
-//   a wave (one after the other here; two at a time in the kernel for few columns), 1.5 us to meet and store: 12 query heads on 2 kv
-//   heads, 32 groups of up to 8 candidates over 304 positions, bf16, 13 MB: 10 us, 8.5 with few columns; two candidates over 80
-//   positions, 4 heads of 64: 5.5 and 5.2.
+//   a wave (one after the other here; the next one on its way meanwhile in the kernel for few columns), 1.5 us to meet and store: 12 query heads on 2 kv
+//   heads, 32 groups of up to 8 candidates over 304 positions, bf16, 13 MB: 10 us, 8.2 with few columns; two candidates over 80
+//   positions, 4 heads of 64: 5.5 and 5.0.
+// Trees of drafted tokens are the same with another mask: a node sees the cached positions and the nodes above it, a word of
+// bits per page of its own (32 trees of 24 nodes, 12 on 2 heads, over 304 positions 11.4 us, 2 of 64 over 32801 179 and 6.3 to join).
 #include <algorithm>
 #include <type_traits>
 
@@ -85,7 +87,7 @@ inline Layout layout_of(const PoolView& p, int n, int tokens, int n_q_heads, boo
   // layer with up to 64 columns, 10.4 with more; 2 groups of up to 8 x 8 tokens over 601 11.9 and 14.7.
   l.parts = least < 2 * kCus && p.max_pages > kLong;
   // Blocks of up to 16 columns where one round of the chip holds all of them: 6.8 us, and 8.1 with blocks of 32, for 8 candidates
-  // over 288 positions (32 heads of 128), 14.7 and 16.3 for 60 over 300, 19.2 and 21.3 for 100.  In more than a round the pages
+  // over 288 positions (32 heads of 128), 12.7 and 16.3 for 60 over 300, 17.3 and 21.3 for 100.  In more than a round the pages
   // are read too often: 150 over 300 34.1 and 28.1, grouped queries, 120 groups of up to 8 over 304, 24.7 and 21.3.
   l.few = !l.parts && cols <= (size_t)16 * n && (cols + 15) / 16 * p.n_kv_heads <= kCus;
   const size_t max_blocks = (l.few ? (cols + 15) / 16 * p.n_kv_heads : least) + (size_t)n * p.n_kv_heads;  // (a group ends in a block of its own)
@@ -961,10 +963,12 @@ template <int HD, bool F16>
 __global__ __launch_bounds__(64 * kWaves) void attend_tree_kernel(AttendArgs a) { attend_columns<HD, F16, true>(a); }
 
 // The same for short lists of blocks of up to 16 columns, no parts: products of 16 x 16 x 32, half the registers per column
-// block, and so two tiles at a time per wave.  A row of K is the key that the second product wants there: the row m = 4 * q + e of
-// product rb is key 16 * (q >> 1) + 8 * rb + 4 * (q & 1) + e, so that the 8 scores of a lane are, in order, the 8 weights that it owes
-// as the second operand, for the 16 bytes of V that lie together in the page.  Bound by latency, then by what a CU fetches: one
-// token of 8 candidates over 288 positions, 32 heads of 128, 6.8 us; 2 groups of up to 8 x 8 tokens over 601 (36 MB) 11.6.
+// block, and so room for two tiles per wave, one of which is on its way while the other is worked on.  A row of K is the key that the
+// second product wants there: the row m = 4 * q + e of product rb is key 16 * (q >> 1) + 8 * rb + 4 * (q & 1) + e, so that the 8 scores
+// of a lane are, in order, the 8 weights that it owes as the second operand, for the 16 bytes of V that lie together in the page.
+// Bound by latency, then by what a CU fetches and a tile's chain of instructions (2200 cycles or so either): one token of 8 candidates over
+// 288 positions, 32 heads of 128, 6.8 us; 60 over 300 12.7; 2 groups of up to 8 x 8 tokens over 601 (36 MB) 11.9; 8 trees of 8 nodes over
+// 1057 11.2.  (Both tiles asked for together, then both worked on: 60 over 300 13.9, 8 trees 12.6.)
 template <int HD, bool F16, bool TREE>
 __device__ __forceinline__ void attend_few_columns(const AttendArgs& a) {
   constexpr int NB = HD / 32, NF = HD / 16;

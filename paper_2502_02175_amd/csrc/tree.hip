@@ -24,7 +24,7 @@ __global__ __launch_bounds__(kAccept) void tree_accept_kernel(const int* __restr
   __syncthreads();
   for (int t = tid; t < tokens; t += kAccept) {
     const int up = parents[at + t];
-    if (t > 0 && up >= 0 && up < t && drafted[at + t] == pick[up]) atomicMin(&next[up], t);
+    if (t > 0 && up >= 0 && up < t && pick[up] >= 0 && drafted[at + t] == pick[up]) atomicMin(&next[up], t);
   }
   __syncthreads();
   if (tid == 0) {

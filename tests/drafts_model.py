@@ -46,7 +46,7 @@ def accept(parents, drafted, chosen):
         return [], -1
     path = [0]
     while True:
-        more = [t for t in range(1, len(parents)) if parents[t] == path[-1] and parents[t] < t and drafted[t] == chosen[path[-1]]]
+        more = [t for t in range(1, len(parents)) if parents[t] == path[-1] and parents[t] < t and drafted[t] == chosen[path[-1]] >= 0]
         if not more:
             return path, chosen[path[-1]]
         path.append(more[0])

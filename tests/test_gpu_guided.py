@@ -120,6 +120,45 @@ def test_only_the_bins_of_an_action():
         gm.close()
 
 
+def test_captured_and_replayed():
+    """A graph of fork, guided decoding and release, replayed with other masks and first tokens in its buffers."""
+    import torch
+    cfg, L, n_new, n = synth.CONFIGS["tiny"], 40, 5, 3
+    gm = GpuModel(cfg, seed=5, max_batch=4, max_seq=64, std=0.05)
+    try:
+        gm.prefill(synth.round_bf16(np.random.default_rng(1).standard_normal((1, L, cfg.d_model))), 32)
+        pool = V.new_pages(cfg.n_layers, cfg.n_kv_heads, cfg.head_dim, 1, 20, 5, 3, DEV)
+        V.vlac_pages_import(gm.ctx, gm.kv, 1, L, pool, i32([0]))
+        rng = np.random.default_rng(4)
+        src, seqs, first = i32([0] * n), i32([1, 2, 3]), i32([0] * n)
+        allowed = torch.full((n * n_new, cfg.vocab // 32), -1, dtype=torch.int32, device=DEV)
+        history, length = i32(rng.integers(0, cfg.vocab, (n, 8)).tolist()), i32([8, 3, 0])
+        rules = V.token_rules(repetition=1.3, frequency=0.2, allowed=allowed, history=history, history_len=length)
+        ws = torch.empty(V.vlac_guided_workspace_bytes(gm.ctx, pool, n), dtype=torch.uint8, device=DEV)
+        toks, logits = torch.zeros((n, n_new), dtype=torch.int32, device=DEV), torch.zeros((n, n_new, cfg.vocab), device=DEV)
+
+        def turn():
+            V.vlac_pages_fork(pool, src, seqs, n)
+            V.vlac_decode_guided(gm.ctx, pool, seqs, n, L, None, n_new, first, rules, toks, logits, ws)
+            V.vlac_pages_free(pool, seqs, n)
+
+        turn()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            turn()
+        for k in range(4):
+            allowed.copy_(gpu(bits(rng.random((n * n_new, cfg.vocab)) < 0.4)))
+            first.copy_(i32(rng.integers(0, cfg.vocab, n).tolist()))
+            graph.replay()
+            got = toks.clone(), logits.clone()
+            turn()
+            assert torch.equal(got[0], toks) and torch.equal(got[1], logits)
+            assert V.vlac_pages_check(pool, check=False) == OK
+    finally:
+        gm.close()
+
+
 def test_refusals():
     import torch
     cfg, L = synth.CONFIGS["tiny"], 40

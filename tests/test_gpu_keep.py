@@ -40,6 +40,11 @@ def test_accept(T, kind, tokens):
         assert path[i] == want + [-1] * (T - len(want)) and count[i] == len(want) and token[i] == after
 
 
+def test_accept_stops_where_nothing_may_follow():
+    path, count, token = accept([[-1, 0, 1, 2], [-1, 0, 0, 2]], [[9, -1, 5, 6], [9, 3, 3, 4]], [[-1, 5, 6, 7], [3, -1, 4, -1]])
+    assert path == [[0, -1, -1, -1], [0, 1, -1, -1]] and count == [1, 2] and token == [-1, -1]
+
+
 class Both:
     """A pool on the GPU and its model, with random values everywhere."""
 

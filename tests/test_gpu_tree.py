@@ -244,3 +244,37 @@ def test_layers_and_strided_queries():
         V.vlac_attend_tree(p, layer, 2, T, hq, q, out, ws)
         want, tol = definition(c, seqs, pos, q, trees, layer)
         assert bool(((out.double() - want).abs() <= tol).all())
+
+
+def test_one_sequence_in_several_entries():
+    """Different trees over the same slots of one sequence, and the same entry twice."""
+    for hq, hkv, hd, T, stem in ((4, 4, 64, 12, 50), (12, 2, 128, 30, 2300)):
+        c = Cache(hkv, hd, 1, seed=T)
+        s, other = c.sequence(stem + T), c.sequence(9 + T)
+        trees = [M.some_tree(k, T, kind) for k, kind in enumerate(("random", "chain", "random", "roots"))]
+        seqs, pos = [s, s, other, s], [stem, stem, 9, stem]
+        p, q = c.pool(), queries(c, 4, T, hq)
+        for group in (None, [1, 1, 2, 2], [0, 1, 2, 3]):
+            compare(c, p, seqs, pos, q, trees, group)
+        q[1] = q[0]                                             # (the order of the sums is each entry's own)
+        compare(c, p, [s, s], [stem, stem], q[:2], [trees[0]] * 2)
+
+
+def test_two_workspaces_on_two_streams():
+    import torch
+    c = Cache(4, 128, 0, seed=2)
+    T, hq = 20, 8
+    pos = [300, 40, 2200]
+    seqs = [c.sequence(x + T) for x in pos]
+    trees = [[M.some_tree(10 * k + i, T) for i in range(3)] for k in range(2)]
+    p = c.pool()
+    q = [queries(c, 3, T, hq) for _ in range(2)]
+    want = [run(p, c, seqs, pos, q[k], trees[k])[0] for k in range(2)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k] = run(p, c, seqs, pos, q[k], trees[k])[0]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(want, got))
