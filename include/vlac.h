@@ -464,7 +464,7 @@ int vlac_rotary_fill(int dims, double base, double factor, double original, doub
  * n_q_heads at most 1024, else unrelated to n_kv_heads.  k, v, kv_stride, and which positions are written or reported: as for
  * vlac_pages_append; an entry whose pos is negative is skipped (its rows of q_out stay), any other has its q_out written.
  * q, k, v, q_out and the gains are 16-byte aligned, strides are multiples of 8.
- * Computed in fp32 (angles in 64 bits), rounded once; beyond fp16's range finite values saturate at +-65504 there.  A head without norm or
+ * n * tokens <= 2^20.  Computed in fp32 (angles in 64 bits), rounded once; beyond fp16's range finite values saturate at +-65504 there.  A head without norm or
  * rotation is copied as it is. */
 int vlac_pages_append_rotated(const vlac_pages* pages, int layer, const int32_t* seqs, const int32_t* pos, int n, int tokens,
                               const vlac_rotary* rot, const int32_t* places, int n_q_heads, const void* q, int64_t q_stride,
