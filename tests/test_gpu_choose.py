@@ -213,3 +213,40 @@ def test_the_binding_checks_sizes():
         V.vlac_choose_tokens(x, V.token_rules(), x, tok[:5], ws)
     with pytest.raises(V.VlacError):
         V.vlac_choose_tokens(x, V.token_rules(), x, tok, ws[:16])
+
+
+@pytest.mark.parametrize("price", [dict(repetition=1.3), dict(repetition=0.25, presence=1e-40), dict(repetition=3.0, frequency=1e-39)])
+def test_the_ends_of_fp32(price):
+    """Subnormal logits and penalties, quotients and products that leave the range."""
+    rng = np.random.default_rng(6)
+    rows, vocab = 3, 3000
+    x = np.exp(rng.uniform(-103, 88.7, (rows, vocab))).astype(F) * rng.choice([-1, 1], (rows, vocab)).astype(F)
+    x[:, :4] = [3e38, -3e38, 1e-45, -1e-45]
+    text = rng.permutation(vocab)[:1500].tolist() + [0, 1, 2, 3]
+    want, token = apply(x, [text] * rows, **price)
+    r = V.token_rules(**price, history=gpu(np.array([text] * rows, np.int32)), history_len=gpu(np.full(rows, len(text), np.int32)))
+    check(x, r, want, token)
+
+
+def test_the_largest_vocabulary():
+    import torch
+    vocab = 1 << 24
+    x = torch.randn((1, vocab), device=DEV)
+    x[0, vocab - 1], x[0, 7] = 99.0, 98.5
+    r = V.token_rules(frequency=1.0, history=gpu(np.array([[vocab - 1, 7, vocab, -1]], np.int32)), history_len=gpu(np.array([1], np.int32)))
+    ws, tok, out = torch.empty(V.vlac_choose_workspace_bytes(1, vocab), dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV), torch.empty_like(x)
+    V.vlac_choose_tokens(x, r, out, tok, ws)
+    assert tok.item() == 7 and out[0, vocab - 1].item() == 98.0 and bool((out[0, :-1] == x[0, :-1]).all())
+    x[0, vocab - 1] = 100.0
+    V.vlac_choose_tokens(x, r, None, tok, ws)
+    assert tok.item() == vocab - 1
+
+
+def test_many_rows():
+    """More rows than a launch of whole pieces would have threads for in one dimension, two tokens each."""
+    import torch
+    rows = 1 << 20
+    x = torch.randn((rows, 2), device=DEV)
+    ws, tok = torch.empty(V.vlac_choose_workspace_bytes(rows, 2), dtype=torch.uint8, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    V.vlac_choose_tokens(x, V.token_rules(), None, tok, ws)
+    assert torch.equal(tok, (x[:, 1] > x[:, 0]).int())

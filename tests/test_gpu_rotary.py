@@ -314,3 +314,27 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(page[layers - 1, which][:, at].permute(1, 0, 2).contiguous().view(torch.float16), k[0])
         page[layers - 1, which][:, at] = 0
     assert not bool(page.any())
+
+
+def test_the_longest_list():
+    """4096 sequences of one token each."""
+    import torch
+    n, hkv, hd = 4096, 2, 64
+    p = V.new_pages(1, hkv, hd, 0, n, n, 1, DEV)
+    data, refs, table, length, _ = p.tensors
+    order = torch.randperm(n, device=DEV).int()
+    table[:, 0], length[:] = order, 1 + torch.arange(n, device=DEV, dtype=torch.int32) % 32
+    refs.fill_(1)
+    seqs = torch.randperm(n, device=DEV).int()
+    pos = length[seqs.long()] - 1
+    q, k, v = (torch.randn((n, 1, h, hd), device=DEV).bfloat16() for h in (3, hkv, hkv))
+    rot, out = V.rotary(hd), torch.empty_like(q)
+    V.vlac_pages_append_rotated(p, 0, seqs, pos, n, 1, rot, None, 3, q, k, v, out)
+    assert V.vlac_pages_check(p, check=False) == OK
+    d = data.view(torch.int16).view(n, 2, hkv, PAGE * hd)[order[seqs.long()].long()]
+    ka, va = (torch.tensor(f(hd), device=DEV)[pos.long()] for f in (k_tile_at, v_tile_at))
+    kk, vv = (torch.gather(d[:, w], 2, at[:, None, :].expand(-1, hkv, -1)).view(torch.bfloat16)[:, None] for w, at in ((0, ka), (1, va)))
+    assert torch.equal(vv, v)
+    for x, got in ((q, out), (k, kk)):
+        want, err = definition(x, pos.long()[:, None], (hd, False, 1.0, rot.tensors[0]), None, 0)
+        near(got, want, err, torch.bfloat16)
