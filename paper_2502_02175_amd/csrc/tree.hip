@@ -49,7 +49,7 @@ struct KeepArgs {
 // them that stay where they are (a path ascends, so all others move).  from, to: where row k comes from and goes to, page * 32 +
 // position in it.  A chain of reads (lists and path, length and table, counts of the pages), about 0.7 us each.
 constexpr int kKeep = 256;
-struct Rows { int from[VLAC_TREE_MAX_NODES], to[VLAC_TREE_MAX_NODES], bad, stay; };
+struct Rows { int from[VLAC_TREE_MAX_NODES], to[VLAC_TREE_MAX_NODES], bad, wrong, stay; };
 __device__ int keep_entry(const KeepArgs& a, int i, Rows& rows, int* stay) {
   constexpr int PER = VLAC_TREE_MAX_NODES / kKeep;
   const PoolView& p = a.p;
@@ -65,7 +65,7 @@ __device__ int keep_entry(const KeepArgs& a, int i, Rows& rows, int* stay) {
   const int l = checked_len(p, s);
   if (tid == 0) {
     rows.bad = l < 0 || m < 0 || m > a.tokens || (long long)p0 + a.tokens != l;
-    rows.stay = 0;
+    rows.wrong = rows.stay = 0;
   }
   bool wrong = false;
   for (int k = tid; k < i; k += kKeep) wrong |= a.seqs[k] == s && a.pos[k] >= 0;
@@ -87,10 +87,10 @@ __device__ int keep_entry(const KeepArgs& a, int i, Rows& rows, int* stay) {
       wrong |= (unsigned)fp >= (unsigned)p.n_pages || (unsigned)gp >= (unsigned)p.n_pages || p.refs[min((unsigned)gp, p.n_pages - 1u)] != 1;
     }
   }
-  if (wrong) rows.bad = 1;
+  if (wrong) rows.wrong = 1;  // (not `bad`, which another wave may still have to look at before it comes to the next barrier)
   __syncthreads();
   *stay = rows.stay;
-  return rows.bad ? -1 : m;
+  return rows.wrong ? -1 : m;
 }
 
 // The rows of the path, one behind the other.  A workgroup takes an entry, a layer and some kv heads; a thread takes 16 bytes of K of

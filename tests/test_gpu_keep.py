@@ -147,6 +147,18 @@ def test_many_entries():
     b.keep(seqs, pos, T, path, [len(x) for x in path])
 
 
+def test_more_work_than_workgroups():
+    """4096 entries of 18 layers: a workgroup takes one after another, some of which do not fit for one row of theirs."""
+    rng = random.Random(2)
+    n, T, layers = 4096, 3, 18
+    b = Both(layers, 1, 64, 1, 2 * n + 8, n, 2)
+    seqs = list(range(n))
+    b.extend(seqs, 30)
+    pos = b.extend(seqs, T)
+    path = [rng.choice([[2], [0, 2], [1, 2], [1], [2, 1], [0, 3], [1, 1], [], [0, 1, 2]]) for _ in seqs]
+    b.keep(seqs, pos, T, path, [len(x) for x in path])
+
+
 def test_offsets_beyond_32_bits():
     import torch
     layers, hkv, hd = 32, 32, 128
