@@ -98,7 +98,7 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   }
   if (COUNTS) {
     constexpr int U = 8;  // of the text's tokens in flight
-    const int n = a.history ? (int)min((long long)max(a.history_len[entry], 0), a.history_stride) : 0;
+    const unsigned n = a.history ? (unsigned)min((long long)max(a.history_len[entry], 0), a.history_stride) : 0u;  // (up to 2^31 - 1)
     const int* text = a.history + entry * a.history_stride;
     for (int k = tid; k < PIECE / 4; k += NT) ((int4*)counts)[k] = make_int4(0, 0, 0, 0);
     if (a.parents)
@@ -108,9 +108,10 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
       }
     __syncthreads();
     auto count = [&](int token) {
-      if ((unsigned)(token - c0) < (unsigned)PIECE) atomicAdd(&counts[token - c0], 1);
+      const unsigned at = (unsigned)token - (unsigned)c0;
+      if (at < (unsigned)PIECE) atomicAdd(&counts[at], 1);
     };
-    for (int k0 = tid; k0 < n; k0 += U * NT) {
+    for (unsigned k0 = tid; k0 < n; k0 += U * NT) {
       int token[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) token[u] = k0 + u * NT < n ? text[k0 + u * NT] : -1;

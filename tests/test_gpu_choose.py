@@ -250,3 +250,20 @@ def test_many_rows():
     ws, tok = torch.empty(V.vlac_choose_workspace_bytes(rows, 2), dtype=torch.uint8, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
     V.vlac_choose_tokens(x, V.token_rules(), None, tok, ws)
     assert torch.equal(tok, (x[:, 1] > x[:, 0]).int())
+
+
+def test_the_longest_text():
+    """2^31 - 1 tokens, 8 GB: the place behind the last turn of the count is beyond 31 bits."""
+    import torch
+    most, vocab = (1 << 31) - 1, 70
+    text = torch.full((1, most), -1, dtype=torch.int32, device=DEV)
+    text[0, 0] = text[0, most - 1] = text[0, 1 << 30] = 9
+    text[0, most - 300] = 69
+    x = torch.zeros((1, vocab), device=DEV)
+    x[0, 9] = 3.5
+    x[0, 8] = 0.25
+    ws, tok = torch.empty(256, dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    want = x.clone()
+    want[0, 9], want[0, 69] = 3.5 - 3 * 1.25, -1.25
+    V.vlac_choose_tokens(x, V.token_rules(frequency=1.25, history=text, history_len=gpu(np.array([most], np.int32))), x, tok, ws)
+    assert torch.equal(x, want) and tok.item() == 8
