@@ -765,12 +765,16 @@ def token_rules(repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=
     if (history is None) != (history_len is None) or (parents is None) != (drafted is None):
         raise ValueError("history and history_len, and parents and drafted, come together")
     if history is not None:
-        r.history, r.history_len, r.history_stride = of_entries(history, "history", 2), of_entries(history_len, "history_len", 1), history.shape[1]
+        at, lengths = of_entries(history, "history", 2), of_entries(history_len, "history_len", 1)
+        if history.shape[1] > 0:   # (else it has no address, and no token)
+            r.history, r.history_len, r.history_stride = at, lengths, history.shape[1]
     r.tokens = 1
     if parents is not None:
         if parents.shape != drafted.shape:
             raise ValueError("parents and drafted differ in shape")
-        r.parents, r.drafted, r.tokens = of_entries(parents, "parents", 2), of_entries(drafted, "drafted", 2), parents.shape[1]
+        r.parents, r.drafted = of_entries(parents, "parents", 2), of_entries(drafted, "drafted", 2)
+        if parents.shape[0] > 0:   # (else they have no address, and there is no row)
+            r.tokens = parents.shape[1]
     r.ref = C.byref(r)
     return r
 

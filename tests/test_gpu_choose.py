@@ -267,3 +267,23 @@ def test_the_longest_text():
     want[0, 9], want[0, 69] = 3.5 - 3 * 1.25, -1.25
     V.vlac_choose_tokens(x, V.token_rules(frequency=1.25, history=text, history_len=gpu(np.array([most], np.int32))), x, tok, ws)
     assert torch.equal(x, want) and tok.item() == 8
+
+
+def test_empty_texts_and_batches():
+    """History without columns is no text (penalties then hit the drafts alone); a batch without entries is nothing to do."""
+    import torch
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)
+    x = torch.tensor([[1.0, 0.5, 0.25], [1.0, 0.5, 2.0]], device=DEV)
+    ws, tok = torch.empty(256, dtype=torch.uint8, device=DEV), i(2)
+    out = torch.empty_like(x)
+    V.vlac_choose_tokens(x, V.token_rules(presence=9.0, history=i(2, 0), history_len=i(2) + 7), out, tok, ws)
+    assert torch.equal(out, x) and tok.tolist() == [0, 2]
+    trees = dict(parents=gpu([[-1, 0]], torch.int32), drafted=gpu([[0, 2]], torch.int32))
+    V.vlac_choose_tokens(x, V.token_rules(presence=9.0, history=i(1, 0), history_len=i(1), **trees), out, tok, ws)
+    assert out.tolist() == [[-8.0, 0.5, 0.25], [-8.0, 0.5, -7.0]] and tok.tolist() == [1, 1]
+    with pytest.raises(ValueError):
+        V.vlac_choose_tokens(x, V.token_rules(history=i(3, 0), history_len=i(3)), out, tok, ws)
+    none = torch.empty((0, 3), device=DEV)
+    V.vlac_choose_tokens(none, V.token_rules(presence=1.0, history=i(0, 4), history_len=i(0), parents=i(0, 5), drafted=i(0, 5)), none, i(0), ws)
+    with pytest.raises(V.VlacError):
+        V.vlac_choose_tokens(x, V.token_rules(parents=i(2, 0), drafted=i(2, 0)), out, tok, ws)
