@@ -290,10 +290,24 @@ __device__ inline void query_key_rows(const RotaryArgs& a, Block& b, int group, 
         widen<F16>(x16[y].z, x[4], x[5]);
         widen<F16>(x16[y].w, x[6], x[7]);
         if (gain) {
-          float sum = 0.f;
+          auto mean_of_squares = [&] {
+            float sum = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-          const float scale = rsqrtf(row_sum<LANES>(sum) * (1.f / HD) + a.eps);
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+            return row_sum<LANES>(sum) * (1.f / HD);
+          };
+          float mean = mean_of_squares() + a.eps;
+          if constexpr (!F16) {
+            // Squares of bf16 leave fp32's range at both ends: once more for such a row, brought nearer to 1 by a power of two
+            // (which all lanes of the row do, and which the quotient does not see)
+            if (__builtin_expect(mean == INFINITY || mean < 0x1p-100f, 0)) {
+              const float nearer = mean == INFINITY ? 0x1p-70f : 0x1p70f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] *= nearer;
+              mean = mean_of_squares() + a.eps * nearer * nearer;
+            }
+          }
+          const float scale = rsqrtf(mean);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = x[e] * scale * g8[e];
         }

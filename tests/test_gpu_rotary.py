@@ -338,3 +338,29 @@ def test_the_longest_list():
     for x, got in ((q, out), (k, kk)):
         want, err = definition(x, pos.long()[:, None], (hd, False, 1.0, rot.tensors[0]), None, 0)
         near(got, want, err, torch.bfloat16)
+
+
+@pytest.mark.parametrize("hd,layout", [(128, V.ROTARY_HALF), (64, V.ROTARY_PAIRS), (64, None)])
+def test_norms_whose_squares_leave_fp32(hd, layout):
+    """bf16 has fp32's range: rows of 2^-120 to 2^126, ordinary ones beside them, and an eps that is far below or far above the squares."""
+    import torch
+    scales = [2.0 ** 126, 2.0 ** 90, 2.0 ** 62, 1.0, 2.0 ** -40, 2.0 ** -62, 2.0 ** -75, 2.0 ** -120]
+    s = Setup(2, hd, 0, [9], len(scales), seed=6)
+    rot = None if layout is None else V.rotary(hd, layout, 1e4)
+    spec = None if rot is None else (hd, layout == V.ROTARY_PAIRS, 1.0, rot.tensors[0])
+    up = torch.tensor(scales, device=DEV, dtype=torch.float64)[None, :, None, None]
+    draw = lambda heads: ((torch.rand((1, len(scales), heads, hd), generator=s.g, device=DEV, dtype=torch.float64) * 2 - 1) * up).to(s.dt)
+    q, k = draw(3), draw(2)
+    gains = s.randn((hd,)), s.randn((hd,))
+    places = i32([list(range(100, 100 + len(scales)))])
+    for eps in (0.0, 2.0 ** -130, 1e-5):
+        out = torch.zeros_like(q)
+        call(s, 0, rot, places, 3, q, k, k, out, gains, eps=eps)
+        kk = s.rows(s.data, 0, 0, 0, range(9, 9 + len(scales)))[None]
+        eps32 = torch.tensor(eps, dtype=torch.float32).double().item()
+        for got, x, gain in ((out, q, gains[0]), (kk, k, gains[1])):
+            want, err = definition(x, places, spec, gain, eps32)
+            near(got, want, err, s.dt)
+    z = torch.zeros_like(q)
+    call(s, 0, rot, places, 3, z, k, k, out, gains, eps=1e-5)
+    assert not bool(out.any())
