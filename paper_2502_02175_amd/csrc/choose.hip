@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "choose.h"
+#include "trees.h"
 
 namespace {
 
@@ -65,7 +66,8 @@ template <bool COUNTS, int PER>
 __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   constexpr int PIECE = NT * PER;
   __shared__ __align__(16) int counts[COUNTS ? PIECE : 4];
-  __shared__ int above[COUNTS ? VLAC_TREE_MAX_NODES : 1];
+  __shared__ short above[COUNTS ? VLAC_TREE_MAX_NODES : 1];
+  __shared__ int drafts[COUNTS ? VLAC_TREE_MAX_NODES : 1];
   __shared__ float sv[NT / 64];
   __shared__ int si[NT / 64];
   read_args(a.logits, a.rows, a.vocab, a.stride, a.out, a.out_stride, a.token, a.token_stride, a.best, a.repetition, a.presence, a.frequency,
@@ -104,7 +106,8 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     if (a.parents)
       for (int t = tid; t < a.tokens; t += NT) {
         const int up = a.parents[(size_t)entry * a.tokens + t];
-        above[t] = up < -2 || up >= t ? -2 : up;
+        drafts[t] = a.drafted[(size_t)entry * a.tokens + t];
+        above[t] = (short)(up < -2 || up >= t ? -2 : up);
       }
     __syncthreads();
     auto count = [&](int token) {
@@ -120,11 +123,12 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     }
     for (int k = tid; k < a.more_n; k += NT) count(a.more[(size_t)entry * a.more_stride + k]);
     if (a.one && tid == 0) count(a.one[entry]);
-    if (a.parents && tid == NT - 64) {
-      int up = node;
-      while (up >= 0) up = above[up];
-      if (up == -1)
-        for (up = node; up >= 0; up = above[up]) count(a.drafted[(size_t)entry * a.tokens + up]);
+    if (a.parents && tid >= NT - 64) {  // (the last wave: the drafts of the row's node and of those above it)
+      uint64_t way;
+      const int end = follow<true>(node, [&](int t) { return t < a.tokens ? (int)above[t] : -2; }, way);
+      if (end == -1)
+        for (int k = 0; 64 * k <= node; ++k)
+          if (part_of(way, k) >> (tid & 63) & 1) count(drafts[64 * k + (tid & 63)]);
     }
     __syncthreads();
   }

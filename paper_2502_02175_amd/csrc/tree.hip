@@ -4,19 +4,21 @@
 #include <type_traits>
 
 #include "pages.h"
+#include "trees.h"
 
 namespace {
 
 // A workgroup takes an entry.  Every node that was drafted as its parent's choice offers itself to the parent, which keeps the
-// first (a minimum: no order decides); then one thread follows the offers from node 0 on, an LDS round trip per node of the path.
+// first (a minimum: no order decides); then a wave follows the offers from node 0 on.  A path ascends (a node's offers come after it), so
+// that a node's place in it is the number of those before it.
 constexpr int kAccept = 256;
 __global__ __launch_bounds__(kAccept) void tree_accept_kernel(const int* __restrict__ parents, const int* __restrict__ drafted,
                                                             const int* __restrict__ chosen, int tokens, int* __restrict__ out_path,
                                                             int* __restrict__ out_count, int* __restrict__ out_token) {
-  __shared__ int pick[VLAC_TREE_MAX_NODES], next[VLAC_TREE_MAX_NODES], path[VLAC_TREE_MAX_NODES];
-  __shared__ int s_count;
+  __shared__ int pick[VLAC_TREE_MAX_NODES], next[VLAC_TREE_MAX_NODES];
   const int tid = threadIdx.x;
   const size_t at = (size_t)blockIdx.x * tokens;
+  const bool begins = parents[at] == -1;
   for (int t = tid; t < tokens; t += kAccept) {
     pick[t] = chosen[at + t];
     next[t] = tokens;
@@ -27,16 +29,21 @@ __global__ __launch_bounds__(kAccept) void tree_accept_kernel(const int* __restr
     if (t > 0 && up >= 0 && up < t && pick[up] >= 0 && drafted[at + t] == pick[up]) atomicMin(&next[up], t);
   }
   __syncthreads();
-  if (tid == 0) {
-    int n = 0;
-    if (parents[at] == -1)
-      for (int t = 0; t < tokens; t = next[t]) path[n++] = t;  // (a node's offers come after it: the path ascends)
-    s_count = n;
-    out_count[blockIdx.x] = n;
-    out_token[blockIdx.x] = n > 0 ? pick[path[n - 1]] : -1;
+  if (tid >= 64) return;
+  uint64_t way = 0;
+  if (begins) follow<false>(0, [&](int t) { return t < tokens && next[t] < tokens ? next[t] : -1; }, way);
+  int n = 0, last = -1;
+  for (int k = 0; 64 * k < tokens; ++k) {
+    const uint64_t part = part_of(way, k);
+    if (part >> tid & 1) out_path[at + n + __popcll(part & ((1ull << tid) - 1))] = 64 * k + tid;
+    n += __popcll(part);
+    if (part) last = 64 * k + 63 - __clzll((long long)part);
   }
-  __syncthreads();
-  for (int t = tid; t < tokens; t += kAccept) out_path[at + t] = t < s_count ? path[t] : -1;
+  for (int t = n + tid; t < tokens; t += 64) out_path[at + t] = -1;
+  if (tid == 0) {
+    out_count[blockIdx.x] = n;
+    out_token[blockIdx.x] = n > 0 ? pick[last] : -1;
+  }
 }
 
 struct KeepArgs {
