@@ -121,49 +121,71 @@ __device__ inline int differs(const int* head, const Made& m) {
   return x;
 }
 
-// The masks of a tree's nodes, and their places in the text.  A workgroup takes an entry: the parents lie in LDS and every node
-// follows them up, twice: to see whether the way ends at the cached sequence, then, word by word (parents come before
-// their nodes, so the bits are met in descending order).  Bound by latency: the lists, then depth x an LDS round trip.
+// The masks of a tree's nodes, and their places in the text.  A workgroup takes an entry.  By doubling: a node has a link, to its parent at
+// first, and the bits of the nodes up to there; every round the bits of the linked node come to its own and the link leads on to that
+// one's, so that a chain of 512 takes 10 rounds.  Bound by latency: the lists, then the rounds.  (Plan of a chain, us, with nodes that
+// are followed up one by one, and so: 64 nodes 11.1 and 7.2, 128 20 and 7.3, 512 110 and 21.8; up to 32 it is hidden behind the plan either way.)
 struct TreeArgs {
   const int* parents;  // nullptr: no trees
   uint32_t* mask;
   int* places;
 };
-__device__ inline void mask_entry(const PoolView& p, const int* seqs, const int* pos, int tokens, const TreeArgs& tree, int i, int* above) {
-  const int tid = threadIdx.x, words = mask_words(tokens);
+// LDS for it: links, then the bits of nodes 32 w .. 32 w + 31 for every node
+__host__ __device__ inline int mask_lds(int tokens) { return tokens * (1 + (tokens + 31) / 32); }
+__device__ inline void mask_entry(const PoolView& p, const int* seqs, const int* pos, int tokens, const TreeArgs& tree, int i, uint32_t* lds) {
+  constexpr int NT = 256, PER = VLAC_TREE_MAX_NODES / NT;
+  const int tid = threadIdx.x, words = mask_words(tokens), own_words = (tokens + 31) / 32;
   const int p0 = pos[i], s = seqs[i];
-  for (int t = tid; t < tokens; t += blockDim.x) above[t] = tree.parents[(size_t)i * tokens + t];
+  int* const links = (int*)lds;
+  uint32_t* const bits = lds + tokens;
+  int link[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) link[u] = tid + u * NT < tokens ? tree.parents[(size_t)i * tokens + tid + u * NT] : -2;
   const int l = checked_len(p, s);
   const bool fits = p0 >= 0 && l >= 0 && (long long)p0 + tokens <= l;
-  for (int t = tid; t < tokens; t += blockDim.x)
-    if (above[t] < -2 || above[t] >= t) {
-      above[t] = -2;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int t = tid + u * NT;
+    if (t >= tokens) break;
+    if (link[u] < -2 || link[u] >= t) {
+      link[u] = -2;
       if (fits) report(p, PAGES_BAD_ENTRY);
     }
-  __syncthreads();
-  const int first = fits ? p0 % kPage : 0;  // bit of node 0
-  for (int t = tid; t < tokens; t += blockDim.x) {
-    const size_t row = (size_t)i * tokens + t;
-    int depth = 0, x = t, up = above[t];
-    while (up >= 0) {
-      ++depth;
-      x = up;
-      up = above[x];
+    links[t] = link[u];
+    for (int w = 0; w < own_words; ++w) bits[w * tokens + t] = w == t >> 5 ? 1u << (t & 31) : 0u;
+  }
+  // (Bits may be read that were written in the same round: they are of nodes above as well.  Links may not.)
+  while (__syncthreads_or(link[0] >= 0 || link[PER - 1] >= 0)) {
+    int further[PER];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      further[u] = link[u] >= 0 ? links[link[u]] : link[u];
+      if (link[u] >= 0)
+        for (int w = 0; w <= link[u] >> 5; ++w) bits[w * tokens + tid + u * NT] |= bits[w * tokens + link[u]];
     }
-    const bool there = fits && up == -1;
-    if (tree.places) tree.places[row] = there ? p0 + depth : -1;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PER; ++u)
+      if (link[u] >= 0) links[tid + u * NT] = link[u] = further[u];
+  }
+  const int first = fits ? p0 % kPage : 0;  // bit of node 0
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int t = tid + u * NT;
+    if (t >= tokens) break;
+    const size_t row = (size_t)i * tokens + t;
+    const bool there = fits && link[u] == -1;
     uint32_t* const out = tree.mask + row * mask_row(tokens);
     out[words] = there;
-    x = there ? t : -1;
-    for (int k = words - 1; k >= 0; --k) {
-      uint32_t bits = 0u;
-      while (x >= 0 && (first + x) / 32 == k) {
-        bits |= 1u << ((first + x) & 31);
-        x = above[x];
-      }
-      if (k == 0 && there) bits |= (1u << first) - 1u;  // cached positions of the same page
-      out[k] = bits;
+    uint32_t before = there ? ~0u : 0u;  // (cached positions of the same page)
+    int nodes = 0;
+    for (int k = 0; k < words; ++k) {
+      const uint32_t now = there && k < own_words ? bits[k * tokens + t] : 0u;
+      out[k] = (uint32_t)(((uint64_t)now << 32 | before) >> (32 - first));
+      before = now;
+      nodes += __popc(now);
     }
+    if (tree.places) tree.places[row] = there ? p0 + nodes - 1 : -1;
   }
 }
 
@@ -224,8 +246,8 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
   if (N <= 128 && blockIdx.x > 0) {  // (a tree's masks: beside the plan)
-    __shared__ int above[VLAC_TREE_MAX_NODES];
-    mask_entry(p, a.seqs, a.pos, a.tokens, a.tree, blockIdx.x - 1, above);
+    extern __shared__ uint32_t tree_lds[];
+    mask_entry(p, a.seqs, a.pos, a.tokens, a.tree, blockIdx.x - 1, tree_lds);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -1304,8 +1326,8 @@ __global__ __launch_bounds__(256) void attend_tree_join_kernel(AttendArgs a) { j
 
 __global__ __launch_bounds__(256) void attend_tree_mask_kernel(PoolView p, const int* __restrict__ seqs, const int* __restrict__ pos, int tokens,
                                                              TreeArgs tree) {
-  __shared__ int above[VLAC_TREE_MAX_NODES];
-  mask_entry(p, seqs, pos, tokens, tree, blockIdx.x, above);
+  extern __shared__ uint32_t tree_lds[];
+  mask_entry(p, seqs, pos, tokens, tree, blockIdx.x, tree_lds);
 }
 
 bool sizes_ok(const vlac_pages* p, int n, int tokens, int n_q_heads) {
@@ -1337,6 +1359,7 @@ static void launch_plan(const PoolView& p, const int* seqs, const int* pos, int 
   const Layout l = layout_of(p, n, tokens, n_q_heads, tree);
   char* b = (char*)ws;
   const TreeArgs masks = {parents, (uint32_t*)(b + l.mask), places};
+  const size_t lds = tree ? sizeof(uint32_t) * mask_lds(tokens) : 0;  // (at most 34 KB)
   const PlanArgs a = {p, made_for(p, n, tokens, n_q_heads, tree), seqs, pos, group, add, n, tokens, n_q_heads, l.part_tiles,
                       (int)l.max_items, l.few ? 16 : 32, (int*)b, (Ent*)(b + l.ent), (Own*)(b + l.own), (Item*)(b + l.item),
                       masks};
@@ -1345,10 +1368,10 @@ static void launch_plan(const PoolView& p, const int* seqs, const int* pos, int 
   // A tree's masks are made by further workgroups of the small kernel, by a launch of their own beside the large one (whose LDS would
   // leave a CU to each of them).
   if (n <= 128 && (long long)n * p.max_pages <= 4096) {
-    hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(tree ? 1 + n : 1), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attend_plan_kernel<256, 128>), dim3(tree ? 1 + n : 1), dim3(256), lds, st, a);
   } else {
     hipLaunchKernelGGL((attend_plan_kernel<1024, VLAC_PAGES_MAX_LIST>), dim3(1), dim3(1024), 0, st, a);
-    if (tree) hipLaunchKernelGGL(attend_tree_mask_kernel, dim3(n), dim3(256), 0, st, p, seqs, pos, tokens, masks);
+    if (tree) hipLaunchKernelGGL(attend_tree_mask_kernel, dim3(n), dim3(256), lds, st, p, seqs, pos, tokens, masks);
   }
 }
 
