@@ -325,7 +325,11 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   const int filled = s_area;  // blocks that last as long as it, x its length
   const bool cut = a.part_tiles > 0 && pages_most > kLong &&
                    (filled < kCus / 2 * s_width || (pages_most > 2 * kLong && filled < kCus * s_width));
-  const int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
+  // Fewer where even the most parts would leave CUs without an item: 9 trees of 2 nodes that share 21184 positions, 12 query heads on
+  // 2 kv heads (4 blocks each), plan and 2 layers 62.3 us by 128 items of 4 blocks, 53.1 by 256 of 2; 32 nodes over 30000, one kv head, 60.9 and 54.7.
+  if (cut)
+    while (log_most > 0 && ((s_blocks / hkv + (1 << log_most) - 1) >> log_most) * hkv * kMaxParts < kCus) --log_most;
   // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
   // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
   // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
