@@ -407,6 +407,15 @@ int vlac_attend_plan(const vlac_pages* pages, const int32_t* seqs, const int32_t
 int vlac_attend_shared(const vlac_pages* pages, int layer, int n, int tokens, int n_q_heads, const void* q,
                        int64_t q_stride, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* How vlac_attend_plan (and vlac_attend_tree_plan) cuts a call's work, for inspection and tests: the rules are evaluated on the
+ * device, these are the same for lists that the host knows.  pos, group (or NULL): host int32 [n], as above (pos negative: the entry is
+ * ignored); common: host int32 [n], of a group's first entry: the pages that its tables have in common.  Results: columns (queries
+ * of a kv head) of a block; places for work items, and how many the workspace holds; block parts that leave their sums to be
+ * joined, and how many the workspace holds.  Of `pages` only the sizes are looked at; needs no GPU.
+ * VLAC_E_NULL / VLAC_E_RANGE / VLAC_E_SHAPE on arguments that the plan does not take. */
+int vlac_plan_attention(const vlac_pages* pages, int n, int tokens, int n_q_heads, const int32_t* pos, const int32_t* group,
+                        const int32_t* common, int* block_columns, int* items, int* items_room, int* parts, int* parts_room);
+
 /* vlac_decode_action for candidates: greedy decode of n_new further tokens for n <= max_batch sequences of a pool,
  * all of length L (imported prefills and their forks; one whose length is another is ignored and
  * reported).  Each continues from its own first token (device int32 [n]: drawn by the caller from the

@@ -8,7 +8,7 @@ from .binding import (VlacError, ModelCfg, LayerW, OPERAND_BF16, OPERAND_F16, OP
                       vlac_profile_read2, vlac_profile_bracket_cost,
                       Pages, pages, new_pages, vlac_page_bytes, vlac_pages_scratch_bytes, vlac_pages_reset, vlac_pages_check,
                       vlac_pages_import, vlac_pages_fork, vlac_pages_extend, vlac_pages_append, vlac_pages_free,
-                      vlac_pages_compact, vlac_attend_workspace_bytes, vlac_attend_plan, vlac_attend_shared,
+                      vlac_pages_compact, vlac_attend_workspace_bytes, vlac_attend_plan, vlac_attend_shared, vlac_plan_attention,
                       vlac_candidates_workspace_bytes, vlac_decode_candidates,
                       Rotary, rotary, ROTARY_HALF, ROTARY_PAIRS, vlac_rotary_fill, vlac_pages_append_rotated, TREE_MAX_NODES,
                       vlac_attend_tree_workspace_bytes, vlac_attend_tree_plan, vlac_attend_tree, TokenRules, token_rules,

@@ -97,6 +97,8 @@ def lib():
         L.vlac_status_string.argtypes = [i32]
         L.vlac_plan_many_rows_gemm.restype = C.c_int
         L.vlac_plan_many_rows_gemm.argtypes = [C.c_int] * 4 + [C.POINTER(C.c_int)] * 3
+        L.vlac_plan_attention.restype = C.c_int
+        L.vlac_plan_attention.argtypes = [C.POINTER(Pages)] + [C.c_int] * 3 + [C.POINTER(C.c_int32)] * 3 + [C.POINTER(C.c_int)] * 5
         L.vlac_plan_unsplit_gemm.restype = C.c_int
         L.vlac_plan_unsplit_gemm.argtypes = [C.c_int] * 3 + [C.POINTER(C.c_int)] * 3
         L.vlac_kv_cache_bytes.restype = C.c_size_t
@@ -588,6 +590,21 @@ def vlac_attend_plan(p, seqs, pos, n, tokens, n_q_heads, group, workspace, strea
     ws, size = _workspace(p, workspace)
     return _call(p, "vlac_attend_plan", stream, check, _ref(p), _list(p, seqs, n, "seqs"), _list(p, pos, n, "pos"), n, tokens,
                  n_q_heads, _list(p, group, n, "group"), ws, size)
+
+
+def vlac_plan_attention(p, tokens, n_q_heads, pos, group, common):
+    """pos, group (or None), common: lists of n whole numbers.  -> columns of a block, (places for work items, room for them), (block
+    parts to join, room for them); no GPU needed."""
+    n = len(pos)
+    if len(common) != n or (group is not None and len(group) != n):
+        raise ValueError("pos, group and common differ in length")
+    lists = [None if x is None else (C.c_int32 * n)(*x) for x in (pos, group, common)]
+    out = [C.c_int() for _ in range(5)]
+    st = lib().vlac_plan_attention(_ref(p), n, tokens, n_q_heads, *lists, *[C.byref(x) for x in out])
+    if st != VLAC_OK:
+        raise VlacError(st, "vlac_plan_attention")
+    cols, items, items_room, parts, parts_room = [x.value for x in out]
+    return cols, (items, items_room), (parts, parts_room)
 
 
 def vlac_attend_shared(p, layer, n, tokens, n_q_heads, q, out, workspace, stream=None, check=True):

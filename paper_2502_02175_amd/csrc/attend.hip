@@ -29,6 +29,7 @@
 // bits per page of its own (32 trees of 24 nodes, 12 on 2 heads, over 304 positions 11.4 us, 2 of 64 over 32801 179 and 6.3 to join).
 #include <algorithm>
 #include <type_traits>
+#include <vector>
 
 #include "pages.h"
 
@@ -221,16 +222,103 @@ __device__ inline Two scan_before(Two x, Two* sums, Two* total) {
   return before;
 }
 
+// The rules by which the plan cuts its work, which vlac_plan_attention shows without a GPU.
+#define VLAC_RULE __host__ __device__ inline
+
+// Lists are cut where they are long and the blocks would not fill the chip (half of it, up to 128 pages) while the longest runs:
+// 4 blocks side by side and a second kernel, instead of many blocks that read the same pages from the L2.  Uncut and cut, us: 20 groups
+// of up to 45 over 2300 positions (16 query heads on 4 of 64) 26 and 35, over 6000 55 and 61; 8 x 19 tokens over 2300 (32 heads of
+// 128) 24 and 31; 24 groups of up to 51 over 6000 (8 on 1 of 128, not quite a chip full of blocks) 87 and 66; up to 64 pages: 8
+// candidates over 1400 (32 heads) 12.4 and 14.9, over 2300 18.8 and 17.2.
+// width: pages before the farthest query; area: blocks that last as long as it, x its length.
+VLAC_RULE bool lists_cut(int part_tiles, int pages_most, int width, int area) {
+  return part_tiles > 0 && pages_most > kLong && (area < kCus / 2 * width || (pages_most > 2 * kLong && area < kCus * width));
+}
+constexpr int kFullArea = kCus << 15;  // (no more than the rule asks for, so that no sum overflows)
+VLAC_RULE int area_of(int blocks, int pages) { return (blocks < 2 * kCus ? blocks : 2 * kCus) * pages; }
+
+// Column blocks side by side in an item (as a power of two, for `blocks` of full width) read their pages together, but have fewer waves each:
+// where the tables have no room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
+VLAC_RULE int side_by_side(bool cut, int block_width, int blocks, int hkv) {
+  int log_most = block_width < 32 ? 0 : cut || blocks > 2 * kCus ? 2 : blocks > kCus ? 1 : 0;
+  // Fewer where even the most parts would leave CUs without an item: 9 trees of 2 nodes that share 21184 positions, 12 query heads on
+  // 2 kv heads (4 blocks each), plan and 2 layers 62.3 us by 128 items of 4 blocks, 53.1 by 256 of 2; 32 nodes over 30000, one kv head, 60.9 and 54.7.
+  if (cut)
+    while (log_most > 0 && ((blocks / hkv + (1 << log_most) - 1) >> log_most) * hkv * kMaxParts < kCus) --log_most;
+  return log_most;
+}
+
+// And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
+// fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
+// of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
+// XCD's runs, below; blocks of 16 for 32 heads: 2 groups of up to 16 over 288 positions 13.2 and 10.0).  Not where lists are cut: those
+// are long, a narrow block reads the shared pages of its list for fewer columns, and its parts take the room of a block's of full width
+// (8 heads on 1, plan and 2 layers, one entry to a block and full width: 16 candidates over 33000 positions 75.6 us and 48.1, 5 over 5000 33.6
+// and 35.0; 4 heads on 1, 48 over 32800 111.6 and 70.6; 12 on 2, 10 over 33000 66.6 and 46.8).
+VLAC_RULE bool may_narrow(bool cut, int log_most, int per_entry, int n_groups, int hkv) {
+  return !cut && log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus;
+}
+VLAC_RULE int blocks_with(int entries, int each) { return (int)(((float)(entries + each - 1) + 0.5f) * (1.f / (float)each)); }
+// blocks(each): of all groups, per kv head.  -> columns of a block
+template <class F>
+VLAC_RULE int narrow_width(int block_width, int per_entry, int hkv, F blocks) {
+  int lo = 1, hi = block_width / per_entry + 1;  // the least that fits, by halving (hi: none does, full width)
+  while (lo < hi) {
+    const int each = (lo + hi) >> 1;
+    if (blocks(each) * hkv <= kCus) hi = each;
+    else lo = each + 1;
+  }
+  return lo * per_entry <= block_width ? lo * per_entry : block_width;
+}
+
 // How a group is cut: column blocks, of which `waves_c` are side by side in an item
 struct Cut { int blocks, waves_c, chunks, wk; };
-__device__ inline Cut cut_of(int cols, int log_most, int width) {
+VLAC_RULE Cut cut_of(int cols, int log_most, int width) {
   Cut x;
   x.blocks = (int)((unsigned)(cols + width - 1) / (unsigned)width);
-  const int log = min(x.blocks >= 3 ? 2 : x.blocks >> 1, log_most);
+  const int by_blocks = x.blocks >= 3 ? 2 : x.blocks >> 1, log = by_blocks < log_most ? by_blocks : log_most;
   x.waves_c = 1 << log;
   x.chunks = (x.blocks + x.waves_c - 1) >> log;
   x.wk = kWaves >> log;
   return x;
+}
+
+// Tiles of the list of a group's block.  (An entry's own tiles are dealt to its blocks as if each had them all; a block of tokens before
+// the last sees fewer.)
+VLAC_RULE int list_tiles(int shared, int own, int entry_blocks, int blocks) {
+  return shared + (int)ceilf((float)own * (float)entry_blocks / (float)(blocks > 1 ? blocks : 1));
+}
+// Parts of a list of so many tiles, where a wave shall have `steps` of them and the workspace has room for `most`: whatever the rules
+// above make of the width, `made` blocks of at most so many parts do not pass it.
+VLAC_RULE int parts_for(int most, int tiles, int steps, int wk) {
+  if (most == 1) return 1;
+  const unsigned per_item = (unsigned)(steps < 1 << 16 ? steps : 1 << 16) * wk;
+  int parts = (int)((tiles + per_item - 1) / per_item);
+  parts = parts < most ? parts : most;
+  parts = parts < kMaxParts ? parts : kMaxParts;
+  return parts > 1 ? parts : 1;
+}
+VLAC_RULE int parts_room(int part_tiles, int made) {
+  const int x = part_tiles / (made > 1 ? made : 1);
+  return x > 1 ? x : 1;
+}
+// Steps of a wave per item: the longest list in 1, 2, ... 64 parts is tried, and what ends first is taken: rounds of one item per CU x (steps
+// + 3 for an item's start and end), + 3 for parts that have to be joined (ties: the fewest parts).
+VLAC_RULE int steps_tried(int longest, int parts) { return (longest + parts - 1) / parts > 1 ? (longest + parts - 1) / parts : 1; }
+VLAC_RULE int cost_of(int items, int most_steps, bool joined) {
+  const float cost = (float)((items + kCus - 1) / kCus) * (float)(most_steps + 3) + (joined ? 3.f : 0.f);
+  return (int)fminf(cost, 1e9f);
+}
+// With many groups (kTryGroups) the chip is full anyhow, and the work per wave is the measure.
+constexpr int kTryGroups = 64;
+VLAC_RULE int steps_by_work(unsigned long long work) {
+  const unsigned long long x = (work + kCus * kWaves - 1) / (kCus * kWaves);
+  return (int)(x < 2 ? 2 : x > 1ull << 30 ? 1ull << 30 : x);
+}
+// Whether every XCD has a run of items of its own, of m runs (items: per kv head)
+VLAC_RULE int xcd_runs(int hkv) { return hkv < 8 && 8 % hkv == 0 ? 8 / hkv : 1; }
+VLAC_RULE bool by_runs(int m, int longest_run, int items, int hkv) {
+  return m > 1 && (longest_run + kCus / 8 - 1) / (kCus / 8) <= (items * hkv + kCus - 1) / kCus && 2 * longest_run * m <= 3 * items;
 }
 
 // One workgroup.  Groups and their common pages, then the cut, then the items.  Memory is asked for in three rounds
@@ -242,7 +330,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __shared__ Two sums[NT / 64];
   __shared__ int g_start[N + 1], g_lead[N], g_shared[N], g_own[N], q_item[N + 1], g_tile[N], l_seq[N], l_pos[N], l_own[N + 1];
   __shared__ unsigned short l_group[N];
-  __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_area, s_own, s_cols;
+  __shared__ int s_run[9], s_bad, s_width, s_steps, s_longest, s_blocks, s_made, s_area, s_own, s_cols;
   __shared__ unsigned long long s_work;
   const PoolView& p = a.p;
   if (N <= 128 && blockIdx.x > 0) {  // (a tree's masks: beside the plan)
@@ -255,7 +343,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
             a.item, p.table, p.len, p.max_seqs, p.max_pages, p.n_kv_heads);
   const int hkv = p.n_kv_heads, grp = a.n_q_heads / hkv, per_entry = a.tokens * grp;  // columns of an entry per kv head
   if (tid == 0) {
-    s_bad = s_width = s_longest = s_blocks = s_area = s_own = 0;
+    s_bad = s_width = s_longest = s_blocks = s_made = s_area = s_own = 0;
     s_work = 0;
   }
   for (int g = tid; g < a.n; g += NT) g_own[g] = 0;
@@ -298,58 +386,33 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
     }
   widest = wave_max(widest);
   auto group_cols = [&](int g) { return (g_start[g + 1] - g_start[g]) * per_entry; };
-  int all_blocks = 0, area = 0;  // (of full width; blocks x pages: no more than the rule below asks for, so that no sum overflows)
-  constexpr int kFull = kCus << 15;
+  int all_blocks = 0, area = 0;  // (of full width)
   for (int g = tid; g < n_groups; g += NT) {
     const int blocks = (group_cols(g) + a.width - 1) / a.width * hkv;
     all_blocks += blocks;
-    area = min(area + min(blocks, 2 * kCus) * g_own[g], kFull);
+    area = min(area + area_of(blocks, g_own[g]), kFullArea);
     g_own[g] = 0;
   }
   all_blocks = wave_sums(all_blocks);
-  area = min(wave_sums(area), kFull);  // (of the last lane: all of them)
+  area = min(wave_sums(area), kFullArea);  // (of the last lane: all of them)
   if (lane == 63) {
     atomicMax(&s_width, widest);
     atomicAdd(&s_blocks, all_blocks);
     atomicAdd(&s_area, area);
   }
   __syncthreads();
-  // Column blocks side by side in an item read their pages together, but have fewer waves each: where the tables have no
-  // room for long lists (no parts) and the blocks do not fill the chip otherwise, each is an item by itself.
-  // Lists are cut where they are long and the blocks would not fill the chip (half of it, up to 128 pages) while the longest runs:
-  // 4 blocks side by side and a second kernel, instead of many blocks that read the same pages from the L2.  Uncut and cut, us: 20 groups
-  // of up to 45 over 2300 positions (16 query heads on 4 of 64) 26 and 35, over 6000 55 and 61; 8 x 19 tokens over 2300 (32 heads of
-  // 128) 24 and 31; 24 groups of up to 51 over 6000 (8 on 1 of 128, not quite a chip full of blocks) 87 and 66; up to 64 pages: 8
-  // candidates over 1400 (32 heads) 12.4 and 14.9, over 2300 18.8 and 17.2.
   const int pages_most = s_width + (a.tokens + kPage - 1) / kPage + 1;
-  const int filled = s_area;  // blocks that last as long as it, x its length
-  const bool cut = a.part_tiles > 0 && pages_most > kLong &&
-                   (filled < kCus / 2 * s_width || (pages_most > 2 * kLong && filled < kCus * s_width));
-  int log_most = a.width < 32 ? 0 : cut || s_blocks > 2 * kCus ? 2 : s_blocks > kCus ? 1 : 0;
-  // Fewer where even the most parts would leave CUs without an item: 9 trees of 2 nodes that share 21184 positions, 12 query heads on
-  // 2 kv heads (4 blocks each), plan and 2 layers 62.3 us by 128 items of 4 blocks, 53.1 by 256 of 2; 32 nodes over 30000, one kv head, 60.9 and 54.7.
-  if (cut)
-    while (log_most > 0 && ((s_blocks / hkv + (1 << log_most) - 1) >> log_most) * hkv * kMaxParts < kCus) --log_most;
-  // And where the chip has room for more blocks than that, a block takes as few whole entries as one round of the chip holds:
-  // fewer own pages are in its list then (up to 8 candidates a group, 6 columns each, 2 kv heads: 8 groups 10.6 us with blocks
-  // of 32 columns, 5 and a third entries, 7.9 with one entry each; 32 groups 11.7, and 10.0 with two entries each and an
-  // XCD's runs, below; blocks of 16 for 32 heads: 2 groups of up to 16 over 288 positions 13.2 and 10.0).
+  const bool cut = lists_cut(a.part_tiles, pages_most, s_width, s_area);
+  const int log_most = side_by_side(cut, a.width, s_blocks, hkv);
   if (w == NT / 64 - 1) {
-    int each = 0;  // entries of a block (0: full width, whatever they are)
-    if (log_most == 0 && per_entry <= 16 && n_groups * hkv <= kCus) {
-      int lo = 1, hi = a.width / per_entry + 1;  // the least that fits, by halving (hi: none does)
-      while (lo < hi) {
-        const int k = (lo + hi) >> 1;
-        const float per = 1.f / (float)k;
+    int cols = a.width;
+    if (may_narrow(cut, log_most, per_entry, n_groups, hkv))
+      cols = narrow_width(a.width, per_entry, hkv, [&](int each) {
         int blocks = 0;
-        for (int g = lane; g < n_groups; g += 64) blocks += (int)(((float)(g_start[g + 1] - g_start[g] + k - 1) + 0.5f) * per);
-        blocks = __builtin_amdgcn_readlane(wave_sums(blocks), 63);
-        if (blocks * hkv <= kCus) hi = k;
-        else lo = k + 1;
-      }
-      each = lo * per_entry <= a.width ? lo : 0;
-    }
-    if (lane == 0) s_cols = each > 0 ? each * per_entry : a.width;
+        for (int g = lane; g < n_groups; g += 64) blocks += blocks_with(g_start[g + 1] - g_start[g], each);
+        return __builtin_amdgcn_readlane(wave_sums(blocks), 63);
+      });
+    if (lane == 0) s_cols = cols;
   }
   // The common pages: every entry's against its group's first.  A wave takes an entry's next 512 pages or, where tables
   // are short, as many entries as they leave lanes for; all of a turn's pages are asked for at once.
@@ -421,14 +484,14 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       }
     }
   }
-  // Work in steps of a wave, a key tile of a column block: tiles of the list of a group's block.  (An entry's own tiles are dealt
-  // to its blocks as if each had them all; a block of tokens before the last sees fewer.)
+  // Work in steps of a wave, a key tile of a column block
   if (cut) {
     unsigned long long work = 0;
-    int longest = 0;
+    int longest = 0, made = 0;
     for (int g = tid; g < n_groups; g += NT) {
       const Cut x = cut_of(group_cols(g), log_most, block_cols);
-      const int tiles = g_shared[g] + (int)ceilf((float)g_own[g] * (float)entry_blocks / (float)max(x.blocks, 1));
+      made += x.blocks * hkv;
+      const int tiles = list_tiles(g_shared[g], g_own[g], entry_blocks, x.blocks);
       g_own[g] = tiles;  // (from here on: of the whole list of a block)
       work += (unsigned long long)x.blocks * tiles * hkv;
       longest = max(longest, (tiles + x.wk - 1) / x.wk);
@@ -436,24 +499,22 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
     longest = wave_max(longest);
-    if (lane == 0) {
+    made = wave_sums(made);  // (of the last lane: all of them)
+    if (lane == 63) {
       atomicAdd(&s_work, work);
       atomicMax(&s_longest, longest);
+      atomicAdd(&s_made, made);
     }
     __syncthreads();
   }
-  // Steps of a wave per item: the lanes of the first wave try the longest list in 1, 2, ... 64 parts, and take what
-  // ends first: rounds of one item per CU x (steps + 3 for an item's start and end), + 3 for parts that have to be joined.
-  // With many groups the chip is full anyhow, and the work per wave is the measure.
-  const int most = cut ? max(1, a.part_tiles / max(s_blocks, 1)) : 1;  // parts that the workspace has room for
+  const int most = cut ? parts_room(a.part_tiles, s_made) : 1;
   auto parts_of = [&](int g, int steps) {
     if (most == 1) return 1;
-    const unsigned per_item = (unsigned)min(steps, 1 << 16) * cut_of(group_cols(g), log_most, block_cols).wk;
-    return max(1, min(min(most, kMaxParts), (int)((g_own[g] + per_item - 1) / per_item)));
+    return parts_for(most, g_own[g], steps, cut_of(group_cols(g), log_most, block_cols).wk);
   };
   if (most > 1 && w == 0) {
-    int steps = max((s_longest + lane) / (lane + 1), 1), best;
-    if (n_groups <= 64) {
+    int steps = steps_tried(s_longest, lane + 1), best;
+    if (n_groups <= kTryGroups) {
       int items = 0, most_steps = 0;  // (the steps that come of it: parts are bounded)
       bool joined = false;
       for (int g = 0; g < n_groups; ++g) {
@@ -463,8 +524,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
         most_steps = max(most_steps, (g_own[g] + parts * x.wk - 1) / (parts * x.wk));
         joined |= parts > 1;
       }
-      const float cost = (float)((items + kCus - 1) / kCus) * (float)(most_steps + 3) + (joined ? 3.f : 0.f);
-      best = (int)fminf(cost, 1e9f);  // (ties: the fewest parts)
+      best = cost_of(items, most_steps, joined);
       int who = lane;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
@@ -473,7 +533,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
       }
       steps = __shfl(steps, who);
     } else {
-      steps = (int)max(2ull, min((s_work + kCus * kWaves - 1) / (kCus * kWaves), 1ull << 30));
+      steps = steps_by_work(s_work);
     }
     if (lane == 0) s_steps = steps;
   }
@@ -484,7 +544,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   // pages belong into one L2.  With 8 kv heads or a multiple of them it is enough that the heads are the fastest index.  With 1, 2
   // or 4 of them the groups are taken residue by residue (mod 8 / heads), and every XCD has a run of items of its own, if
   // the longest run takes no more rounds than the items dealt one by one.
-  const int m = hkv < 8 && 8 % hkv == 0 ? 8 / hkv : 1, whole = n_groups / m, rest = n_groups - whole * m;
+  const int m = xcd_runs(hkv), whole = n_groups / m, rest = n_groups - whole * m;
   auto group_at = [&](int q, int* residue) {  // the q-th group in that order
     *residue = 0;
     if (m == 1) return q;
@@ -519,7 +579,7 @@ __global__ __launch_bounds__(NT) void attend_plan_kernel(PlanArgs a) {
   __syncthreads();
   int longest_run = 0;
   for (int r = 0; r < m; ++r) longest_run = max(longest_run, s_run[r + 1] - s_run[r]);
-  const bool runs = m > 1 && (longest_run + kCus / 8 - 1) / (kCus / 8) <= (items * hkv + kCus - 1) / kCus && 2 * longest_run * m <= 3 * items;
+  const bool runs = by_runs(m, longest_run, items, hkv);
   items *= hkv;
   // Workgroup i takes the items at i, i + grid, ..., so a place is its XCD + 8 x its number there.
   const int places = min(runs ? 8 * longest_run : items, a.max_items);
@@ -1455,7 +1515,100 @@ static int attend_layer(const vlac_pages* pages, int layer, int n, int tokens, i
   return hipGetLastError() == hipSuccess ? VLAC_OK : VLAC_E_HIP;
 }
 
+// The plan's rules over lists that the host knows: the same steps as the kernel's, group by group
+static void host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const int* pos, const int* group, const int* common,
+                      int* block_cols, long long* places, size_t* places_room, long long* tiles, int* tiles_room) {
+  struct Group { int first, entries, shared, own, tiles; };
+  const Layout l = layout_of(p, n, tokens, n_q_heads, false);
+  const int hkv = p.n_kv_heads, grp = n_q_heads / hkv, per_entry = tokens * grp, full = l.few ? 16 : 32;
+  std::vector<Group> groups;
+  int width = 0, blocks = 0, area = 0;
+  for (int i = 0; i < n;) {
+    Group g = {i, 0, 0x7fffffff, 0, 0};
+    int farthest = 0;
+    for (; i < n && (i == g.first || (group ? group[i] : 0) == (group ? group[g.first] : 0)); ++i, ++g.entries)
+      if (pos[i] >= 0) {
+        g.shared = std::min(g.shared, pos[i] / kPage);
+        farthest = std::max(farthest, pos[i] / kPage);
+      }
+    g.shared = g.shared == 0x7fffffff ? 0 : std::min(g.shared, std::max(common[g.first], 0));
+    for (int k = g.first; k < i; ++k)
+      if (pos[k] >= 0) g.own += (pos[k] + tokens + kPage - 1) / kPage - g.shared;
+    width = std::max(width, farthest);
+    const int b = (g.entries * per_entry + full - 1) / full * hkv;
+    blocks += b;
+    area = std::min(area + area_of(b, farthest), kFullArea);
+    groups.push_back(g);
+  }
+  const int n_groups = (int)groups.size(), pages_most = width + (tokens + kPage - 1) / kPage + 1;
+  const bool cut = lists_cut(l.part_tiles, pages_most, width, area);
+  const int log_most = side_by_side(cut, full, blocks, hkv);
+  int cols = full;
+  if (may_narrow(cut, log_most, per_entry, n_groups, hkv))
+    cols = narrow_width(full, per_entry, hkv, [&](int each) {
+      int x = 0;
+      for (const Group& g : groups) x += blocks_with(g.entries, each);
+      return x;
+    });
+  auto cut_group = [&](const Group& g) { return cut_of(g.entries * per_entry, log_most, cols); };
+  unsigned long long work = 0;
+  int longest = 0, made = 0;
+  for (Group& g : groups) {
+    const Cut x = cut_group(g);
+    made += x.blocks * hkv;
+    g.tiles = list_tiles(g.shared, g.own, (per_entry + cols - 1) / cols, x.blocks);
+    work += (unsigned long long)x.blocks * g.tiles * hkv;
+    longest = std::max(longest, (g.tiles + x.wk - 1) / x.wk);
+  }
+  const int most = cut ? parts_room(l.part_tiles, made) : 1;
+  int steps = steps_by_work(work), least = 0x7fffffff;
+  for (int tried = 1; tried <= 64 && n_groups <= kTryGroups; ++tried) {
+    const int s = steps_tried(longest, tried);
+    int items = 0, most_steps = 0;
+    bool joined = false;
+    for (const Group& g : groups) {
+      const Cut x = cut_group(g);
+      const int parts = parts_for(most, g.tiles, s, x.wk);
+      items += hkv * x.chunks * parts;
+      most_steps = std::max(most_steps, (g.tiles + parts * x.wk - 1) / (parts * x.wk));
+      joined |= parts > 1;
+    }
+    const int cost = cost_of(items, most_steps, joined);
+    if (cost < least) { least = cost; steps = s; }
+  }
+  const int m = xcd_runs(hkv);
+  int run[8] = {0}, items = 0;
+  *tiles = 0;
+  for (int g = 0; g < n_groups; ++g) {
+    const Cut x = cut_group(groups[g]);
+    const int parts = parts_for(most, groups[g].tiles, steps, x.wk);
+    items += x.chunks * parts;
+    run[g % m] += x.chunks * parts;
+    if (parts > 1) *tiles += (long long)hkv * x.blocks * parts;
+  }
+  const int longest_run = *std::max_element(run, run + m);
+  *block_cols = cols;
+  *places = by_runs(m, longest_run, items, hkv) ? 8LL * longest_run : (long long)items * hkv;
+  *places_room = l.max_items;
+  *tiles_room = l.part_tiles;
+}
+
 extern "C" {
+
+int vlac_plan_attention(const vlac_pages* pages, int n, int tokens, int n_q_heads, const int32_t* pos, const int32_t* group,
+                        const int32_t* common, int* block_columns, int* items, int* items_room, int* parts, int* parts_room) {
+  if (!pos || !common || !block_columns || !items || !items_room || !parts || !parts_room) return VLAC_E_NULL;
+  const int rc = check_pages(pages, false);
+  if (rc != VLAC_OK) return rc;
+  if (n < 1 || !sizes_ok(pages, n, tokens, n_q_heads)) return n_q_heads >= 1 && n_q_heads % pages->n_kv_heads ? VLAC_E_SHAPE : VLAC_E_RANGE;
+  for (int i = 0; i < n; ++i)
+    if (pos[i] >= 0 && (long long)pos[i] + tokens > (long long)pages->max_pages * kPage) return VLAC_E_RANGE;
+  long long places, tiles;
+  size_t room;
+  host_plan(pool_view(pages), n, tokens, n_q_heads, pos, group, common, block_columns, &places, &room, &tiles, parts_room);
+  *items = (int)places; *items_room = (int)room; *parts = (int)tiles;
+  return VLAC_OK;
+}
 
 size_t vlac_attend_workspace_bytes(const vlac_pages* pages, int n, int tokens, int n_q_heads) {
   if (check_pages(pages, false) != VLAC_OK || !sizes_ok(pages, n, tokens, n_q_heads)) return 0;
