@@ -132,7 +132,6 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     }
     __syncthreads();
   }
-  float* const out = a.out ? a.out + row * a.out_stride : nullptr;
   float best = -INFINITY;
   int best_u = -1;
 #pragma unroll
