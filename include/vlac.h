@@ -412,7 +412,7 @@ int vlac_attend_shared(const vlac_pages* pages, int layer, int n, int tokens, in
  * ignored); common: host int32 [n], of a group's first entry: the pages that its tables have in common.  Results: columns (queries
  * of a kv head) of a block; places for work items, and how many the workspace holds; block parts that leave their sums to be
  * joined, and how many the workspace holds.  Of `pages` only the sizes are looked at; needs no GPU.
- * VLAC_E_NULL / VLAC_E_RANGE / VLAC_E_SHAPE on arguments that the plan does not take. */
+ * VLAC_E_NULL / VLAC_E_RANGE / VLAC_E_SHAPE on arguments that the plan does not take, VLAC_E_NOMEM without host memory. */
 int vlac_plan_attention(const vlac_pages* pages, int n, int tokens, int n_q_heads, const int32_t* pos, const int32_t* group,
                         const int32_t* common, int* block_columns, int* items, int* items_room, int* parts, int* parts_room);
 

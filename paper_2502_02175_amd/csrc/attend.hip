@@ -28,8 +28,9 @@
 // Trees of drafted tokens are the same with another mask: a node sees the cached positions and the nodes above it, a word of
 // bits per page of its own (32 trees of 24 nodes, 12 on 2 heads, over 304 positions 11.4 us, 2 of 64 over 32801 179 and 6.3 to join).
 #include <algorithm>
+#include <memory>
+#include <new>
 #include <type_traits>
-#include <vector>
 
 #include "pages.h"
 
@@ -1516,13 +1517,14 @@ static int attend_layer(const vlac_pages* pages, int layer, int n, int tokens, i
 }
 
 // The plan's rules over lists that the host knows: the same steps as the kernel's, group by group
-static void host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const int* pos, const int* group, const int* common,
-                      int* block_cols, long long* places, size_t* places_room, long long* tiles, int* tiles_room) {
+static int host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const int* pos, const int* group, const int* common,
+                     int* block_cols, long long* places, size_t* places_room, long long* tiles, int* tiles_room) {
   struct Group { int first, entries, shared, own, tiles; };
   const Layout l = layout_of(p, n, tokens, n_q_heads, false);
   const int hkv = p.n_kv_heads, grp = n_q_heads / hkv, per_entry = tokens * grp, full = l.few ? 16 : 32;
-  std::vector<Group> groups;
-  int width = 0, blocks = 0, area = 0;
+  const std::unique_ptr<Group[]> groups(new (std::nothrow) Group[n]);
+  if (!groups) return VLAC_E_NOMEM;
+  int n_groups = 0, width = 0, blocks = 0, area = 0;
   for (int i = 0; i < n;) {
     Group g = {i, 0, 0x7fffffff, 0, 0};
     int farthest = 0;
@@ -1538,22 +1540,23 @@ static void host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const
     const int b = (g.entries * per_entry + full - 1) / full * hkv;
     blocks += b;
     area = std::min(area + area_of(b, farthest), kFullArea);
-    groups.push_back(g);
+    groups[n_groups++] = g;
   }
-  const int n_groups = (int)groups.size(), pages_most = width + (tokens + kPage - 1) / kPage + 1;
+  const int pages_most = width + (tokens + kPage - 1) / kPage + 1;
   const bool cut = lists_cut(l.part_tiles, pages_most, width, area);
   const int log_most = side_by_side(cut, full, blocks, hkv);
   int cols = full;
   if (may_narrow(cut, log_most, per_entry, n_groups, hkv))
     cols = narrow_width(full, per_entry, hkv, [&](int each) {
       int x = 0;
-      for (const Group& g : groups) x += blocks_with(g.entries, each);
+      for (int g = 0; g < n_groups; ++g) x += blocks_with(groups[g].entries, each);
       return x;
     });
   auto cut_group = [&](const Group& g) { return cut_of(g.entries * per_entry, log_most, cols); };
   unsigned long long work = 0;
   int longest = 0, made = 0;
-  for (Group& g : groups) {
+  for (int k = 0; k < n_groups; ++k) {
+    Group& g = groups[k];
     const Cut x = cut_group(g);
     made += x.blocks * hkv;
     g.tiles = list_tiles(g.shared, g.own, (per_entry + cols - 1) / cols, x.blocks);
@@ -1566,7 +1569,8 @@ static void host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const
     const int s = steps_tried(longest, tried);
     int items = 0, most_steps = 0;
     bool joined = false;
-    for (const Group& g : groups) {
+    for (int k = 0; k < n_groups; ++k) {
+      const Group& g = groups[k];
       const Cut x = cut_group(g);
       const int parts = parts_for(most, g.tiles, s, x.wk);
       items += hkv * x.chunks * parts;
@@ -1591,6 +1595,7 @@ static void host_plan(const PoolView& p, int n, int tokens, int n_q_heads, const
   *places = by_runs(m, longest_run, items, hkv) ? 8LL * longest_run : (long long)items * hkv;
   *places_room = l.max_items;
   *tiles_room = l.part_tiles;
+  return VLAC_OK;
 }
 
 extern "C" {
@@ -1605,7 +1610,8 @@ int vlac_plan_attention(const vlac_pages* pages, int n, int tokens, int n_q_head
     if (pos[i] >= 0 && (long long)pos[i] + tokens > (long long)pages->max_pages * kPage) return VLAC_E_RANGE;
   long long places, tiles;
   size_t room;
-  host_plan(pool_view(pages), n, tokens, n_q_heads, pos, group, common, block_columns, &places, &room, &tiles, parts_room);
+  const int st = host_plan(pool_view(pages), n, tokens, n_q_heads, pos, group, common, block_columns, &places, &room, &tiles, parts_room);
+  if (st != VLAC_OK) return st;
   *items = (int)places; *items_room = (int)room; *parts = (int)tiles;
   return VLAC_OK;
 }
