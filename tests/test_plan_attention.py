@@ -76,7 +76,7 @@ def test_rules():
     assert plan(6, 1, 8, 9)[0] == 6 and plan(6, 1, 600, 9)[0] == 16
     # 32 kv heads x 16 entries: 512 blocks of one entry are more than a round, 256 of two are one
     assert plan(32, 32, 16, 9)[0] == 2
-    # 1 block of 32 heads over 1025 pages is cut: 8 items to a CU's share of 256 at most, none of less than a step for each wave
+    # one block for each of 32 heads over 1025 pages: 8 parts of it make a round of 256 items
     cols, (items, _), (parts, room) = plan(32, 32, 8, 1025)
     assert cols == 32 and parts == items == 256 and room == 2048
     # lists of up to 64 pages are left whole
